@@ -77,7 +77,7 @@ def draw(rng):
     B, causal = rng.choice([1, 2, 3]), rng.random() < 0.4
     most = 1.2e9 if dtype == "bf16" else 2e8
     while True:
-        Lk = _log(rng, 1, 32760)
+        Lk = _log(rng, 2 if train else 1, 32760)     # over one key, p is 1 and dq is 0: nothing to compare
         Lq = _ragged(max(1, Lk - rng.choice([0, 0, 1, 100, -7]))) if causal else _log(rng, 1, 16380)
         if B * H_kv * group * Lq * Lk <= most:
             break
