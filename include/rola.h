@@ -400,6 +400,156 @@ rola_status_t rola_attention_block(const rola_config_t* cfg, const void* X, cons
 rola_status_t rola_lowrank_summary_static(const rola_config_t* cfg, const void* k, const void* v,
                                           const void* P_k, float* C, float* z, void* stream);
 
+/* ------------------------------------------------------------------------
+ * The rest of a transformer block around the module: the norm before each
+ * sub-layer, softmax attention over a dense key set (cross-attention, a causal
+ * sequence, a single new token) and the gated feed-forward, each with its
+ * backward pass.  The conventions above hold: device pointers, 16-byte aligned
+ * where not said otherwise, densely packed, nothing allocated, asynchronous
+ * on `stream`.  Every reduction has a fixed order: the same call gives the same
+ * bits.
+ */
+
+/*
+ * Layer norm of each row of x, with the affine map of each channel:
+ *   mu = mean_i x_i,  rstd = (mean_i (x_i - mu)^2 + eps)^(-1/2)
+ *   y_i = (x_i - mu) rstd gamma_i + beta_i
+ * The variance is taken about the row's mean (two passes over the row, which
+ * stays in registers), in fp32 whatever the dtype.
+ *   x     : [rows][d], dtype;  gamma, beta : [d], dtype, or NULL (1 and 0)
+ *   y     : out, [rows][d], dtype; may be x
+ *   mean, rstd : out, fp32 [rows], what the backward pass reads; or both NULL
+ * Any rows >= 1 and 1 <= d <= 2^20; x, gamma, beta and y need their element's alignment only
+ * (with d a multiple of 16 bytes and 16-byte aligned pointers the wide path
+ * runs).  eps >= 0.
+ */
+rola_status_t rola_layer_norm(int64_t rows, int32_t d, rola_dtype_t dtype, const void* x, const void* gamma,
+                              const void* beta, float eps, void* y, float* mean, float* rstd, void* stream);
+
+/* Bytes of workspace rola_layer_norm_backward needs (256-byte aligned); 0 if the sizes are invalid. */
+size_t rola_layer_norm_backward_workspace_bytes(int64_t rows, int32_t d, rola_dtype_t dtype);
+
+/*
+ * Gradients of rola_layer_norm, with xh = (x - mu) rstd and a = dy gamma:
+ *   dx = rstd (a - mean_i a_i - xh mean_i (a_i xh_i))
+ *   dgamma_i = sum_rows dy_i xh_i,   dbeta_i = sum_rows dy_i
+ *   x, gamma, mean, rstd : as rola_layer_norm read and wrote them
+ *   dy     : [rows][d], dtype;  dx : out, [rows][d], dtype; may be dy
+ *   dgamma, dbeta : out, fp32 [d], or both NULL
+ * The rows are summed per CTA and the CTAs' sums in a fixed order, all in fp32.
+ */
+rola_status_t rola_layer_norm_backward(int64_t rows, int32_t d, rola_dtype_t dtype, const void* x, const void* gamma,
+                                       const float* mean, const float* rstd, const void* dy, void* dx, float* dgamma,
+                                       float* dbeta, void* ws, size_t ws_bytes, void* stream);
+
+/* Sizes of a gated feed-forward.  Fill with rola_ffn_config_init, then set the sizes. */
+typedef struct {
+    int32_t tokens;            /* rows of X, >= 1 */
+    int32_t d_model, d_ff;     /* widths, multiples of 8, at most 2^20 */
+    int32_t act;               /* phi, one of rola_lowrank_act_t; default ROLA_LOWRANK_ACT_SILU */
+    rola_dtype_t dtype;        /* ROLA_BF16 (default) or ROLA_FP32 */
+    int32_t wait_limit_ms;     /* bound of every device-side wait (0 = 2000 ms); at most 60000 */
+    int32_t debug_flags;       /* 0 normally.  ROLA_DEBUG_SKIP_FIRST_K_COPY makes each CTA of the bf16
+                                  products skip its first load, so a bounded wait runs out and the call
+                                  reports ROLA_ERR_TIMEOUT (tests the timeout path) */
+} rola_ffn_config_t;
+
+/* Fill *cfg with defaults (sizes zero).  Returns ROLA_ERR_INVALID_ARG on NULL. */
+rola_status_t rola_ffn_config_init(rola_ffn_config_t* cfg);
+
+/* Bytes of workspace rola_ffn / rola_ffn_train and rola_ffn_backward need (256-byte aligned; its
+ * first bytes hold the status word rola_get_device_status reads); 0 if cfg is invalid. */
+size_t rola_ffn_workspace_bytes(const rola_ffn_config_t* cfg);
+size_t rola_ffn_backward_workspace_bytes(const rola_ffn_config_t* cfg);
+
+/*
+ * Gated feed-forward:
+ *   G = X W_gate^T,  U = X W_up^T,  H = phi(G) * U,  Y = H W_down^T
+ * Both projections, phi and the product are one kernel: G and U stay in fp32
+ * on chip and only H is written (rounded once to dtype).
+ *   X : [tokens][d_model];  W_gate, W_up : [d_ff][d_model];  W_down : [d_model][d_ff]
+ *       (the nn.Linear layout), all cfg->dtype
+ *   Y : out, [tokens][d_model], cfg->dtype
+ */
+rola_status_t rola_ffn(const rola_ffn_config_t* cfg, const void* X, const void* W_gate, const void* W_up,
+                       const void* W_down, void* Y, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * rola_ffn for training: also writes G and U (fp32 [tokens][d_ff]), which
+ * rola_ffn_backward reads.  They are kept in fp32: the gradients multiply them,
+ * and two more bf16 roundings would show in every gradient.
+ */
+rola_status_t rola_ffn_train(const rola_ffn_config_t* cfg, const void* X, const void* W_gate, const void* W_up,
+                             const void* W_down, void* Y, float* G, float* U, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Gradients of the gated feed-forward:
+ *   dH = dY W_down,  dG = dH * U * phi'(G),  dU = dH * phi(G)
+ *   dX = dG W_gate + dU W_up
+ *   dW_gate = dG^T X,  dW_up = dU^T X,  dW_down = dY^T H
+ * phi' of ROLA_LOWRANK_ACT_RELU at 0 is 0.  dH stays in fp32 on chip; dG, dU and
+ * H are rounded once to dtype, as the operands of the products after them.
+ *   X, W_*, G, U : as rola_ffn_train read and wrote them;  dY : [tokens][d_model]
+ *   dX : out, [tokens][d_model];  dW_* : out, the shapes of W_*; all cfg->dtype
+ */
+rola_status_t rola_ffn_backward(const rola_ffn_config_t* cfg, const void* X, const void* W_gate, const void* W_up,
+                                const void* W_down, const float* G, const float* U, const void* dY, void* dX,
+                                void* dW_gate, void* dW_up, void* dW_down, void* ws, size_t ws_bytes, void* stream);
+
+/* Sizes of an attention over a dense key set.  Fill with rola_attention_config_init, then set the sizes. */
+typedef struct {
+    int32_t B, H, H_kv;        /* batch, query heads, key heads; H_kv divides H: query head h reads key head
+                                  h / (H / H_kv) */
+    int32_t Lq, Lk, d_h;       /* queries, keys (both >= 1), head dim (d_h == 128) */
+    int32_t causal;            /* 1: query i of a sequence with n keys sees keys j <= i + n - Lq (the last
+                                  query sees every key); 0: every query sees every key */
+    float scale;               /* of the scores; 0 (default) = 1 / sqrt(d_h) */
+    rola_dtype_t dtype;        /* ROLA_BF16 (default) or ROLA_FP32 */
+    int32_t wait_limit_ms;     /* bound of every device-side wait (0 = 2000 ms); at most 60000 */
+    int32_t debug_flags;       /* as rola_ffn_config_t */
+} rola_attention_config_t;
+
+/* Fill *cfg with defaults (sizes zero).  Returns ROLA_ERR_INVALID_ARG on NULL. */
+rola_status_t rola_attention_config_init(rola_attention_config_t* cfg);
+
+/* Bytes of workspace rola_attention and rola_attention_backward need (256-byte aligned; its first
+ * bytes hold the status word); 0 if cfg is invalid. */
+size_t rola_attention_workspace_bytes(const rola_attention_config_t* cfg);
+size_t rola_attention_backward_workspace_bytes(const rola_attention_config_t* cfg);
+
+/*
+ * Softmax attention over the keys each query sees:
+ *   o_i = sum_j p_ij v_j,  p_ij = exp(s_ij - lse_i),  s_ij = scale q_i . k_j,
+ *   lse_i = log sum_j exp(s_ij)
+ * over j < kv_len[b], and with `causal` j <= i + kv_len[b] - Lq.  A query that
+ * sees no key (kv_len 0, or an early causal query) has o = 0 and lse = -inf.
+ * Keys past kv_len take no part whatever they hold (NaN and infinities too).
+ * The running maximum and sum are fp32; bf16 rounds p once, as the operand of
+ * the product with v.  Few queries over many keys: the keys are split over
+ * CTAs and the parts joined in a fixed order.
+ *   q      : [B][H][Lq][d_h];  k, v : [B][H_kv][Lk][d_h], dtype (already rotated
+ *            where positions matter)
+ *   kv_len : int32 [B] on the device, or NULL (all Lk); values outside
+ *            [0, Lk] are clamped to it
+ *   o      : out, [B][H][Lq][d_h], dtype, not overlapping q;  lse : out, fp32 [B][H][Lq], or NULL
+ */
+rola_status_t rola_attention(const rola_attention_config_t* cfg, const void* q, const void* k, const void* v,
+                             const int32_t* kv_len, void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Gradients of rola_attention.  The probabilities are recomputed from q, k and
+ * lse, tile by tile; nothing of size Lq x Lk is kept.
+ *   D_i = dO_i . o_i,  dp_ij = dO_i . v_j,  ds_ij = scale p_ij (dp_ij - D_i)
+ *   dv_j = sum_i p_ij dO_i,  dq_i = sum_j ds_ij k_j,  dk_j = sum_i ds_ij q_i
+ * dk and dv are summed over the query heads that share a key head; they are 0 at
+ * the keys no query sees, and dq is 0 for a query that sees no key.
+ *   q, k, v, kv_len, o, lse : as rola_attention read and wrote them
+ *   dO : [B][H][Lq][d_h];  dq : out, as q;  dk, dv : out, as k and v; dtype
+ */
+rola_status_t rola_attention_backward(const rola_attention_config_t* cfg, const void* q, const void* k, const void* v,
+                                      const int32_t* kv_len, const void* o, const float* lse, const void* dO, void* dq,
+                                      void* dk, void* dv, void* ws, size_t ws_bytes, void* stream);
+
 /*
  * Synchronises `stream`, then reads the device status word at the start of
  * ws: ROLA_OK, or ROLA_ERR_TIMEOUT if a bounded device wait expired since the

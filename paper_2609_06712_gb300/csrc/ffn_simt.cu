@@ -1,0 +1,249 @@
+// The gated feed-forward's products in plain fp32 arithmetic (no tensor
+// cores): the fp32 mode.
+//
+//   H = phi(X Wg^T) * (X Wu^T),  Y = H Wd^T
+//   dG, dU, H from dH = dY Wd;  dX = dG Wg + dU Wu;  dWg = dG^T X,  dWu = dU^T X,  dWd = dY^T H
+//
+// One kernel computes C(m, n) = sum_k A(m, k) B(n, k) for 128 x 128 tiles, 256
+// threads with 8 x 8 outputs each (two groups of four rows and of four columns,
+// so that shared memory is read in 16-byte words without conflicts: 4 words for
+// 64 fused multiply-adds), K in steps of 16, the next step's words loaded into
+// registers under the present step's arithmetic.  Each operand is contiguous
+// along k or along m / n.  The B tile of the gate + up kernel is 64 rows of Wg
+// and the same 64 rows of Wu, so that a thread holds g and u of the same
+// features (columns tx*4 .. and 64 + tx*4 ..) and phi and the product need no
+// exchange.  Bound by fp32 FMA issue.
+#include "block_ops.cuh"
+
+namespace rola {
+namespace {
+
+constexpr int kTile = 128, kStep = 16, kPad = 132;
+
+enum Epilogue { kStore, kGateUp, kGateGrad };
+
+// An operand: element (i, k) at p[i * ld + k] (k contiguous) or p[k * ld + i].
+// ld and the contiguous extent are multiples of 8 elements, p is 16-byte aligned.
+template <typename T>
+struct Operand {
+    const T* p;
+    int rows;                    // extent of i
+    int ld;
+};
+
+struct Args {
+    int M, N, K, sources, act;
+    int ldc;
+    const float *G_in, *U_in;
+    float *G, *U;
+    void *C, *C2, *C3;
+};
+
+// This thread's 8 elements of a 128 x 16 tile: along k, row t / 2 and k = 8 (t % 2); along i, k = t / 16 and
+// rows 8 (t % 16).  Elements outside the operand are 0.
+template <typename T, bool KC>
+__device__ __forceinline__ void fetch(const Operand<T>& o, int i0, int k0, int K, float (&x)[8])
+{
+    const int t = threadIdx.x;
+    const int i = KC ? i0 + t / 2 : i0 + (t % 16) * 8, k = KC ? k0 + (t % 2) * 8 : k0 + t / 16;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+    // the contiguous extent is a multiple of 8, so the 8 elements are all inside or all outside
+    if (i < o.rows && k < K) {
+        const T* p = KC ? o.p + (size_t)i * o.ld + k : o.p + (size_t)k * o.ld + i;
+        const float4 a = load4(p), b = load4(p + 4);
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    }
+}
+template <bool KC>
+__device__ __forceinline__ void stage(float (*s)[kPad], const float (&x)[8])
+{
+    const int t = threadIdx.x;
+    if constexpr (KC) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[(t % 2) * 8 + e][t / 2] = x[e];
+    } else {
+        *reinterpret_cast<float4*>(&s[t / 16][(t % 16) * 8]) = make_float4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<float4*>(&s[t / 16][(t % 16) * 8 + 4]) = make_float4(x[4], x[5], x[6], x[7]);
+    }
+}
+
+// The B tile of kGateUp: rows 0-63 from b0, 64-127 from b1, the same 64 features.
+template <typename T, bool BK, int E>
+__device__ __forceinline__ void fetch_b(const Operand<T>& b0, const Operand<T>& b1, int n0, int k0, int K, float (&x)[8])
+{
+    if constexpr (E == kGateUp) {
+        static_assert(BK, "the weights are contiguous along k");
+        const bool up = threadIdx.x >= 128;
+        fetch<T, true>(up ? b1 : b0, up ? n0 - 64 : n0, k0, K, x);
+    } else {
+        fetch<T, BK>(b0, n0, k0, K, x);
+    }
+}
+
+template <typename T, bool AK, bool BK, int E>
+__global__ void __launch_bounds__(256, 2) simt_gemm_kernel(Operand<T> a0, Operand<T> b0, Operand<T> a1, Operand<T> b1,
+                                                           const Args p)
+{
+    __shared__ __align__(16) float as[2][kStep][kPad];
+    __shared__ __align__(16) float bs[2][kStep][kPad];
+    const int m0 = blockIdx.y * kTile, n0 = blockIdx.x * (E == kGateUp ? 64 : kTile);
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    float acc[8][8] = {};
+    const int steps = (p.K + kStep - 1) / kStep, total = steps * p.sources;
+    float xa[8], xb[8];
+    auto next = [&](int s) {
+        const bool second = s >= steps;                // dX: the second product of the sum
+        const int k0 = (second ? s - steps : s) * kStep;
+        fetch<T, AK>(second ? a1 : a0, m0, k0, p.K, xa);
+        if constexpr (E == kGateUp) fetch_b<T, BK, E>(b0, b1, n0, k0, p.K, xb);
+        else fetch_b<T, BK, E>(second ? b1 : b0, b1, n0, k0, p.K, xb);
+    };
+    next(0);
+    stage<AK>(as[0], xa);
+    stage<BK>(bs[0], xb);
+    __syncthreads();
+    for (int s = 0; s < total; ++s) {
+        if (s + 1 < total) next(s + 1);
+        const int cur = s & 1;
+#pragma unroll
+        for (int k = 0; k < kStep; ++k) {
+            float a[8], b[8];
+            *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(&as[cur][k][ty * 4]);
+            *reinterpret_cast<float4*>(a + 4) = *reinterpret_cast<const float4*>(&as[cur][k][64 + ty * 4]);
+            *reinterpret_cast<float4*>(b) = *reinterpret_cast<const float4*>(&bs[cur][k][tx * 4]);
+            *reinterpret_cast<float4*>(b + 4) = *reinterpret_cast<const float4*>(&bs[cur][k][64 + tx * 4]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+        }
+        if (s + 1 < total) {
+            stage<AK>(as[cur ^ 1], xa);                // last read before the previous barrier
+            stage<BK>(bs[cur ^ 1], xb);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int m = m0 + (i < 4 ? ty * 4 + i : 60 + ty * 4 + i);
+        if (m >= p.M) continue;
+        if constexpr (E == kGateUp) {
+            const int n = n0 + tx * 4;                 // N is a multiple of 8
+            if (n < p.N) {
+                const size_t at = (size_t)m * p.ldc + n;
+                const float4 g = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+                const float4 u = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
+                store4(static_cast<T*>(p.C) + at,
+                       make_float4(gate_act(p.act, g.x) * u.x, gate_act(p.act, g.y) * u.y, gate_act(p.act, g.z) * u.z,
+                                   gate_act(p.act, g.w) * u.w));
+                if (p.G) {
+                    store4(p.G + at, g);
+                    store4(p.U + at, u);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int n = n0 + h * 64 + tx * 4;
+                if (n >= p.N) continue;
+                const size_t at = (size_t)m * p.ldc + n;
+                const float* c = &acc[i][4 * h];
+                if constexpr (E == kStore) {
+                    store4(static_cast<T*>(p.C) + at, make_float4(c[0], c[1], c[2], c[3]));
+                } else {
+                    const float4 g4 = load4(p.G_in + at), u4 = load4(p.U_in + at);
+                    const float g[4] = {g4.x, g4.y, g4.z, g4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
+                    float hh[4], dg[4], du[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float ph, dph;
+                        gate_act_grad(p.act, g[e], ph, dph);
+                        hh[e] = ph * u[e];
+                        dg[e] = c[e] * u[e] * dph;
+                        du[e] = c[e] * ph;
+                    }
+                    store4(static_cast<T*>(p.C) + at, make_float4(hh[0], hh[1], hh[2], hh[3]));
+                    store4(static_cast<T*>(p.C2) + at, make_float4(dg[0], dg[1], dg[2], dg[3]));
+                    store4(static_cast<T*>(p.C3) + at, make_float4(du[0], du[1], du[2], du[3]));
+                }
+            }
+        }
+    }
+}
+
+template <typename T, bool AK, bool BK, int E>
+cudaError_t gemm(Operand<T> a0, Operand<T> b0, Operand<T> a1, Operand<T> b1, const Args& p, cudaStream_t st)
+{
+    const int nt = E == kGateUp ? 64 : kTile;
+    const dim3 grid((p.N + nt - 1) / nt, (p.M + kTile - 1) / kTile);
+    simt_gemm_kernel<T, AK, BK, E><<<grid, 256, 0, st>>>(a0, b0, a1, b1, p);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+template <typename T>
+cudaError_t launch_ffn_up_simt(const FfnShape& s, const void* X, const void* Wg, const void* Wu, void* H, float* G,
+                               float* U, cudaStream_t st)
+{
+    Args p{};
+    p.M = s.M; p.N = s.F; p.K = s.D; p.sources = 1; p.act = s.act; p.ldc = s.F;
+    p.C = H; p.G = G; p.U = U;
+    const Operand<T> x{static_cast<const T*>(X), s.M, s.D};
+    return gemm<T, true, true, kGateUp>(x, {static_cast<const T*>(Wg), s.F, s.D}, x,
+                                        {static_cast<const T*>(Wu), s.F, s.D}, p, st);
+}
+
+template <typename T>
+cudaError_t launch_ffn_down_simt(const FfnShape& s, const void* H, const void* Wd, void* Y, cudaStream_t st)
+{
+    Args p{};
+    p.M = s.M; p.N = s.D; p.K = s.F; p.sources = 1; p.ldc = s.D;
+    p.C = Y;
+    const Operand<T> h{static_cast<const T*>(H), s.M, s.F}, w{static_cast<const T*>(Wd), s.D, s.F};
+    return gemm<T, true, true, kStore>(h, w, h, w, p, st);
+}
+
+template <typename T>
+cudaError_t launch_ffn_backward_simt(const FfnShape& s, const void* X, const void* Wg, const void* Wu, const void* Wd,
+                                     const float* G, const float* U, const void* dY, void* H, void* dG, void* dU,
+                                     void* dX, void* dWg, void* dWu, void* dWd, cudaStream_t st)
+{
+    auto op = [](const void* p, int rows, int ld) { return Operand<T>{static_cast<const T*>(p), rows, ld}; };
+    Args p{};
+    p.M = s.M; p.N = s.F; p.K = s.D; p.sources = 1; p.act = s.act; p.ldc = s.F;
+    p.G_in = G; p.U_in = U; p.C = H; p.C2 = dG; p.C3 = dU;
+    cudaError_t e = gemm<T, true, false, kGateGrad>(op(dY, s.M, s.D), op(Wd, s.F, s.F), op(dY, s.M, s.D),
+                                                    op(Wd, s.F, s.F), p, st);
+    if (e != cudaSuccess) return e;
+    p = Args{};
+    p.M = s.M; p.N = s.D; p.K = s.F; p.sources = 2; p.ldc = s.D; p.C = dX;
+    e = gemm<T, true, false, kStore>(op(dG, s.M, s.F), op(Wg, s.D, s.D), op(dU, s.M, s.F), op(Wu, s.D, s.D), p, st);
+    if (e != cudaSuccess) return e;
+    // the weights' gradients: both operands contiguous along their output index, k = token
+    const struct { const void *a, *b; int m, n; void* c; } w[3] = {
+        {dG, X, s.F, s.D, dWg}, {dU, X, s.F, s.D, dWu}, {dY, H, s.D, s.F, dWd}};
+    for (const auto& g : w) {
+        p = Args{};
+        p.M = g.m; p.N = g.n; p.K = s.M; p.sources = 1; p.ldc = g.n; p.C = g.c;
+        e = gemm<T, false, false, kStore>(op(g.a, g.m, g.m), op(g.b, g.n, g.n), op(g.a, g.m, g.m), op(g.b, g.n, g.n),
+                                          p, st);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+#define ROLA_INSTANTIATE(T)                                                                                          \
+    template cudaError_t launch_ffn_up_simt<T>(const FfnShape&, const void*, const void*, const void*, void*,        \
+                                               float*, float*, cudaStream_t);                                        \
+    template cudaError_t launch_ffn_down_simt<T>(const FfnShape&, const void*, const void*, void*, cudaStream_t);    \
+    template cudaError_t launch_ffn_backward_simt<T>(const FfnShape&, const void*, const void*, const void*,         \
+                                                     const void*, const float*, const float*, const void*, void*,    \
+                                                     void*, void*, void*, void*, void*, void*, cudaStream_t);
+ROLA_INSTANTIATE(float)
+ROLA_INSTANTIATE(__nv_bfloat16)
+#undef ROLA_INSTANTIATE
+
+}  // namespace rola

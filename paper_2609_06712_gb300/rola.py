@@ -43,6 +43,25 @@ class RolaConfig(ctypes.Structure):
     ]
 
 
+class RolaFfnConfig(ctypes.Structure):
+    """Mirror of rola_ffn_config_t."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "d_model", "d_ff", "act", "dtype", "wait_limit_ms",
+                                              "debug_flags")]
+
+
+class RolaAttentionConfig(ctypes.Structure):
+    """Mirror of rola_attention_config_t."""
+    _fields_ = [
+        ("B", ctypes.c_int32), ("H", ctypes.c_int32), ("H_kv", ctypes.c_int32),
+        ("Lq", ctypes.c_int32), ("Lk", ctypes.c_int32), ("d_h", ctypes.c_int32),
+        ("causal", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("dtype", ctypes.c_int32),
+        ("wait_limit_ms", ctypes.c_int32),
+        ("debug_flags", ctypes.c_int32),
+    ]
+
+
 ROLA_DEBUG_SKIP_FIRST_K_COPY = 1
 # rola_lowrank_rope_t: where the truncated RoPE sits in the low-rank features
 ROLA_LOWRANK_ROPE_OUTSIDE, ROLA_LOWRANK_ROPE_INSIDE, ROLA_LOWRANK_ROPE_NONE = 0, 1, 2
@@ -68,7 +87,9 @@ def _load():
                           "(the RoLA module has no CPU fallback)")
     lib = ctypes.CDLL(LIB_PATH)
     P, S = ctypes.c_void_p, ctypes.c_size_t
+    I32, I64 = ctypes.c_int32, ctypes.c_int64
     cfgp = ctypes.POINTER(RolaConfig)
+    ffnp, attnp = ctypes.POINTER(RolaFfnConfig), ctypes.POINTER(RolaAttentionConfig)
     st = ctypes.c_int
     sig = {
         "rola_config_init": (st, [cfgp]),
@@ -89,6 +110,20 @@ def _load():
         "rola_gate": (st, [cfgp, P, P, ctypes.c_float, ctypes.c_int32, P, P]),
         "rola_out_proj": (st, [cfgp, P, P, P, ctypes.c_int32, P, P, S, P]),
         "rola_attention_block": (st, [cfgp, P, P, ctypes.c_float, ctypes.c_int32] + [P] * 12 + [S, P]),
+        "rola_layer_norm": (st, [I64, I32, I32, P, P, P, ctypes.c_float, P, P, P, P]),
+        "rola_layer_norm_backward_workspace_bytes": (S, [I64, I32, I32]),
+        "rola_layer_norm_backward": (st, [I64, I32, I32] + [P] * 9 + [S, P]),
+        "rola_ffn_config_init": (st, [ffnp]),
+        "rola_ffn_workspace_bytes": (S, [ffnp]),
+        "rola_ffn_backward_workspace_bytes": (S, [ffnp]),
+        "rola_ffn": (st, [ffnp] + [P] * 6 + [S, P]),
+        "rola_ffn_train": (st, [ffnp] + [P] * 8 + [S, P]),
+        "rola_ffn_backward": (st, [ffnp] + [P] * 12 + [S, P]),
+        "rola_attention_config_init": (st, [attnp]),
+        "rola_attention_workspace_bytes": (S, [attnp]),
+        "rola_attention_backward_workspace_bytes": (S, [attnp]),
+        "rola_attention": (st, [attnp] + [P] * 7 + [S, P]),
+        "rola_attention_backward": (st, [attnp] + [P] * 11 + [S, P]),
         "rola_get_device_status": (st, [P, P]),
         "rola_status_string": (ctypes.c_char_p, [st]),
     }
@@ -255,6 +290,155 @@ def forward_timed(c, q, k, v, P_q, P_k, gate, o, kv_idx_out, ws, events, stream=
            "rola_forward_timed")
 
 
+# ---------------------------------------------------------------- the block around the module
+
+_DTYPES = {torch.bfloat16: ROLA_BF16, torch.float32: ROLA_FP32}
+_TORCH_DTYPES = {v: k for k, v in _DTYPES.items()}
+
+
+def _dtype_of(t, where: str) -> int:
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"{where}: tensors must be bfloat16 or float32, not {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _expect(where: str, dtype, **tensors):
+    """Each tensor=(t, shape) is of `dtype` and of that shape; a None tensor is left to the library."""
+    for name, (t, shape) in tensors.items():
+        if t is not None and (t.dtype != dtype or tuple(t.shape) != shape):
+            raise ValueError(f"{where}: {name} must be {dtype} of shape {shape}, not {t.dtype} {tuple(t.shape)}")
+
+
+def _bytes(n: int, where: str, device) -> torch.Tensor:
+    if n == 0:
+        raise RolaError(ROLA_ERR_INVALID_ARG, where)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _rows_of(x):
+    d = x.shape[-1]
+    return (x.numel() // d if d else 0), d
+
+
+def layer_norm(x, gamma, beta, eps: float, y, mean=None, rstd=None, stream=None):
+    """y = (x - mean) rstd gamma + beta over the last axis of x; gamma and beta [d] in x's dtype or None.
+    mean and rstd (fp32, one per row), if given, receive what layer_norm_backward reads."""
+    w, (rows, d) = "rola_layer_norm", _rows_of(x)
+    dt = _dtype_of(x, w)
+    _expect(w, x.dtype, gamma=(gamma, (d,)), beta=(beta, (d,)), y=(y, tuple(x.shape)))
+    _expect(w, torch.float32, mean=(mean, tuple(x.shape[:-1])), rstd=(rstd, tuple(x.shape[:-1])))
+    _check(_lib.rola_layer_norm(rows, d, dt, _p(x), _p(gamma), _p(beta), eps, _p(y), _p(mean), _p(rstd),
+                                _stream(stream)), w)
+
+
+def layer_norm_backward_workspace(x) -> torch.Tensor:
+    w, (rows, d) = "rola_layer_norm_backward_workspace_bytes", _rows_of(x)
+    return _bytes(_lib.rola_layer_norm_backward_workspace_bytes(rows, d, _dtype_of(x, w)), w, x.device)
+
+
+def layer_norm_backward(x, gamma, mean, rstd, dy, dx, dgamma, dbeta, ws, stream=None):
+    """dx of layer_norm, and dgamma, dbeta (fp32 [d], or both None)."""
+    w, (rows, d) = "rola_layer_norm_backward", _rows_of(x)
+    dt = _dtype_of(x, w)
+    _expect(w, x.dtype, gamma=(gamma, (d,)), dy=(dy, tuple(x.shape)), dx=(dx, tuple(x.shape)))
+    _expect(w, torch.float32, mean=(mean, tuple(x.shape[:-1])), rstd=(rstd, tuple(x.shape[:-1])),
+            dgamma=(dgamma, (d,)), dbeta=(dbeta, (d,)))
+    _check(_lib.rola_layer_norm_backward(rows, d, dt, _p(x), _p(gamma), _p(mean), _p(rstd), _p(dy), _p(dx), _p(dgamma),
+                                         _p(dbeta), _p(ws), ws.numel(), _stream(stream)), w)
+
+
+def make_ffn_config(tokens: int, d_model: int, d_ff: int, act="silu", dtype: int = ROLA_BF16) -> RolaFfnConfig:
+    """rola_ffn_config_t of a gated feed-forward; act is a name in LOWRANK_ACTS or its number."""
+    c = RolaFfnConfig()
+    _lib.rola_ffn_config_init(ctypes.byref(c))
+    c.tokens, c.d_model, c.d_ff, c.dtype = tokens, d_model, d_ff, dtype
+    c.act = LOWRANK_ACTS[act] if isinstance(act, str) else int(act)
+    return c
+
+
+def ffn_workspace(c: RolaFfnConfig, device="cuda") -> torch.Tensor:
+    return _bytes(_lib.rola_ffn_workspace_bytes(ctypes.byref(c)), "rola_ffn_workspace_bytes", device)
+
+
+def ffn_backward_workspace(c: RolaFfnConfig, device="cuda") -> torch.Tensor:
+    return _bytes(_lib.rola_ffn_backward_workspace_bytes(ctypes.byref(c)), "rola_ffn_backward_workspace_bytes", device)
+
+
+def _expect_ffn(w, c, X, W_gate, W_up, W_down, **rows):
+    m, d, f = (c.tokens, c.d_model), (c.d_ff, c.d_model), (c.d_model, c.d_ff)
+    _expect(w, _TORCH_DTYPES.get(c.dtype), X=(X, m), W_gate=(W_gate, d), W_up=(W_up, d), W_down=(W_down, f),
+            **{n: (t, m) for n, t in rows.items()})
+
+
+def ffn(c, X, W_gate, W_up, W_down, Y, ws, stream=None):
+    """Y = (phi(X W_gate^T) * (X W_up^T)) W_down^T; X, Y [tokens][d_model], weights in the nn.Linear layout."""
+    _expect_ffn("rola_ffn", c, X, W_gate, W_up, W_down, Y=Y)
+    _check(_lib.rola_ffn(ctypes.byref(c), _p(X), _p(W_gate), _p(W_up), _p(W_down), _p(Y), _p(ws), ws.numel(),
+                         _stream(stream)), "rola_ffn")
+
+
+def ffn_train(c, X, W_gate, W_up, W_down, Y, G, U, ws, stream=None):
+    """ffn keeping G = X W_gate^T and U = X W_up^T (fp32 [tokens][d_ff]) for ffn_backward."""
+    w, kept = "rola_ffn_train", (c.tokens, c.d_ff)
+    _expect_ffn(w, c, X, W_gate, W_up, W_down, Y=Y)
+    _expect(w, torch.float32, G=(G, kept), U=(U, kept))
+    _check(_lib.rola_ffn_train(ctypes.byref(c), _p(X), _p(W_gate), _p(W_up), _p(W_down), _p(Y), _p(G), _p(U), _p(ws),
+                               ws.numel(), _stream(stream)), w)
+
+
+def ffn_backward(c, X, W_gate, W_up, W_down, G, U, dY, dX, dW_gate, dW_up, dW_down, ws, stream=None):
+    """Gradients of ffn_train: dX and the three weights', in the weights' dtype."""
+    w, kept = "rola_ffn_backward", (c.tokens, c.d_ff)
+    _expect_ffn(w, c, X, W_gate, W_up, W_down, dY=dY, dX=dX)
+    _expect_ffn(w, c, X, dW_gate, dW_up, dW_down)
+    _expect(w, torch.float32, G=(G, kept), U=(U, kept))
+    _check(_lib.rola_ffn_backward(ctypes.byref(c), _p(X), _p(W_gate), _p(W_up), _p(W_down), _p(G), _p(U), _p(dY),
+                                  _p(dX), _p(dW_gate), _p(dW_up), _p(dW_down), _p(ws), ws.numel(), _stream(stream)), w)
+
+
+def make_attention_config(B: int, H: int, H_kv: int, Lq: int, Lk: int, causal: bool = False, scale: float = 0.0,
+                          dtype: int = ROLA_BF16) -> RolaAttentionConfig:
+    """rola_attention_config_t; scale 0 is 1 / sqrt(d_h)."""
+    c = RolaAttentionConfig()
+    _lib.rola_attention_config_init(ctypes.byref(c))
+    c.B, c.H, c.H_kv, c.Lq, c.Lk, c.causal, c.scale, c.dtype = B, H, H_kv, Lq, Lk, int(causal), scale, dtype
+    return c
+
+
+def attention_workspace(c: RolaAttentionConfig, device="cuda") -> torch.Tensor:
+    return _bytes(_lib.rola_attention_workspace_bytes(ctypes.byref(c)), "rola_attention_workspace_bytes", device)
+
+
+def attention_backward_workspace(c: RolaAttentionConfig, device="cuda") -> torch.Tensor:
+    return _bytes(_lib.rola_attention_backward_workspace_bytes(ctypes.byref(c)),
+                  "rola_attention_backward_workspace_bytes", device)
+
+
+def _expect_attention(w, c, queries, keys, kv_len, lse):
+    rows, cols = (c.B, c.H, c.Lq, c.d_h), (c.B, c.H_kv, c.Lk, c.d_h)
+    _expect(w, _TORCH_DTYPES.get(c.dtype), **{n: (t, rows) for n, t in queries.items()},
+            **{n: (t, cols) for n, t in keys.items()})
+    _expect(w, torch.int32, kv_len=(kv_len, (c.B,)))
+    _expect(w, torch.float32, lse=(lse, rows[:3]))
+
+
+def attention(c, q, k, v, kv_len, o, lse, ws, stream=None):
+    """o = softmax(scale q k^T) v over the first kv_len[b] keys (int32 [B]; None: all), causal if c.causal;
+    q, o [B][H][Lq][128], k, v [B][H_kv][Lk][128].  lse (fp32 [B][H][Lq]) is what attention_backward reads."""
+    w = "rola_attention"
+    _expect_attention(w, c, dict(q=q, o=o), dict(k=k, v=v), kv_len, lse)
+    _check(_lib.rola_attention(ctypes.byref(c), _p(q), _p(k), _p(v), _p(kv_len), _p(o), _p(lse), _p(ws), ws.numel(),
+                               _stream(stream)), w)
+
+
+def attention_backward(c, q, k, v, kv_len, o, lse, dO, dq, dk, dv, ws, stream=None):
+    """Gradients of attention from its o and lse; the probabilities are recomputed."""
+    w = "rola_attention_backward"
+    _expect_attention(w, c, dict(q=q, o=o, dO=dO, dq=dq), dict(k=k, v=v, dk=dk, dv=dv), kv_len, lse)
+    _check(_lib.rola_attention_backward(ctypes.byref(c), _p(q), _p(k), _p(v), _p(kv_len), _p(o), _p(lse), _p(dO),
+                                        _p(dq), _p(dk), _p(dv), _p(ws), ws.numel(), _stream(stream)), w)
+
+
 def get_device_status(ws, stream=None) -> int:
     return _lib.rola_get_device_status(_p(ws), _stream(stream))
 
@@ -318,3 +502,76 @@ class RoLAFunction(torch.autograd.Function):
         backward(c, q, k, v, P_q, P_k, gate, kv, o_s, lse, C, dO, dq, dk, dv, dP_q, dP_k, dgate, ws)
         return None, dq, dk, dv, dP_q.to(P_q.dtype), dP_k.to(P_k.dtype), dgate
 
+
+
+class LayerNormFunction(torch.autograd.Function):
+    """Layer norm over the last axis as a differentiable torch op: ``apply(x, gamma, beta, eps)``;
+    gamma and beta are both tensors or both None."""
+
+    @staticmethod
+    def forward(ctx, x, gamma, beta, eps):
+        x = x.contiguous()
+        y = torch.empty_like(x)
+        mean, rstd = (torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) for _ in range(2))
+        layer_norm(x, gamma, beta, eps, y, mean, rstd)
+        ctx.save_for_backward(x, gamma, mean, rstd)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, gamma, mean, rstd = ctx.saved_tensors
+        dx, dgamma, dbeta = torch.empty_like(x), None, None
+        if gamma is not None:
+            dgamma, dbeta = (torch.empty_like(gamma, dtype=torch.float32) for _ in range(2))
+        layer_norm_backward(x, gamma, mean, rstd, dy.contiguous(), dx, dgamma, dbeta, layer_norm_backward_workspace(x))
+        if gamma is not None:
+            dgamma, dbeta = dgamma.to(gamma.dtype), dbeta.to(gamma.dtype)
+        return dx, dgamma, dbeta, None
+
+
+class FfnFunction(torch.autograd.Function):
+    """The gated feed-forward as a differentiable torch op: ``apply(X, W_gate, W_up, W_down, act)``;
+    X [..., d_model]."""
+
+    @staticmethod
+    def forward(ctx, X, W_gate, W_up, W_down, act):
+        x = X.contiguous().view(-1, X.shape[-1])
+        c = make_ffn_config(x.shape[0], x.shape[1], W_gate.shape[0], act, _dtype_of(x, "rola_ffn"))
+        Y = torch.empty_like(x)
+        G, U = (torch.empty((c.tokens, c.d_ff), dtype=torch.float32, device=x.device) for _ in range(2))
+        ffn_train(c, x, W_gate, W_up, W_down, Y, G, U, ffn_workspace(c, x.device))
+        ctx.c = c
+        ctx.save_for_backward(x, W_gate, W_up, W_down, G, U)
+        return Y.view(X.shape)
+
+    @staticmethod
+    def backward(ctx, dY):
+        x, W_gate, W_up, W_down, G, U = ctx.saved_tensors
+        dX, dWg, dWu, dWd = (torch.empty_like(t) for t in (x, W_gate, W_up, W_down))
+        ffn_backward(ctx.c, x, W_gate, W_up, W_down, G, U, dY.contiguous().view_as(x), dX, dWg, dWu, dWd,
+                     ffn_backward_workspace(ctx.c, x.device))
+        return dX.view(dY.shape), dWg, dWu, dWd, None
+
+
+class AttentionFunction(torch.autograd.Function):
+    """Attention over a dense key set as a differentiable torch op: ``apply(q, k, v, kv_len, causal)``;
+    kv_len int32 [B] or None."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, kv_len, causal):
+        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+        B, H, Lq, _ = q.shape
+        c = make_attention_config(B, H, k.shape[1], Lq, k.shape[2], causal, dtype=_dtype_of(q, "rola_attention"))
+        o, lse = torch.empty_like(q), torch.empty((B, H, Lq), dtype=torch.float32, device=q.device)
+        attention(c, q, k, v, kv_len, o, lse, attention_workspace(c, q.device))
+        ctx.c = c
+        ctx.save_for_backward(q, k, v, kv_len, o, lse)
+        return o
+
+    @staticmethod
+    def backward(ctx, dO):
+        q, k, v, kv_len, o, lse = ctx.saved_tensors
+        dq, dk, dv = (torch.empty_like(t) for t in (q, k, v))
+        attention_backward(ctx.c, q, k, v, kv_len, o, lse, dO.contiguous(), dq, dk, dv,
+                           attention_backward_workspace(ctx.c, q.device))
+        return dq, dk, dv, None, None
