@@ -21,8 +21,7 @@ constexpr int kT = 64, kRow = 132, kPRow = 68;
 constexpr int kTileF = kT * kRow, kPF = kT * kPRow;      // floats of an operand tile, of a 64 x 64 tile
 
 // rows [r0, r0 + 64) of a [n][128] matrix, zeros past n
-template <typename T>
-__device__ __forceinline__ void load_tile(float* s, const T* p, int r0, int n)
+__device__ __forceinline__ void load_tile(float* s, const float* p, int r0, int n)
 {
     for (int e = threadIdx.x; e < kT * 32; e += 256) {
         const int r = e / 32, c = (e % 32) * 4;
@@ -93,8 +92,7 @@ __device__ __forceinline__ float row_sum(float x)
     return x;
 }
 
-template <typename T>
-__device__ __forceinline__ void store_row(T* p, int tx, const float (&x)[8])
+__device__ __forceinline__ void store_row(float* p, int tx, const float (&x)[8])
 {
     store4(p + tx * 4, make_float4(x[0], x[1], x[2], x[3]));
     store4(p + 64 + tx * 4, make_float4(x[4], x[5], x[6], x[7]));
@@ -102,7 +100,6 @@ __device__ __forceinline__ void store_row(T* p, int tx, const float (&x)[8])
 
 // grid (row tiles, heads, splits).  Part z of n parts takes the key tiles [z t / n, (z + 1) t / n) of the
 // t that the row tile sees.
-template <typename T>
 __global__ void __launch_bounds__(256) attention_simt_kernel(const AttnShape s, const AttnArgs a)
 {
     extern __shared__ __align__(16) float sm[];
@@ -113,8 +110,8 @@ __global__ void __launch_bounds__(256) attention_simt_kernel(const AttnShape s, 
     const int last = min(r0 + kT, s.R) - 1;
     const int tiles = (attn_seen_most(s, len, r0, last) + kT - 1) / kT;
     const int t0 = (int)((long long)tiles * blockIdx.z / s.splits), t1 = (int)((long long)tiles * (blockIdx.z + 1) / s.splits);
-    const T *q = static_cast<const T*>(a.q) + (size_t)head * s.R * kDh, *k = static_cast<const T*>(a.k) + (size_t)head * s.Lk * kDh,
-            *v = static_cast<const T*>(a.v) + (size_t)head * s.Lk * kDh;
+    const float *q = static_cast<const float*>(a.q) + (size_t)head * s.R * kDh, *k = static_cast<const float*>(a.k) + (size_t)head * s.Lk * kDh,
+            *v = static_cast<const float*>(a.v) + (size_t)head * s.Lk * kDh;
     load_tile(Q, q, r0, s.R);
     float m[4], l[4], o[4][8] = {};
     int seen[4];
@@ -172,7 +169,7 @@ __global__ void __launch_bounds__(256) attention_simt_kernel(const AttnShape s, 
             store_row(a.part_o + at * kDh, tx, o[i]);
             if (tx == 0) a.part_lse[at] = lse;
         } else {
-            store_row(static_cast<T*>(a.o) + row * kDh, tx, o[i]);
+            store_row(static_cast<float*>(a.o) + row * kDh, tx, o[i]);
             if (a.lse && tx == 0) a.lse[row] = lse;
         }
     }
@@ -244,7 +241,6 @@ __device__ __forceinline__ void grad_tile(const AttnShape& s, const float* Q, co
 }
 
 // grid (row tiles, heads)
-template <typename T>
 __global__ void __launch_bounds__(256) attention_dq_simt_kernel(const AttnShape s, const AttnArgs a)
 {
     extern __shared__ __align__(16) float sm[];
@@ -254,8 +250,8 @@ __global__ void __launch_bounds__(256) attention_dq_simt_kernel(const AttnShape 
     const int len = attn_len(s, a.kv_len, b);
     const int tiles = (attn_seen_most(s, len, r0, min(r0 + kT, s.R) - 1) + kT - 1) / kT;
     const size_t qh = (size_t)head * s.R * kDh, kh = (size_t)head * s.Lk * kDh;
-    load_tile(Q, static_cast<const T*>(a.q) + qh, r0, s.R);
-    load_tile(dO, static_cast<const T*>(a.dO) + qh, r0, s.R);
+    load_tile(Q, static_cast<const float*>(a.q) + qh, r0, s.R);
+    load_tile(dO, static_cast<const float*>(a.dO) + qh, r0, s.R);
     float lse[4], D[4], dq[4][8] = {};
     int seen[4];
 #pragma unroll
@@ -268,8 +264,8 @@ __global__ void __launch_bounds__(256) attention_dq_simt_kernel(const AttnShape 
     }
     for (int t = 0; t < tiles; ++t) {
         __syncthreads();
-        load_tile(K, static_cast<const T*>(a.k) + kh, t * kT, len);
-        load_tile(V, static_cast<const T*>(a.v) + kh, t * kT, len);
+        load_tile(K, static_cast<const float*>(a.k) + kh, t * kT, len);
+        load_tile(V, static_cast<const float*>(a.v) + kh, t * kT, len);
         __syncthreads();
         Grad4 g;
         grad_tile(s, Q, K, dO, V, lse, D, seen, t * kT, tx, ty, g);
@@ -283,12 +279,11 @@ __global__ void __launch_bounds__(256) attention_dq_simt_kernel(const AttnShape 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = r0 + ty + 16 * i;
-        if (r < s.R) store_row(static_cast<T*>(a.dq) + qh + (size_t)r * kDh, tx, dq[i]);
+        if (r < s.R) store_row(static_cast<float*>(a.dq) + qh + (size_t)r * kDh, tx, dq[i]);
     }
 }
 
 // grid (key tiles, heads): dk and dv of 64 keys over all rows, in row order
-template <typename T>
 __global__ void __launch_bounds__(256) attention_dkdv_simt_kernel(const AttnShape s, const AttnArgs a)
 {
     extern __shared__ __align__(16) float sm[];
@@ -297,14 +292,14 @@ __global__ void __launch_bounds__(256) attention_dkdv_simt_kernel(const AttnShap
     const int head = blockIdx.y, b = head / s.Hk, k0 = blockIdx.x * kT;
     const int len = attn_len(s, a.kv_len, b);
     const size_t qh = (size_t)head * s.R * kDh, kh = (size_t)head * s.Lk * kDh;
-    load_tile(K, static_cast<const T*>(a.k) + kh, k0, len);
-    load_tile(V, static_cast<const T*>(a.v) + kh, k0, len);
+    load_tile(K, static_cast<const float*>(a.k) + kh, k0, len);
+    load_tile(V, static_cast<const float*>(a.v) + kh, k0, len);
     float dk[4][8] = {}, dv[4][8] = {};
     for (int r0 = 0; r0 < s.R && k0 < len; r0 += kT) {
         if (attn_seen_most(s, len, r0, min(r0 + kT, s.R) - 1) <= k0) continue;
         __syncthreads();
-        load_tile(Q, static_cast<const T*>(a.q) + qh, r0, s.R);
-        load_tile(dO, static_cast<const T*>(a.dO) + qh, r0, s.R);
+        load_tile(Q, static_cast<const float*>(a.q) + qh, r0, s.R);
+        load_tile(dO, static_cast<const float*>(a.dO) + qh, r0, s.R);
         float lse[4], D[4];
         int seen[4];
 #pragma unroll
@@ -333,8 +328,8 @@ __global__ void __launch_bounds__(256) attention_dkdv_simt_kernel(const AttnShap
     for (int i = 0; i < 4; ++i) {
         const int j = k0 + ty + 16 * i;
         if (j < s.Lk) {
-            store_row(static_cast<T*>(a.dk) + kh + (size_t)j * kDh, tx, dk[i]);
-            store_row(static_cast<T*>(a.dv) + kh + (size_t)j * kDh, tx, dv[i]);
+            store_row(static_cast<float*>(a.dk) + kh + (size_t)j * kDh, tx, dk[i]);
+            store_row(static_cast<float*>(a.dv) + kh + (size_t)j * kDh, tx, dv[i]);
         }
     }
 }
@@ -351,10 +346,9 @@ cudaError_t launch(K kernel, dim3 grid, size_t floats, const AttnShape& s, const
 
 }  // namespace
 
-template <typename T>
 cudaError_t launch_attention_simt(const AttnShape& s, const AttnArgs& a, cudaStream_t st)
 {
-    return launch(attention_simt_kernel<T>, dim3((s.R + kT - 1) / kT, s.heads, s.splits), 3 * kTileF + kPF, s, a, st);
+    return launch(attention_simt_kernel, dim3((s.R + kT - 1) / kT, s.heads, s.splits), 3 * kTileF + kPF, s, a, st);
 }
 
 template <typename T>
@@ -374,20 +368,17 @@ cudaError_t launch_attention_rowdot(const AttnShape& s, const AttnArgs& a, cudaS
     return cudaGetLastError();
 }
 
-template <typename T>
 cudaError_t launch_attention_backward_simt(const AttnShape& s, const AttnArgs& a, cudaStream_t st)
 {
-    cudaError_t e = launch(attention_dkdv_simt_kernel<T>, dim3((s.Lk + kT - 1) / kT, s.heads), 4 * kTileF + 2 * kPF, s,
+    cudaError_t e = launch(attention_dkdv_simt_kernel, dim3((s.Lk + kT - 1) / kT, s.heads), 4 * kTileF + 2 * kPF, s,
                            a, st);
     if (e != cudaSuccess) return e;
-    return launch(attention_dq_simt_kernel<T>, dim3((s.R + kT - 1) / kT, s.heads), 4 * kTileF + kPF, s, a, st);
+    return launch(attention_dq_simt_kernel, dim3((s.R + kT - 1) / kT, s.heads), 4 * kTileF + kPF, s, a, st);
 }
 
 #define ROLA_INSTANTIATE(T)                                                                                   \
-    template cudaError_t launch_attention_simt<T>(const AttnShape&, const AttnArgs&, cudaStream_t);           \
     template cudaError_t launch_attention_join<T>(const AttnShape&, const AttnArgs&, cudaStream_t);           \
-    template cudaError_t launch_attention_rowdot<T>(const AttnShape&, const AttnArgs&, cudaStream_t);         \
-    template cudaError_t launch_attention_backward_simt<T>(const AttnShape&, const AttnArgs&, cudaStream_t);
+    template cudaError_t launch_attention_rowdot<T>(const AttnShape&, const AttnArgs&, cudaStream_t);
 ROLA_INSTANTIATE(float)
 ROLA_INSTANTIATE(__nv_bfloat16)
 #undef ROLA_INSTANTIATE

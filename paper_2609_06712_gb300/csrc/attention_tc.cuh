@@ -1,0 +1,59 @@
+// Shared by the tensor-core attention kernels over a dense key set (forward
+// and backward).
+#pragma once
+
+#include <cuda.h>
+
+#include "block_ops.cuh"
+#include "tcgen05.cuh"
+
+namespace rola {
+
+// A [heads][rows][128] bf16 tensor as (d, row, head), boxes of 64 d x box_rows
+// rows in 128-byte swizzle: a d-chunk of a tile.  Rows past `rows` read as zero.
+bool encode_rows(CUtensorMap* m, const void* ptr, int64_t rows, int64_t heads, int box_rows);
+
+namespace tc {
+
+// D[tmem] (+)= A[tmem] * B[smem]: A is M rows of K 16-bit values in TMEM,
+// two per 32-bit column (the lower K index in the low half).
+__device__ __forceinline__ void mma_ts_split(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi,
+                                             uint32_t idesc, uint32_t accum)
+{
+    asm volatile(
+        "{\n.reg .pred p;\n.reg .b64 db;\n"
+        "setp.ne.b32 p, %5, 0;\n"
+        "mov.b64 db, {%2, %3};\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n}\n" ::"r"(d_tmem),
+        "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accum)
+        : "memory");
+}
+
+// NC consecutive columns of this thread's TMEM lane
+template <int NC>
+__device__ __forceinline__ void row_load(uint32_t taddr, float (&v)[NC])
+{
+#pragma unroll
+    for (int c = 0; c < NC / 16; ++c) tmem_ld16(taddr + c * 16, *reinterpret_cast<float(*)[16]>(&v[c * 16]));
+    tmem_ld_wait(*reinterpret_cast<float(*)[16]>(&v[0]));
+#pragma unroll
+    for (int c = 1; c < NC / 16; ++c) reg_fence(*reinterpret_cast<float(*)[16]>(&v[c * 16]));
+}
+__device__ __forceinline__ void row_load128(uint32_t taddr, float (&v)[128]) { row_load<128>(taddr, v); }
+
+// (a, b) = (a * m + c, b * m + c), one packed f32x2 instruction (each element an IEEE fma)
+__device__ __forceinline__ void ffma2(float& a, float& b, float m, float c)
+{
+    asm("{\n.reg .b64 ra, rm, rc;\nmov.b64 ra, {%0, %1};\nmov.b64 rm, {%2, %2};\nmov.b64 rc, {%3, %3};\n"
+        "fma.rn.f32x2 ra, ra, rm, rc;\nmov.b64 {%0, %1}, ra;\n}\n"
+        : "+f"(a), "+f"(b) : "f"(m), "f"(c));
+}
+__device__ __forceinline__ void fadd2(float& a, float& b, float p, float q)
+{
+    asm("{\n.reg .b64 ra, rp;\nmov.b64 ra, {%0, %1};\nmov.b64 rp, {%2, %3};\n"
+        "add.rn.f32x2 ra, ra, rp;\nmov.b64 {%0, %1}, ra;\n}\n"
+        : "+f"(a), "+f"(b) : "f"(p), "f"(q));
+}
+
+}  // namespace tc
+}  // namespace rola

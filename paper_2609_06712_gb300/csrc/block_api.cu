@@ -100,11 +100,11 @@ rola_status_t ffn_forward(const rola_ffn_config_t* cfg, const void* X, const voi
     void* H = at<void>(ws, w.H);
     ROLA_TRY(cudaMemsetAsync(at<uint8_t>(ws, w.status), 0, sizeof(DeviceStatus), st));
     if (cfg->dtype == ROLA_BF16) {
-        ROLA_TRY(launch_ffn_up_simt<__nv_bfloat16>(s, X, Wg, Wu, H, G, U, st));
-        ROLA_TRY(launch_ffn_down_simt<__nv_bfloat16>(s, H, Wd, Y, st));
+        ROLA_TRY(launch_ffn_up_tc(s, X, Wg, Wu, H, G, U, at<DeviceStatus>(ws, w.status), st));
+        ROLA_TRY(launch_ffn_down_tc(s, H, Wd, Y, at<DeviceStatus>(ws, w.status), st));
     } else {
-        ROLA_TRY(launch_ffn_up_simt<float>(s, X, Wg, Wu, H, G, U, st));
-        ROLA_TRY(launch_ffn_down_simt<float>(s, H, Wd, Y, st));
+        ROLA_TRY(launch_ffn_up_simt(s, X, Wg, Wu, H, G, U, st));
+        ROLA_TRY(launch_ffn_down_simt(s, H, Wd, Y, st));
     }
     return ROLA_OK;
 }
@@ -153,7 +153,8 @@ AttnShape make_shape(const rola_attention_config_t& c)
     const double scale = c.scale > 0.0f ? (double)c.scale : 1.0 / sqrt((double)kDh);
     s.scale = (float)scale;
     s.scale_log2 = (float)(scale * 1.4426950408889634);
-    s.splits = attn_splits((int64_t)s.heads * ((s.R + 63) / 64), (s.Lk + 63) / 64);
+    const int rows = c.dtype == ROLA_BF16 ? 256 : 64, keys = c.dtype == ROLA_BF16 ? 128 : 64;   // of an item, of a tile
+    s.splits = attn_splits((int64_t)s.heads * ((s.R + rows - 1) / rows), (s.Lk + keys - 1) / keys);
     s.wait_limit_ns = wait_limit_ns(c.wait_limit_ms);
     s.debug_flags = c.debug_flags;
     return s;
@@ -257,11 +258,11 @@ rola_status_t rola_ffn_backward(const rola_ffn_config_t* cfg, const void* X, con
     void *H = at<void>(ws, w.H), *dG = at<void>(ws, w.dG), *dU = at<void>(ws, w.dU);
     ROLA_TRY(cudaMemsetAsync(at<uint8_t>(ws, w.status), 0, sizeof(DeviceStatus), st));
     if (cfg->dtype == ROLA_BF16)
-        ROLA_TRY(launch_ffn_backward_simt<__nv_bfloat16>(s, X, W_gate, W_up, W_down, G, U, dY, H, dG, dU, dX, dW_gate,
-                                                         dW_up, dW_down, st));
+        ROLA_TRY(launch_ffn_backward_tc(s, X, W_gate, W_up, W_down, G, U, dY, H, dG, dU, dX, dW_gate, dW_up, dW_down,
+                                        at<DeviceStatus>(ws, w.status), st));
     else
-        ROLA_TRY(launch_ffn_backward_simt<float>(s, X, W_gate, W_up, W_down, G, U, dY, H, dG, dU, dX, dW_gate, dW_up,
-                                                 dW_down, st));
+        ROLA_TRY(launch_ffn_backward_simt(s, X, W_gate, W_up, W_down, G, U, dY, H, dG, dU, dX, dW_gate, dW_up, dW_down,
+                                          st));
     return ROLA_OK;
 }
 
@@ -299,7 +300,7 @@ rola_status_t rola_attention(const rola_attention_config_t* cfg, const void* q, 
     a.status = at<DeviceStatus>(ws, w.status);
     ROLA_TRY(cudaMemsetAsync(a.status, 0, sizeof(DeviceStatus), st));
     const bool bf16 = cfg->dtype == ROLA_BF16;
-    ROLA_TRY(bf16 ? launch_attention_simt<__nv_bfloat16>(s, a, st) : launch_attention_simt<float>(s, a, st));
+    ROLA_TRY(bf16 ? launch_attention_tc(s, a, st) : launch_attention_simt(s, a, st));
     if (s.splits > 1)
         ROLA_TRY(bf16 ? launch_attention_join<__nv_bfloat16>(s, a, st) : launch_attention_join<float>(s, a, st));
     return ROLA_OK;
@@ -326,10 +327,10 @@ rola_status_t rola_attention_backward(const rola_attention_config_t* cfg, const 
     ROLA_TRY(cudaMemsetAsync(a.status, 0, sizeof(DeviceStatus), st));
     if (cfg->dtype == ROLA_BF16) {
         ROLA_TRY(launch_attention_rowdot<__nv_bfloat16>(s, a, st));
-        ROLA_TRY(launch_attention_backward_simt<__nv_bfloat16>(s, a, st));
+        ROLA_TRY(launch_attention_backward_tc(s, a, st));
     } else {
         ROLA_TRY(launch_attention_rowdot<float>(s, a, st));
-        ROLA_TRY(launch_attention_backward_simt<float>(s, a, st));
+        ROLA_TRY(launch_attention_backward_simt(s, a, st));
     }
     return ROLA_OK;
 }

@@ -160,26 +160,34 @@ cudaError_t launch_layer_norm_backward(rola_dtype_t dt, long long rows, int d, c
                                        const float* mean, const float* rstd, const void* dy, void* dx, float* dgamma,
                                        float* dbeta, float* part, cudaStream_t st);
 
-// H = phi(X Wg^T) * (X Wu^T), G and U kept where given (both or neither)
-template <typename T>
+// H = phi(X Wg^T) * (X Wu^T), G and U kept where given (both or neither): fp32, bf16 (tensor cores)
 cudaError_t launch_ffn_up_simt(const FfnShape& s, const void* X, const void* Wg, const void* Wu, void* H, float* G,
                                float* U, cudaStream_t st);
+cudaError_t launch_ffn_up_tc(const FfnShape& s, const void* X, const void* Wg, const void* Wu, void* H, float* G,
+                             float* U, DeviceStatus* status, cudaStream_t st);
 // Y = H Wd^T
-template <typename T>
 cudaError_t launch_ffn_down_simt(const FfnShape& s, const void* H, const void* Wd, void* Y, cudaStream_t st);
+cudaError_t launch_ffn_down_tc(const FfnShape& s, const void* H, const void* Wd, void* Y, DeviceStatus* status,
+                               cudaStream_t st);
 // dG, dU, H from dY Wd, G and U; then the four gradients
-template <typename T>
 cudaError_t launch_ffn_backward_simt(const FfnShape& s, const void* X, const void* Wg, const void* Wu, const void* Wd,
                                      const float* G, const float* U, const void* dY, void* H, void* dG, void* dU,
                                      void* dX, void* dWg, void* dWu, void* dWd, cudaStream_t st);
+cudaError_t launch_ffn_backward_tc(const FfnShape& s, const void* X, const void* Wg, const void* Wu, const void* Wd,
+                                   const float* G, const float* U, const void* dY, void* H, void* dG, void* dU,
+                                   void* dX, void* dWg, void* dWu, void* dWd, DeviceStatus* status, cudaStream_t st);
 
-template <typename T>
+// o and lse, or the parts of a split key axis: fp32, bf16 (tensor cores)
 cudaError_t launch_attention_simt(const AttnShape& s, const AttnArgs& a, cudaStream_t st);
+cudaError_t launch_attention_tc(const AttnShape& s, const AttnArgs& a, cudaStream_t st);
+// o and lse from the parts
 template <typename T>
 cudaError_t launch_attention_join(const AttnShape& s, const AttnArgs& a, cudaStream_t st);
+// D = rowsum(dO o)
 template <typename T>
 cudaError_t launch_attention_rowdot(const AttnShape& s, const AttnArgs& a, cudaStream_t st);
-template <typename T>
+// dq, dk, dv from D
 cudaError_t launch_attention_backward_simt(const AttnShape& s, const AttnArgs& a, cudaStream_t st);
+cudaError_t launch_attention_backward_tc(const AttnShape& s, const AttnArgs& a, cudaStream_t st);
 
 }  // namespace rola

@@ -24,9 +24,8 @@ enum Epilogue { kStore, kGateUp, kGateGrad };
 
 // An operand: element (i, k) at p[i * ld + k] (k contiguous) or p[k * ld + i].
 // ld and the contiguous extent are multiples of 8 elements, p is 16-byte aligned.
-template <typename T>
 struct Operand {
-    const T* p;
+    const float* p;
     int rows;                    // extent of i
     int ld;
 };
@@ -41,8 +40,8 @@ struct Args {
 
 // This thread's 8 elements of a 128 x 16 tile: along k, row t / 2 and k = 8 (t % 2); along i, k = t / 16 and
 // rows 8 (t % 16).  Elements outside the operand are 0.
-template <typename T, bool KC>
-__device__ __forceinline__ void fetch(const Operand<T>& o, int i0, int k0, int K, float (&x)[8])
+template <bool KC>
+__device__ __forceinline__ void fetch(const Operand& o, int i0, int k0, int K, float (&x)[8])
 {
     const int t = threadIdx.x;
     const int i = KC ? i0 + t / 2 : i0 + (t % 16) * 8, k = KC ? k0 + (t % 2) * 8 : k0 + t / 16;
@@ -50,7 +49,7 @@ __device__ __forceinline__ void fetch(const Operand<T>& o, int i0, int k0, int K
     for (int e = 0; e < 8; ++e) x[e] = 0.0f;
     // the contiguous extent is a multiple of 8, so the 8 elements are all inside or all outside
     if (i < o.rows && k < K) {
-        const T* p = KC ? o.p + (size_t)i * o.ld + k : o.p + (size_t)k * o.ld + i;
+        const float* p = KC ? o.p + (size_t)i * o.ld + k : o.p + (size_t)k * o.ld + i;
         const float4 a = load4(p), b = load4(p + 4);
         x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
         x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
@@ -70,20 +69,20 @@ __device__ __forceinline__ void stage(float (*s)[kPad], const float (&x)[8])
 }
 
 // The B tile of kGateUp: rows 0-63 from b0, 64-127 from b1, the same 64 features.
-template <typename T, bool BK, int E>
-__device__ __forceinline__ void fetch_b(const Operand<T>& b0, const Operand<T>& b1, int n0, int k0, int K, float (&x)[8])
+template <bool BK, int E>
+__device__ __forceinline__ void fetch_b(const Operand& b0, const Operand& b1, int n0, int k0, int K, float (&x)[8])
 {
     if constexpr (E == kGateUp) {
         static_assert(BK, "the weights are contiguous along k");
         const bool up = threadIdx.x >= 128;
-        fetch<T, true>(up ? b1 : b0, up ? n0 - 64 : n0, k0, K, x);
+        fetch<true>(up ? b1 : b0, up ? n0 - 64 : n0, k0, K, x);
     } else {
-        fetch<T, BK>(b0, n0, k0, K, x);
+        fetch<BK>(b0, n0, k0, K, x);
     }
 }
 
-template <typename T, bool AK, bool BK, int E>
-__global__ void __launch_bounds__(256, 2) simt_gemm_kernel(Operand<T> a0, Operand<T> b0, Operand<T> a1, Operand<T> b1,
+template <bool AK, bool BK, int E>
+__global__ void __launch_bounds__(256, 2) simt_gemm_kernel(Operand a0, Operand b0, Operand a1, Operand b1,
                                                            const Args p)
 {
     __shared__ __align__(16) float as[2][kStep][kPad];
@@ -96,9 +95,9 @@ __global__ void __launch_bounds__(256, 2) simt_gemm_kernel(Operand<T> a0, Operan
     auto next = [&](int s) {
         const bool second = s >= steps;                // dX: the second product of the sum
         const int k0 = (second ? s - steps : s) * kStep;
-        fetch<T, AK>(second ? a1 : a0, m0, k0, p.K, xa);
-        if constexpr (E == kGateUp) fetch_b<T, BK, E>(b0, b1, n0, k0, p.K, xb);
-        else fetch_b<T, BK, E>(second ? b1 : b0, b1, n0, k0, p.K, xb);
+        fetch<AK>(second ? a1 : a0, m0, k0, p.K, xa);
+        if constexpr (E == kGateUp) fetch_b<BK, E>(b0, b1, n0, k0, p.K, xb);
+        else fetch_b<BK, E>(second ? b1 : b0, b1, n0, k0, p.K, xb);
     };
     next(0);
     stage<AK>(as[0], xa);
@@ -135,7 +134,7 @@ __global__ void __launch_bounds__(256, 2) simt_gemm_kernel(Operand<T> a0, Operan
                 const size_t at = (size_t)m * p.ldc + n;
                 const float4 g = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
                 const float4 u = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
-                store4(static_cast<T*>(p.C) + at,
+                store4(static_cast<float*>(p.C) + at,
                        make_float4(gate_act(p.act, g.x) * u.x, gate_act(p.act, g.y) * u.y, gate_act(p.act, g.z) * u.z,
                                    gate_act(p.act, g.w) * u.w));
                 if (p.G) {
@@ -151,7 +150,7 @@ __global__ void __launch_bounds__(256, 2) simt_gemm_kernel(Operand<T> a0, Operan
                 const size_t at = (size_t)m * p.ldc + n;
                 const float* c = &acc[i][4 * h];
                 if constexpr (E == kStore) {
-                    store4(static_cast<T*>(p.C) + at, make_float4(c[0], c[1], c[2], c[3]));
+                    store4(static_cast<float*>(p.C) + at, make_float4(c[0], c[1], c[2], c[3]));
                 } else {
                     const float4 g4 = load4(p.G_in + at), u4 = load4(p.U_in + at);
                     const float g[4] = {g4.x, g4.y, g4.z, g4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
@@ -164,63 +163,60 @@ __global__ void __launch_bounds__(256, 2) simt_gemm_kernel(Operand<T> a0, Operan
                         dg[e] = c[e] * u[e] * dph;
                         du[e] = c[e] * ph;
                     }
-                    store4(static_cast<T*>(p.C) + at, make_float4(hh[0], hh[1], hh[2], hh[3]));
-                    store4(static_cast<T*>(p.C2) + at, make_float4(dg[0], dg[1], dg[2], dg[3]));
-                    store4(static_cast<T*>(p.C3) + at, make_float4(du[0], du[1], du[2], du[3]));
+                    store4(static_cast<float*>(p.C) + at, make_float4(hh[0], hh[1], hh[2], hh[3]));
+                    store4(static_cast<float*>(p.C2) + at, make_float4(dg[0], dg[1], dg[2], dg[3]));
+                    store4(static_cast<float*>(p.C3) + at, make_float4(du[0], du[1], du[2], du[3]));
                 }
             }
         }
     }
 }
 
-template <typename T, bool AK, bool BK, int E>
-cudaError_t gemm(Operand<T> a0, Operand<T> b0, Operand<T> a1, Operand<T> b1, const Args& p, cudaStream_t st)
+template <bool AK, bool BK, int E>
+cudaError_t gemm(Operand a0, Operand b0, Operand a1, Operand b1, const Args& p, cudaStream_t st)
 {
     const int nt = E == kGateUp ? 64 : kTile;
     const dim3 grid((p.N + nt - 1) / nt, (p.M + kTile - 1) / kTile);
-    simt_gemm_kernel<T, AK, BK, E><<<grid, 256, 0, st>>>(a0, b0, a1, b1, p);
+    simt_gemm_kernel<AK, BK, E><<<grid, 256, 0, st>>>(a0, b0, a1, b1, p);
     return cudaGetLastError();
 }
 
 }  // namespace
 
-template <typename T>
 cudaError_t launch_ffn_up_simt(const FfnShape& s, const void* X, const void* Wg, const void* Wu, void* H, float* G,
                                float* U, cudaStream_t st)
 {
     Args p{};
     p.M = s.M; p.N = s.F; p.K = s.D; p.sources = 1; p.act = s.act; p.ldc = s.F;
     p.C = H; p.G = G; p.U = U;
-    const Operand<T> x{static_cast<const T*>(X), s.M, s.D};
-    return gemm<T, true, true, kGateUp>(x, {static_cast<const T*>(Wg), s.F, s.D}, x,
-                                        {static_cast<const T*>(Wu), s.F, s.D}, p, st);
+    const Operand x{static_cast<const float*>(X), s.M, s.D};
+    return gemm<true, true, kGateUp>(x, {static_cast<const float*>(Wg), s.F, s.D}, x,
+                                        {static_cast<const float*>(Wu), s.F, s.D}, p, st);
 }
 
-template <typename T>
 cudaError_t launch_ffn_down_simt(const FfnShape& s, const void* H, const void* Wd, void* Y, cudaStream_t st)
 {
     Args p{};
     p.M = s.M; p.N = s.D; p.K = s.F; p.sources = 1; p.ldc = s.D;
     p.C = Y;
-    const Operand<T> h{static_cast<const T*>(H), s.M, s.F}, w{static_cast<const T*>(Wd), s.D, s.F};
-    return gemm<T, true, true, kStore>(h, w, h, w, p, st);
+    const Operand h{static_cast<const float*>(H), s.M, s.F}, w{static_cast<const float*>(Wd), s.D, s.F};
+    return gemm<true, true, kStore>(h, w, h, w, p, st);
 }
 
-template <typename T>
 cudaError_t launch_ffn_backward_simt(const FfnShape& s, const void* X, const void* Wg, const void* Wu, const void* Wd,
                                      const float* G, const float* U, const void* dY, void* H, void* dG, void* dU,
                                      void* dX, void* dWg, void* dWu, void* dWd, cudaStream_t st)
 {
-    auto op = [](const void* p, int rows, int ld) { return Operand<T>{static_cast<const T*>(p), rows, ld}; };
+    auto op = [](const void* p, int rows, int ld) { return Operand{static_cast<const float*>(p), rows, ld}; };
     Args p{};
     p.M = s.M; p.N = s.F; p.K = s.D; p.sources = 1; p.act = s.act; p.ldc = s.F;
     p.G_in = G; p.U_in = U; p.C = H; p.C2 = dG; p.C3 = dU;
-    cudaError_t e = gemm<T, true, false, kGateGrad>(op(dY, s.M, s.D), op(Wd, s.F, s.F), op(dY, s.M, s.D),
+    cudaError_t e = gemm<true, false, kGateGrad>(op(dY, s.M, s.D), op(Wd, s.F, s.F), op(dY, s.M, s.D),
                                                     op(Wd, s.F, s.F), p, st);
     if (e != cudaSuccess) return e;
     p = Args{};
     p.M = s.M; p.N = s.D; p.K = s.F; p.sources = 2; p.ldc = s.D; p.C = dX;
-    e = gemm<T, true, false, kStore>(op(dG, s.M, s.F), op(Wg, s.D, s.D), op(dU, s.M, s.F), op(Wu, s.D, s.D), p, st);
+    e = gemm<true, false, kStore>(op(dG, s.M, s.F), op(Wg, s.D, s.D), op(dU, s.M, s.F), op(Wu, s.D, s.D), p, st);
     if (e != cudaSuccess) return e;
     // the weights' gradients: both operands contiguous along their output index, k = token
     const struct { const void *a, *b; int m, n; void* c; } w[3] = {
@@ -228,22 +224,11 @@ cudaError_t launch_ffn_backward_simt(const FfnShape& s, const void* X, const voi
     for (const auto& g : w) {
         p = Args{};
         p.M = g.m; p.N = g.n; p.K = s.M; p.sources = 1; p.ldc = g.n; p.C = g.c;
-        e = gemm<T, false, false, kStore>(op(g.a, g.m, g.m), op(g.b, g.n, g.n), op(g.a, g.m, g.m), op(g.b, g.n, g.n),
+        e = gemm<false, false, kStore>(op(g.a, g.m, g.m), op(g.b, g.n, g.n), op(g.a, g.m, g.m), op(g.b, g.n, g.n),
                                           p, st);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
 }
-
-#define ROLA_INSTANTIATE(T)                                                                                          \
-    template cudaError_t launch_ffn_up_simt<T>(const FfnShape&, const void*, const void*, const void*, void*,        \
-                                               float*, float*, cudaStream_t);                                        \
-    template cudaError_t launch_ffn_down_simt<T>(const FfnShape&, const void*, const void*, void*, cudaStream_t);    \
-    template cudaError_t launch_ffn_backward_simt<T>(const FfnShape&, const void*, const void*, const void*,         \
-                                                     const void*, const float*, const float*, const void*, void*,    \
-                                                     void*, void*, void*, void*, void*, void*, cudaStream_t);
-ROLA_INSTANTIATE(float)
-ROLA_INSTANTIATE(__nv_bfloat16)
-#undef ROLA_INSTANTIATE
 
 }  // namespace rola
