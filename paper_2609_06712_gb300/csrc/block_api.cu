@@ -99,7 +99,9 @@ rola_status_t ffn_forward(const rola_ffn_config_t* cfg, const void* X, const voi
     const FfnShape s = make_shape(*cfg);
     void* H = at<void>(ws, w.H);
     ROLA_TRY(cudaMemsetAsync(at<uint8_t>(ws, w.status), 0, sizeof(DeviceStatus), st));
-    if (cfg->dtype == ROLA_BF16) {
+    if (cfg->dtype == ROLA_BF16 && s.M <= kFfnFewTokens) {
+        ROLA_TRY(launch_ffn_few(s, X, Wg, Wu, Wd, H, G, U, Y, at<DeviceStatus>(ws, w.status), st));
+    } else if (cfg->dtype == ROLA_BF16) {
         ROLA_TRY(launch_ffn_up_tc(s, X, Wg, Wu, H, G, U, at<DeviceStatus>(ws, w.status), st));
         ROLA_TRY(launch_ffn_down_tc(s, H, Wd, Y, at<DeviceStatus>(ws, w.status), st));
     } else {

@@ -169,6 +169,13 @@ cudaError_t launch_ffn_up_tc(const FfnShape& s, const void* X, const void* Wg, c
 cudaError_t launch_ffn_down_simt(const FfnShape& s, const void* H, const void* Wd, void* Y, cudaStream_t st);
 cudaError_t launch_ffn_down_tc(const FfnShape& s, const void* H, const void* Wd, void* Y, DeviceStatus* status,
                                cudaStream_t st);
+// Few tokens: both products of the forward (and G, U where given); H, dG, dU and dX of the backward.
+constexpr int kFfnFewTokens = 96;    // their sums of two accumulators fit a CTA's shared memory
+cudaError_t launch_ffn_few(const FfnShape& s, const void* X, const void* Wg, const void* Wu, const void* Wd, void* H,
+                           float* G, float* U, void* Y, DeviceStatus* status, cudaStream_t st);
+cudaError_t launch_ffn_few_grad(const FfnShape& s, const void* Wg, const void* Wu, const void* Wd, const float* G,
+                                const float* U, const void* dY, void* H, void* dG, void* dU, void* dX,
+                                DeviceStatus* status, cudaStream_t st);
 // dG, dU, H from dY Wd, G and U; then the four gradients
 cudaError_t launch_ffn_backward_simt(const FfnShape& s, const void* X, const void* Wg, const void* Wu, const void* Wd,
                                      const float* G, const float* U, const void* dY, void* H, void* dG, void* dU,

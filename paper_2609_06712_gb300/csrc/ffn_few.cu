@@ -1,0 +1,383 @@
+// The gated feed-forward's products for few tokens (bf16 operands, tcgen05):
+// every weight is read once for all of them, and that is what bounds the work
+// (one token at widths 5120 x 13824: 425 MB of weights, 63 us at the measured
+// 6.8 TB/s; its 0.4 GFLOP are nothing).
+//
+// The tokens are the N axis and 128 weight rows the M axis of the tensor core,
+// so that a single token costs a tile of 16 columns instead of 128 rows:
+//   kUp     g, u (128 features x tokens) = Wg X^T, Wu X^T;  H = phi(g) * u
+//   kDown   Y^T  = Wd H^T
+//   kGrad   dH^T = Wd^T dY^T  (Wd read MN-major);  H, dG, dU from it and G, U
+//   kDX     dX^T = Wg^T dG^T + Wu^T dU^T  (MN-major; one sum over 2 d_ff)
+// There are too few row tiles to occupy the GPU (12 of 128 rows at d_model
+// 1536), so the K axis of a tile is split over a cluster of up to 8 CTAs.  Each
+// streams its share through a TMA ring into its own TMEM accumulator, then the
+// accumulators meet in the cluster's shared memory: CTA r of s adds the s parts
+// of its share of the tokens, in rank order, and writes them.  No partial sum
+// goes through global memory and the order of every sum is fixed.  About 110 KB
+// of shared memory per CTA let two CTAs share an SM, so up to 304 CTAs stream
+// at once (some 30 MB of loads in flight) and the last wave is never nearly empty.
+//
+// The second kernel of a pair is launched while the first still runs
+// (programmatic dependent launch): it loads its first weights, which nothing
+// before it writes, and waits for the first kernel only for the tokens.
+//
+// Warps (192 threads): 0 TMA, 1 products and TMEM, 2-5 epilogue.  Every mbarrier
+// wait is bounded; all threads reach the cluster barriers whatever happens.
+#include "block_ops.cuh"
+#include "tcgen05.cuh"
+#include "tma_2d.cuh"
+
+namespace rola {
+namespace {
+
+using namespace tc;
+
+enum Mode { kUp, kDown, kGrad, kDX };
+
+constexpr int kTileM = 128, kStepK = 64, kThreads = 192, kMaxStages = 8;
+constexpr uint32_t kABytes = kTileM * kStepK * 2;
+constexpr uint32_t kSmemBudget = 112 * 1024;                 // two CTAs of an SM's 227 KB
+constexpr int kMaxCluster = 8;
+
+enum Bar { FULL = 0, EMPTY = FULL + kMaxStages, ACC_FULL = EMPTY + kMaxStages, DRAIN, NUM_BARS };
+struct Ctrl {
+    uint64_t bar[NUM_BARS];
+    uint32_t tmem_base;
+    int abort;
+};
+
+struct Params {
+    CUtensorMap a[2], b[2];          // weights (kUp: gate and up; kDX: the two sources), tokens
+    int M, rows;                     // tokens; weight rows of the output (d_ff or d_model)
+    int nt;                          // tokens rounded up to a multiple of 16: the N of the products
+    int k_steps, sources;            // K steps of 64 of one source
+    int stages, act, skip_first;
+    uint32_t stage_bytes, tiles_bytes;   // of a stage; of the tiles in front of the control block
+    __nv_bfloat16 *c0, *c1, *c2;     // H / Y / dX; dG, dU
+    float *G, *U;                    // kUp: out or NULL; kGrad: in
+    DeviceStatus* status;
+    uint64_t wait_limit_ns;
+};
+
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;\n" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;\n" ::: "memory");
+}
+// The address of `local` in the shared memory of CTA `rank` of the cluster, and a load from there.
+__device__ __forceinline__ uint32_t peer(uint32_t local, uint32_t rank)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(a) : "r"(local), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ float ld_peer(uint32_t addr)
+{
+    float x;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(x) : "r"(addr));
+    return x;
+}
+
+template <int MODE>
+__global__ void __launch_bounds__(kThreads, 2) ffn_few_kernel(const __grid_constant__ Params p)
+{
+    constexpr bool AMn = MODE == kGrad || MODE == kDX;
+    constexpr int ACCS = MODE == kUp ? 2 : 1;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    const uint32_t sbase = smem_u32(smem_raw);
+    Ctrl& cb = *reinterpret_cast<Ctrl*>(smem_raw + p.tiles_bytes);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    auto bar = [&](int i) { return smem_u32(&cb.bar[i]); };
+    auto timeout = [&](int where) {
+        if (atomicCAS(&p.status->code, 0, (int)ROLA_ERR_TIMEOUT) == 0) p.status->where = 128 + where;
+    };
+    if (tid == 0) {
+        cb.abort = 0;
+        for (int i = 0; i < p.stages; ++i) {
+            mbar_init(bar(FULL + i), 1);
+            mbar_init(bar(EMPTY + i), 1);
+        }
+        mbar_init(bar(ACC_FULL), 1);
+        mbar_init(bar(DRAIN), 1);
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(&cb.tmem_base), 128 * ACCS);
+        tmem_relinquish();
+    }
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    // the next kernel of the stream may be launched now; it waits for this one where it has to
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    const uint32_t tmem = cb.tmem_base;
+    volatile int* abort = &cb.abort;
+    const uint64_t limit = p.wait_limit_ns;
+    const int s = (int)cluster_size(), rank = (int)cluster_rank();
+    const int tile = blockIdx.x / s, total = p.k_steps * p.sources;
+    const int k_begin = (int)((long long)total * rank / s), k_end = (int)((long long)total * (rank + 1) / s);
+    const int steps = k_end - k_begin;
+    const uint32_t b_off = ACCS * kABytes;               // the tokens' part of a stage
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ TMA producer
+        // a box per lane: weights on lanes 0, 1 (kUp: Wg and Wu; MN-major: 64 rows each), tokens on lane 2
+        bool ok = true;
+        auto coords = [&](int i, int& src, int& k0) {
+            const int ks = k_begin + i;
+            src = ks >= p.k_steps ? 1 : 0;
+            k0 = (ks - src * p.k_steps) * kStepK;
+        };
+        auto load_weights = [&](int i) {
+            int src, k0;
+            coords(i, src, k0);
+            const uint32_t dst = sbase + (i % p.stages) * p.stage_bytes, b = bar(FULL + i % p.stages);
+            if (AMn) {
+                if (lane < 2) tma_load_2d(dst + lane * 8192, &p.a[src], b, tile * kTileM + lane * 64, k0);
+            } else if (lane < ACCS) {
+                tma_load_2d(dst + lane * kABytes, &p.a[lane], b, k0, tile * kTileM);
+            }
+        };
+        auto load_tokens = [&](int i) {
+            int src, k0;
+            coords(i, src, k0);
+            if (lane == 2)
+                tma_load_2d(sbase + (i % p.stages) * p.stage_bytes + b_off, &p.b[src], bar(FULL + i % p.stages), k0, 0);
+        };
+        // test hook: the first stage is never announced nor loaded, so the waits on it run out
+        const int first = p.skip_first && steps > 0 ? 1 : 0, ahead = min(p.stages, steps);
+        for (int i = first; i < ahead; ++i) {
+            if (lane == 0) mbar_expect_tx(bar(FULL + i), p.stage_bytes);
+            __syncwarp();
+            load_weights(i);
+        }
+        asm volatile("griddepcontrol.wait;\n" ::: "memory");     // the tokens may be the previous kernel's output
+        for (int i = first; i < ahead; ++i) load_tokens(i);
+        int i = ahead;
+        for (; i < steps; ++i) {
+            const int st = i % p.stages;
+            ok = __shfl_sync(0xffffffffu, mbar_wait(bar(EMPTY + st), ((i / p.stages) - 1) & 1, abort, limit), 0);
+            if (!ok) break;
+            if (lane == 0) mbar_expect_tx(bar(FULL + st), p.stage_bytes);
+            __syncwarp();
+            load_weights(i);
+            load_tokens(i);
+        }
+        if (lane == 0) {
+            if (!ok) timeout(1);
+            // the copies still in flight land before the CTA exits
+            int never = 0;
+            for (int u = max(i - p.stages, first); u < i; ++u)
+                mbar_wait(bar(FULL + u % p.stages), (u / p.stages) & 1, &never, limit);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ products
+        if (lane == 0) {
+            const uint32_t idesc = idesc_bf16(kTileM, p.nt, AMn, false);
+            const uint64_t da = smem_desc(sbase, AMn ? 8192 : 16, 1024), db = smem_desc(sbase + b_off, 16, 1024);
+            const uint32_t a_lo = (uint32_t)da, a_hi = (uint32_t)(da >> 32), b_lo = (uint32_t)db, b_hi = (uint32_t)(db >> 32);
+            constexpr uint32_t a_k = AMn ? 128 : 2;
+            bool ok = true;
+            for (int i = 0; i < steps; ++i) {
+                const int st = i % p.stages;
+                if (!(ok = mbar_wait(bar(FULL + st), (i / p.stages) & 1, abort, limit))) break;
+                fence_after_sync();
+                const uint32_t off = st * (p.stage_bytes >> 4);
+#pragma unroll
+                for (int acc = 0; acc < ACCS; ++acc)
+#pragma unroll
+                    for (int kk = 0; kk < kStepK / 16; ++kk)
+                        mma_ss_split(tmem + acc * 128, a_lo + off + acc * (kABytes >> 4) + kk * a_k, a_hi, b_lo + off + kk * 2,
+                                     b_hi, idesc, (i > 0 || kk > 0) ? 1u : 0u);
+                mma_commit(bar(EMPTY + st));
+            }
+            if (ok) mma_commit(bar(ACC_FULL));
+            else timeout(2);
+            // every product issued completes before TMEM is released
+            int never = 0;
+            mma_commit(bar(DRAIN));
+            mbar_wait(bar(DRAIN), 0, &never, limit);
+        }
+        __syncwarp();
+    } else {
+        // this CTA's part of the sums into shared memory: [acc][token][128 rows] over the stages, which
+        // every product has read
+        const int q = warp & 3, row = q * 32 + lane;
+        const bool ok = mbar_wait(bar(ACC_FULL), 0, abort, limit);
+        if (!ok) timeout(3);
+        else {
+            fence_after_sync();
+            for (int acc = 0; acc < ACCS; ++acc)
+                for (int c = 0; c < p.nt; c += 16) {
+                    float v[16];
+                    tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + acc * 128 + c, v);
+                    tmem_ld_wait(v);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        *reinterpret_cast<float*>(smem_raw + ((size_t)(acc * p.nt + c + e) * kTileM + row) * 4) = v[e];
+                }
+        }
+    }
+    fence_before_sync();
+    cluster_sync();
+    fence_after_sync();
+    if (warp == 1) tmem_dealloc(tmem, 128 * ACCS);
+    if (warp >= 2) {
+        const int row = (warp & 3) * 32 + lane, f = tile * kTileM + row;
+        const int m0 = p.M * rank / s, m1 = p.M * (rank + 1) / s;
+        uint32_t from[kMaxCluster];
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; ++r) from[r] = r < s ? peer(sbase + (uint32_t)row * 4, r) : 0;
+        for (int m = m0; m < m1; ++m) {
+            // all parts are on their way before the first is added
+            float part[ACCS][kMaxCluster];
+#pragma unroll
+            for (int acc = 0; acc < ACCS; ++acc)
+#pragma unroll
+                for (int r = 0; r < kMaxCluster; ++r)
+                    part[acc][r] = r < s ? ld_peer(from[r] + (uint32_t)((acc * p.nt + m) * kTileM) * 4) : 0.0f;
+            auto sum = [&](int acc) {
+                float x = part[acc][0];
+#pragma unroll
+                for (int r = 1; r < kMaxCluster; ++r) x += part[acc][r];
+                return x;
+            };
+            const float x = sum(0);
+            const size_t at = (size_t)m * p.rows + f;
+            if constexpr (MODE == kUp) {
+                const float u = sum(1);
+                if (f < p.rows) {
+                    p.c0[at] = __float2bfloat16_rn(gate_act(p.act, x) * u);
+                    if (p.G) {
+                        p.G[at] = x;
+                        p.U[at] = u;
+                    }
+                }
+            } else if (f < p.rows) {
+                if constexpr (MODE == kGrad) {
+                    float a, da;
+                    gate_act_grad(p.act, p.G[at], a, da);
+                    const float u = p.U[at];
+                    p.c0[at] = __float2bfloat16_rn(a * u);
+                    p.c1[at] = __float2bfloat16_rn(x * u * da);
+                    p.c2[at] = __float2bfloat16_rn(x * a);
+                } else {
+                    p.c0[at] = __float2bfloat16_rn(x);
+                }
+            }
+        }
+    }
+    cluster_sync();                                      // the peers' shared memory stays until all have read it
+}
+
+// ---------------------------------------------------------------- host side
+
+bool map_of(CUtensorMap* m, const void* p, int rows, int cols, int box_rows)
+{
+    return encode_2d(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p, rows, cols, kStepK, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+template <int MODE>
+cudaError_t launch(const FfnShape& s, Params& p, bool dependent, DeviceStatus* status, cudaStream_t st)
+{
+    constexpr int ACCS = MODE == kUp ? 2 : 1;
+    p.M = s.M;
+    p.act = s.act;
+    p.status = status;
+    p.wait_limit_ns = s.wait_limit_ns;
+    p.skip_first = s.debug_flags & ROLA_DEBUG_SKIP_FIRST_K_COPY ? 1 : 0;
+    const int tiles = (p.rows + kTileM - 1) / kTileM, total = p.k_steps * p.sources;
+    // as many CTAs as two per SM hold, each with two K steps at least
+    int cluster = 304 / tiles;
+    if (cluster > total / 2) cluster = total / 2;
+    if (cluster > kMaxCluster) cluster = kMaxCluster;
+    if (cluster < 1) cluster = 1;
+    p.stage_bytes = ACCS * kABytes + p.nt * kStepK * 2;
+    p.stages = (int)((kSmemBudget - sizeof(Ctrl)) / p.stage_bytes);
+    if (p.stages > kMaxStages) p.stages = kMaxStages;
+    const uint32_t sums = (uint32_t)(ACCS * p.nt * kTileM * 4);
+    p.tiles_bytes = p.stages * p.stage_bytes;
+    if (p.tiles_bytes < sums) p.tiles_bytes = sums;
+    p.tiles_bytes = (p.tiles_bytes + 1023) & ~1023u;
+    const size_t smem = p.tiles_bytes + sizeof(Ctrl);
+    auto kernel = ffn_few_kernel<MODE>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(tiles * cluster);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = cluster;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = dependent ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
+int steps(int k) { return (k + kStepK - 1) / kStepK; }
+
+Params params(const FfnShape& s)
+{
+    Params p{};
+    p.nt = (s.M + 15) / 16 * 16;
+    return p;
+}
+
+}  // namespace
+
+cudaError_t launch_ffn_few(const FfnShape& s, const void* X, const void* Wg, const void* Wu, const void* Wd, void* H,
+                           float* G, float* U, void* Y, DeviceStatus* status, cudaStream_t st)
+{
+    Params p = params(s);
+    p.rows = s.F; p.k_steps = steps(s.D); p.sources = 1;
+    p.c0 = static_cast<__nv_bfloat16*>(H); p.G = G; p.U = U;
+    if (!map_of(&p.a[0], Wg, s.F, s.D, kTileM) || !map_of(&p.a[1], Wu, s.F, s.D, kTileM) || !map_of(&p.b[0], X, s.M, s.D, p.nt))
+        return cudaErrorInvalidValue;
+    cudaError_t e = launch<kUp>(s, p, false, status, st);
+    if (e != cudaSuccess) return e;
+    p = params(s);
+    p.rows = s.D; p.k_steps = steps(s.F); p.sources = 1;
+    p.c0 = static_cast<__nv_bfloat16*>(Y);
+    if (!map_of(&p.a[0], Wd, s.D, s.F, kTileM) || !map_of(&p.b[0], H, s.M, s.F, p.nt)) return cudaErrorInvalidValue;
+    return launch<kDown>(s, p, true, status, st);
+}
+
+cudaError_t launch_ffn_few_grad(const FfnShape& s, const void* Wg, const void* Wu, const void* Wd, const float* G,
+                                const float* U, const void* dY, void* H, void* dG, void* dU, void* dX,
+                                DeviceStatus* status, cudaStream_t st)
+{
+    Params p = params(s);
+    p.rows = s.F; p.k_steps = steps(s.D); p.sources = 1;
+    p.c0 = static_cast<__nv_bfloat16*>(H); p.c1 = static_cast<__nv_bfloat16*>(dG); p.c2 = static_cast<__nv_bfloat16*>(dU);
+    p.G = const_cast<float*>(G); p.U = const_cast<float*>(U);
+    if (!map_of(&p.a[0], Wd, s.D, s.F, kStepK) || !map_of(&p.b[0], dY, s.M, s.D, p.nt)) return cudaErrorInvalidValue;
+    cudaError_t e = launch<kGrad>(s, p, false, status, st);
+    if (e != cudaSuccess) return e;
+    p = params(s);
+    p.rows = s.D; p.k_steps = steps(s.F); p.sources = 2;
+    p.c0 = static_cast<__nv_bfloat16*>(dX);
+    if (!map_of(&p.a[0], Wg, s.F, s.D, kStepK) || !map_of(&p.a[1], Wu, s.F, s.D, kStepK) ||
+        !map_of(&p.b[0], dG, s.M, s.F, p.nt) || !map_of(&p.b[1], dU, s.M, s.F, p.nt))
+        return cudaErrorInvalidValue;
+    return launch<kDX>(s, p, true, status, st);
+}
+
+}  // namespace rola

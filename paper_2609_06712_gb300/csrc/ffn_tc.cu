@@ -520,6 +520,10 @@ cudaError_t launch_ffn_backward_tc(const FfnShape& s, const void* X, const void*
     const auto bf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     const auto f32 = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
     const auto sw128 = CU_TENSOR_MAP_SWIZZLE_128B, sw64 = CU_TENSOR_MAP_SWIZZLE_64B;
+    if (s.M <= kFfnFewTokens) {
+        cudaError_t e = launch_ffn_few_grad(s, Wg, Wu, Wd, G, U, dY, H, dG, dU, dX, status, st);
+        if (e != cudaSuccess) return e;
+    } else {
     {   // dH = dY Wd, and from it H, dG, dU
         Params<kGateGrad> p{};
         Problem& r = p.pr[0];
@@ -544,6 +548,7 @@ cudaError_t launch_ffn_backward_tc(const FfnShape& s, const void* X, const void*
             return cudaErrorInvalidValue;
         cudaError_t e = launch<false, true, kStore>(s, p, status, st);
         if (e != cudaSuccess) return e;
+    }
     }
     // dWg = dG^T X, dWu = dU^T X, dWd = dY^T H: K is the token
     Params<kStore> p{};

@@ -5,31 +5,56 @@
 //   dgamma = sum_rows dy xh,   dbeta = sum_rows dy
 //
 // HBM-bound: x once in and y once out forward, x and dy in and dx out backward
-// (a few fp32 operations per element against 4 or 6 bytes).  A row is held by
-// a group of TPR threads in registers, NV pieces of V elements each, so that
-// mean, centred sum of squares and output take one read of the row.  V is 16
-// bytes where the row length and the pointers allow it, else one element.
-// TPR = 32 (no barrier, one shuffle reduction) while the row needs at most
-// kMaxWarpPieces pieces per lane, then 128 and 512 threads.
+// (a few fp32 operations per element against 4 or 6 bytes).  A row is held in
+// registers by the threads of a group, NV pieces each, so that mean, centred
+// sum of squares and output take one read of the row; a piece is 16 bytes where
+// the row length and the pointers allow it, else one element.  gamma and beta
+// are converted once and stay in registers.  Short rows have a warp each (four
+// in a CTA, no barrier), longer ones a CTA whose size is rounded up from the
+// row's pieces, so that few threads idle.
+//
+// To keep HBM busy an SM needs some 60 KB of loads in flight (44 bytes per ns at
+// over 1 us of latency); a row per CTA in registers is 10 KB at d = 5120.  So with
+// 16-byte pieces the CTA's coming rows are copied ahead into a ring in shared
+// memory (bulk asynchronous copies, one per row, each with its mbarrier).
+// Rows of single elements, which need not start on 16 bytes, are fetched one
+// ahead into registers instead.
 //
 // Backward: every thread keeps the dgamma / dbeta sums of its own columns in
 // registers over all the rows its group takes (row r of group g: g, g + G, ...),
 // the groups of a CTA add theirs through shared memory in group order, and each
-// CTA writes one partial row; a second kernel adds the partial rows in CTA
+// CTA writes one partial row; a second kernel adds the partial rows in a fixed
 // order.  All sums are fp32.
 #include "block_ops.cuh"
+#include "tcgen05.cuh"
 
 namespace rola {
 namespace {
 
-constexpr int kLnThreads = 128;          // of a CTA whose rows have a warp or 128 threads each
+constexpr int kWarpGroups = 4;           // rows of a CTA whose rows have a warp each
+constexpr int kMaxThreads = 512;         // of a CTA that has one row
 
-
+// A piece as loaded: 16 bytes (V elements), or one element (V = 1).
 template <typename T, int V>
-__device__ __forceinline__ void load_piece(const T* p, float (&x)[V])
+struct Piece {
+    uint4 w;
+};
+template <typename T>
+struct Piece<T, 1> {
+    T w;
+};
+template <typename T, int V>
+__device__ __forceinline__ Piece<T, V> load_piece(const T* p)
 {
-    if constexpr (V == 1) x[0] = to_float(p[0]);
-    else load16(p, x);
+    Piece<T, V> x;
+    x.w = *reinterpret_cast<const decltype(x.w)*>(p);
+    return x;
+}
+template <typename T, int V>
+__device__ __forceinline__ void unpack(const Piece<T, V>& x, float (&v)[V])
+{
+    if constexpr (V == 1) v[0] = to_float(x.w);
+    else load16(reinterpret_cast<const T*>(&x.w), v);
 }
 template <typename T, int V>
 __device__ __forceinline__ void store_piece(T* p, const float (&x)[V])
@@ -38,110 +63,348 @@ __device__ __forceinline__ void store_piece(T* p, const float (&x)[V])
     else store16(p, x);
 }
 
-// Sum of (a, b) over the TPR threads of a group, the same bits in every thread.
-template <int TPR>
-__device__ __forceinline__ float2 group_sum(float a, float b, float2* red)
+// Sum of (a, b) over the threads of a group, the same bits in every thread.  A
+// group of more than one warp is the whole CTA; `turn` alternates between two
+// buffers, so that one barrier separates a sum's writes from its reads and the
+// next sum's barrier its reads from the writes after that.
+template <bool WARP>
+__device__ __forceinline__ float2 group_sum(float a, float b, float2 (*red)[32], int& turn)
 {
 #pragma unroll
     for (int off = 16; off >= 1; off >>= 1) {
         a += __shfl_xor_sync(0xffffffffu, a, off);
         b += __shfl_xor_sync(0xffffffffu, b, off);
     }
-    if constexpr (TPR > 32) {
-        __syncthreads();                               // the previous sum has been read
-        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = make_float2(a, b);
+    if constexpr (!WARP) {
+        const int lane = threadIdx.x & 31;
+        float2* buf = red[turn];
+        turn ^= 1;
+        if (lane == 0) buf[threadIdx.x >> 5] = make_float2(a, b);
         __syncthreads();
-        a = b = 0.0f;
+        const float2 t = lane < (int)(blockDim.x >> 5) ? buf[lane] : make_float2(0.0f, 0.0f);
+        a = t.x;
+        b = t.y;
 #pragma unroll
-        for (int w = 0; w < TPR / 32; ++w) {
-            a += red[w].x;
-            b += red[w].y;
+        for (int off = 16; off >= 1; off >>= 1) {
+            a += __shfl_xor_sync(0xffffffffu, a, off);
+            b += __shfl_xor_sync(0xffffffffu, b, off);
         }
     }
     return make_float2(a, b);
 }
 
-template <typename T, int V, int TPR, int NV>
-__global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR)
-    ln_fwd_kernel(long long rows, int d, const T* x, const T* __restrict__ gamma,
-                  const T* __restrict__ beta, float eps, T* y, float* __restrict__ mean, float* __restrict__ rstd)
-{
-    __shared__ float2 red[TPR / 32];
-    constexpr int kGroups = TPR < kLnThreads ? kLnThreads / TPR : 1;
-    const int gt = threadIdx.x % TPR;                  // thread of the group
-    const int pieces = d / V;
-    const float inv_d = 1.0f / (float)d;
-    const long long stride = (long long)gridDim.x * kGroups;
-    // with TPR > 32 the CTA is one group, so the barriers in group_sum are uniform
-    for (long long r = (long long)blockIdx.x * kGroups + threadIdx.x / TPR; r < rows; r += stride) {
-        const T* xr = x + r * d;
-        float v[NV][V];
-        float s = 0.0f;
+constexpr int kMaxDepth = 16;            // rows in a group's ring
+constexpr uint64_t kWaitLimitNs = 2000000000ull;     // bound of the wait for a row
+
+// A group's rows r0, r0 + stride, ... of N matrices, brought ahead.  RING: into
+// `depth` slots of N rows in shared memory, one bulk copy per matrix; a slot is
+// refilled after its row has been read into registers (a barrier of the group lies
+// between).  Otherwise one row ahead in registers.
+template <typename T, int V, int NV, int N, bool WARP, bool RING>
+struct Rows {
+    const T* src[N];
+    long long rows, stride, next;        // next: the row the next copy is of
+    int d, tpr, gt, pieces, depth, slot, phase;
+    uint32_t ring, bars;                 // shared memory: the slots, their mbarriers
+    Piece<T, V> p[RING ? 1 : N][NV];
+
+    __device__ __forceinline__ void copy(int to)         // one thread
+    {
+        const uint32_t bytes = (uint32_t)d * sizeof(T), bar = bars + to * 8;
+        tc::mbar_expect_tx(bar, N * bytes);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = gt + i * TPR;
-            if (c < pieces) load_piece<T, V>(xr + (size_t)c * V, v[i]);
-            else
+        for (int n = 0; n < N; ++n)
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n" ::"r"(
+                             ring + (uint32_t)(to * N + n) * bytes),
+                         "l"(src[n] + next * d), "r"(bytes), "r"(bar)
+                         : "memory");
+        next += stride;
+    }
+    __device__ __forceinline__ void fetch(long long r)   // registers
+    {
 #pragma unroll
-                for (int e = 0; e < V; ++e) v[i][e] = 0.0f;
+        for (int n = 0; n < N; ++n)
 #pragma unroll
-            for (int e = 0; e < V; ++e) s += v[i][e];
+            for (int i = 0; i < NV; ++i) {
+                const int c = gt + i * tpr;
+                if (c < pieces) p[n][i] = load_piece<T, V>(src[n] + r * d + (size_t)c * V);
+            }
+    }
+    __device__ __forceinline__ void start(long long r0)
+    {
+        if constexpr (RING) {
+            next = r0;
+            slot = phase = 0;
+            if (gt == 0) {
+                for (int i = 0; i < depth; ++i) tc::mbar_init(bars + i * 8, 1);
+                tc::fence_mbar_init();
+                for (int i = 0; i < depth && next < rows; ++i) copy(i);
+            }
+            if constexpr (WARP) __syncwarp();
+            else __syncthreads();
+        } else if (r0 < rows) {
+            fetch(r0);
         }
-        const float mu = group_sum<TPR>(s, 0.0f, red).x * inv_d;
-        float q = 0.0f;
+    }
+    // The present row's pieces as fp32.  In the ring its slot is then refilled by `refill`, after a barrier.
+    __device__ __forceinline__ void read(float (&v)[N][NV][V])
+    {
+        // a copy that never arrives leaves NaN in the row's results (the call has no status word)
+        bool ok = true;
+        if constexpr (RING) {
+            int never = 0;
+            ok = tc::mbar_wait(bars + slot * 8, phase, &never, kWaitLimitNs);
+        }
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (gt + i * TPR < pieces) {
+        for (int n = 0; n < N; ++n)
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float t = v[i][e] - mu;
-                    q = fmaf(t, t, q);
+            for (int i = 0; i < NV; ++i) {
+                const int c = gt + i * tpr;
+                if (c < pieces) {
+                    if constexpr (RING) {
+                        Piece<T, V> x;
+                        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n"
+                                     : "=r"(x.w.x), "=r"(x.w.y), "=r"(x.w.z), "=r"(x.w.w)
+                                     : "r"(ring + (uint32_t)(slot * N + n) * d * (uint32_t)sizeof(T) + c * 16)
+                                     : "memory");
+                        unpack<T, V>(x, v[n][i]);
+                        if (!ok) v[n][i][0] = __int_as_float(0x7fc00000);
+                    } else {
+                        unpack<T, V>(p[n][i], v[n][i]);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[n][i][e] = 0.0f;
                 }
             }
-        const float rs = 1.0f / sqrtf(group_sum<TPR>(q, 0.0f, red).x * inv_d + eps);
-        if (mean && gt == 0) {
+    }
+    __device__ __forceinline__ void ahead(long long r)   // registers: row r + stride
+    {
+        if constexpr (!RING)
+            if (r + stride < rows) fetch(r + stride);
+    }
+    __device__ __forceinline__ void refill()             // ring: after every thread of the group has read
+    {
+        if constexpr (RING) {
+            if (gt == 0 && next < rows) copy(slot);
+            if (++slot == depth) {
+                slot = 0;
+                phase ^= 1;
+            }
+        }
+    }
+};
+
+// Dynamic shared memory: the groups' mbarriers, then their rings (each a whole number of rows of 16-byte pieces).
+template <typename R>
+__device__ __forceinline__ void place(R& q, unsigned char* smem, int depth, int n, bool warp, int esz)
+{
+    const uint32_t group = warp ? threadIdx.x >> 5 : 0, groups = warp ? kWarpGroups : 1;
+    q.depth = depth;
+    q.bars = smem_u32(smem) + group * kMaxDepth * 8;
+    q.ring = smem_u32(smem) + groups * kMaxDepth * 8 + group * (uint32_t)(depth * n * q.d * esz);
+}
+
+template <typename T, int V, int NV, bool WARP>
+__global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : kMaxThreads)
+    ln_fwd_kernel(long long rows, int d, const T* x, const T* __restrict__ gamma, const T* __restrict__ beta, float eps,
+                  T* y, float* __restrict__ mean, float* __restrict__ rstd, int depth)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float2 red[2][32];
+    int turn = 0;
+    Rows<T, V, NV, 1, WARP, (V > 1)> q;
+    q.src[0] = x;
+    q.rows = rows;
+    q.d = d;
+    q.tpr = WARP ? 32 : blockDim.x;
+    q.gt = WARP ? threadIdx.x & 31 : threadIdx.x;
+    q.pieces = d / V;
+    q.stride = (long long)gridDim.x * (WARP ? kWarpGroups : 1);
+    place(q, smem, depth, 1, WARP, sizeof(T));
+    const float inv_d = 1.0f / (float)d;
+    long long r = WARP ? (long long)blockIdx.x * kWarpGroups + (threadIdx.x >> 5) : blockIdx.x;
+    q.start(r);
+    float g[NV][V], b[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = q.gt + i * q.tpr;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            g[i][e] = 1.0f;
+            b[i][e] = 0.0f;
+        }
+        if (gamma && c < q.pieces) unpack<T, V>(load_piece<T, V>(gamma + (size_t)c * V), g[i]);
+        if (beta && c < q.pieces) unpack<T, V>(load_piece<T, V>(beta + (size_t)c * V), b[i]);
+    }
+    for (; r < rows; r += q.stride) {    // uniform over a group
+        float v[1][NV][V];
+        q.read(v);
+        q.ahead(r);
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) s += v[0][i][e];
+        const float mu = group_sum<WARP>(s, 0.0f, red, turn).x * inv_d;
+        q.refill();
+        float sq = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (q.gt + i * q.tpr < q.pieces) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    v[0][i][e] -= mu;
+                    sq = fmaf(v[0][i][e], v[0][i][e], sq);
+                }
+            }
+        const float rs = 1.0f / sqrtf(group_sum<WARP>(sq, 0.0f, red, turn).x * inv_d + eps);
+        if (mean && q.gt == 0) {
             mean[r] = mu;
             rstd[r] = rs;
         }
         T* yr = y + r * d;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = gt + i * TPR;
-            if (c < pieces) {
-                float g[V], b[V];
-                if (gamma) load_piece<T, V>(gamma + (size_t)c * V, g);
-                if (beta) load_piece<T, V>(beta + (size_t)c * V, b);
+            const int c = q.gt + i * q.tpr;
+            if (c < q.pieces) {
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    float t = (v[i][e] - mu) * rs;
-                    if (gamma) t *= g[e];
-                    if (beta) t += b[e];
-                    v[i][e] = t;
-                }
-                store_piece<T, V>(yr + (size_t)c * V, v[i]);
+                for (int e = 0; e < V; ++e) v[0][i][e] = fmaf(v[0][i][e] * rs, g[i][e], b[i][e]);
+                store_piece<T, V>(yr + (size_t)c * V, v[0][i]);
             }
         }
     }
 }
 
-// Rows too long for registers: one CTA per row, three passes over it (L2).
+template <typename T, int V, int NV, bool WARP>
+__global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : kMaxThreads)
+    ln_bwd_kernel(long long rows, int d, const T* __restrict__ x, const T* __restrict__ gamma,
+                  const float* __restrict__ mean, const float* __restrict__ rstd, const T* dy, T* dx,
+                  float* __restrict__ part, int depth)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float2 red[2][32];
+    int turn = 0;
+    Rows<T, V, NV, 2, WARP, (V > 1)> q;
+    q.src[0] = x;
+    q.src[1] = dy;
+    q.rows = rows;
+    q.d = d;
+    q.tpr = WARP ? 32 : blockDim.x;
+    q.gt = WARP ? threadIdx.x & 31 : threadIdx.x;
+    q.pieces = d / V;
+    q.stride = (long long)gridDim.x * (WARP ? kWarpGroups : 1);
+    place(q, smem, depth, 2, WARP, sizeof(T));
+    const float inv_d = 1.0f / (float)d;
+    long long r = WARP ? (long long)blockIdx.x * kWarpGroups + (threadIdx.x >> 5) : blockIdx.x;
+    q.start(r);
+    float g[NV][V], dg[NV][V], db[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = q.gt + i * q.tpr;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            g[i][e] = 1.0f;
+            dg[i][e] = db[i][e] = 0.0f;
+        }
+        if (gamma && c < q.pieces) unpack<T, V>(load_piece<T, V>(gamma + (size_t)c * V), g[i]);
+    }
+    float mu = r < rows ? mean[r] : 0.0f, rs = r < rows ? rstd[r] : 0.0f;
+    for (; r < rows; r += q.stride) {
+        float v[2][NV][V];               // xh, a
+        q.read(v);
+        q.ahead(r);
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (q.gt + i * q.tpr < q.pieces) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    float &xh = v[0][i][e], &a = v[1][i][e];
+                    xh = (xh - mu) * rs;
+                    dg[i][e] = fmaf(a, xh, dg[i][e]);
+                    db[i][e] += a;
+                    a *= g[i][e];
+                    s1 += a;
+                    s2 = fmaf(a, xh, s2);
+                }
+            }
+        }
+        const float rs0 = rs;
+        if (r + q.stride < rows) {
+            mu = mean[r + q.stride];
+            rs = rstd[r + q.stride];
+        }
+        const float2 m = group_sum<WARP>(s1, s2, red, turn);
+        q.refill();
+        const float m1 = m.x * inv_d, m2 = m.y * inv_d;
+        T* dxr = dx + r * d;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = q.gt + i * q.tpr;
+            if (c < q.pieces) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[1][i][e] = rs0 * (v[1][i][e] - m1 - v[0][i][e] * m2);
+                store_piece<T, V>(dxr + (size_t)c * V, v[1][i]);
+            }
+        }
+    }
+    if (!part) return;
+    float* pg = part + (size_t)blockIdx.x * 2 * d;
+    if constexpr (!WARP) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = q.gt + i * q.tpr;
+            if (c < q.pieces)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    pg[(size_t)c * V + e] = dg[i][e];
+                    pg[d + (size_t)c * V + e] = db[i][e];
+                }
+        }
+    } else {
+        // the CTA's sums [2 d] take the place of the rings, whose last rows have been read by then
+        float* cols = reinterpret_cast<float*>(smem + kWarpGroups * kMaxDepth * 8);
+        __syncthreads();
+        for (int w = 0; w < kWarpGroups; ++w) {          // in group order: the same bits every time
+            if ((int)(threadIdx.x >> 5) == w) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int c = q.gt + i * q.tpr;
+                    if (c < q.pieces)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            float *qg = cols + c * V + e, *qb = qg + d;
+                            *qg = w == 0 ? dg[i][e] : *qg + dg[i][e];
+                            *qb = w == 0 ? db[i][e] : *qb + db[i][e];
+                        }
+                }
+            }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < 2 * d; c += 32 * kWarpGroups) pg[c] = cols[c];
+    }
+}
+
+// Rows too long for registers: one CTA per row, passes over it from L2.
 template <typename T>
 __global__ void __launch_bounds__(512) ln_fwd_long_kernel(long long rows, int d, const T* x, const T* __restrict__ gamma,
                                                           const T* __restrict__ beta, float eps, T* y,
                                                           float* __restrict__ mean, float* __restrict__ rstd)
 {
-    __shared__ float2 red[16];
+    __shared__ float2 red[2][32];
+    int turn = 0;
     for (long long r = blockIdx.x; r < rows; r += gridDim.x) {
         const T* xr = x + r * d;
         float s = 0.0f;
         for (int c = threadIdx.x; c < d; c += 512) s += to_float(xr[c]);
-        const float mu = group_sum<512>(s, 0.0f, red).x / (float)d;
+        const float mu = group_sum<false>(s, 0.0f, red, turn).x / (float)d;
         float q = 0.0f;
         for (int c = threadIdx.x; c < d; c += 512) {
             const float t = to_float(xr[c]) - mu;
             q = fmaf(t, t, q);
         }
-        const float rs = 1.0f / sqrtf(group_sum<512>(q, 0.0f, red).x / (float)d + eps);
+        const float rs = 1.0f / sqrtf(group_sum<false>(q, 0.0f, red, turn).x / (float)d + eps);
         if (mean && threadIdx.x == 0) {
             mean[r] = mu;
             rstd[r] = rs;
@@ -155,108 +418,14 @@ __global__ void __launch_bounds__(512) ln_fwd_long_kernel(long long rows, int d,
     }
 }
 
-template <typename T, int V, int TPR, int NV>
-__global__ void __launch_bounds__(TPR < kLnThreads ? kLnThreads : TPR)
-    ln_bwd_kernel(long long rows, int d, const T* __restrict__ x, const T* __restrict__ gamma,
-                  const float* __restrict__ mean, const float* __restrict__ rstd, const T* dy, T* dx,
-                  float* __restrict__ part)
-{
-    extern __shared__ float cols[];                    // [d] of a CTA's column sums, twice; TPR = 32 only
-    __shared__ float2 red[TPR / 32];
-    constexpr int kGroups = TPR < kLnThreads ? kLnThreads / TPR : 1;
-    const int gt = threadIdx.x % TPR, group = threadIdx.x / TPR;
-    const int pieces = d / V;
-    const float inv_d = 1.0f / (float)d;
-    float dg[NV][V], db[NV][V];
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int e = 0; e < V; ++e) dg[i][e] = db[i][e] = 0.0f;
-    const long long stride = (long long)gridDim.x * kGroups;
-    for (long long r = (long long)blockIdx.x * kGroups + group; r < rows; r += stride) {
-        const T *xr = x + r * d, *dyr = dy + r * d;
-        float xh[NV][V], a[NV][V];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = gt + i * TPR;
-            if (c < pieces) {
-                load_piece<T, V>(xr + (size_t)c * V, xh[i]);
-                load_piece<T, V>(dyr + (size_t)c * V, a[i]);
-            }
-        }
-        const float mu = mean[r], rs = rstd[r];
-        float s1 = 0.0f, s2 = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = gt + i * TPR;
-            if (c < pieces) {
-                float g[V];
-                if (gamma) load_piece<T, V>(gamma + (size_t)c * V, g);
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    xh[i][e] = (xh[i][e] - mu) * rs;
-                    dg[i][e] = fmaf(a[i][e], xh[i][e], dg[i][e]);
-                    db[i][e] += a[i][e];
-                    if (gamma) a[i][e] *= g[e];
-                    s1 += a[i][e];
-                    s2 = fmaf(a[i][e], xh[i][e], s2);
-                }
-            }
-        }
-        const float2 m = group_sum<TPR>(s1, s2, red);
-        const float m1 = m.x * inv_d, m2 = m.y * inv_d;
-        T* dxr = dx + r * d;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = gt + i * TPR;
-            if (c < pieces) {
-#pragma unroll
-                for (int e = 0; e < V; ++e) a[i][e] = rs * (a[i][e] - m1 - xh[i][e] * m2);
-                store_piece<T, V>(dxr + (size_t)c * V, a[i]);
-            }
-        }
-    }
-    if (!part) return;
-    float* pg = part + (size_t)blockIdx.x * 2 * d;
-    if constexpr (kGroups == 1) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = gt + i * TPR;
-            if (c < pieces)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    pg[(size_t)c * V + e] = dg[i][e];
-                    pg[d + (size_t)c * V + e] = db[i][e];
-                }
-        }
-    } else {
-        for (int g = 0; g < kGroups; ++g) {            // in group order: the same bits every time
-            if (group == g) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int c = gt + i * TPR;
-                    if (c < pieces)
-#pragma unroll
-                        for (int e = 0; e < V; ++e) {
-                            float *qg = cols + c * V + e, *qb = qg + d;
-                            *qg = g == 0 ? dg[i][e] : *qg + dg[i][e];
-                            *qb = g == 0 ? db[i][e] : *qb + db[i][e];
-                        }
-                }
-            }
-            __syncthreads();
-        }
-        for (int c = threadIdx.x; c < 2 * d; c += kLnThreads) pg[c] = cols[c];
-    }
-}
-
 // Rows too long for registers: dx, one CTA per row.
 template <typename T>
 __global__ void __launch_bounds__(512) ln_bwd_long_kernel(long long rows, int d, const T* __restrict__ x,
                                                           const T* __restrict__ gamma, const float* __restrict__ mean,
                                                           const float* __restrict__ rstd, const T* dy, T* dx)
 {
-    __shared__ float2 red[16];
+    __shared__ float2 red[2][32];
+    int turn = 0;
     for (long long r = blockIdx.x; r < rows; r += gridDim.x) {
         const float mu = mean[r], rs = rstd[r];
         float s1 = 0.0f, s2 = 0.0f;
@@ -266,7 +435,7 @@ __global__ void __launch_bounds__(512) ln_bwd_long_kernel(long long rows, int d,
             s1 += a;
             s2 = fmaf(a, (to_float(x[r * d + c]) - mu) * rs, s2);
         }
-        const float2 m = group_sum<512>(s1, s2, red);
+        const float2 m = group_sum<false>(s1, s2, red, turn);
         for (int c = threadIdx.x; c < d; c += 512) {
             float a = to_float(dy[r * d + c]);
             if (gamma) a *= to_float(gamma[c]);
@@ -295,31 +464,30 @@ __global__ void __launch_bounds__(128) ln_bwd_long_cols_kernel(long long rows, i
 }
 
 // dgamma / dbeta = the sum of the n partial rows [n][2 d].  A CTA takes 32
-// columns; its 8 warps add every eighth partial row, then the warps' sums meet
-// in warp order.
-__global__ void __launch_bounds__(256) ln_bwd_reduce_kernel(int n, int d, const float* __restrict__ part,
-                                                            float* __restrict__ dgamma, float* __restrict__ dbeta)
+// columns; its 32 warps add every 32nd partial row (four loads in flight each),
+// then the warps' sums meet in warp order.
+__global__ void __launch_bounds__(1024) ln_bwd_reduce_kernel(int n, int d, const float* __restrict__ part,
+                                                             float* __restrict__ dgamma, float* __restrict__ dbeta)
 {
-    __shared__ float s[8][32];
+    __shared__ float s[32][33];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;
     float a = 0.0f;
-    if (c < 2 * d)
-        for (int i = w; i < n; i += 8) a += part[(size_t)i * 2 * d + c];
+    if (c < 2 * d) {
+#pragma unroll 4
+        for (int i = w; i < n; i += 32) a += part[(size_t)i * 2 * d + c];
+    }
     s[w][lane] = a;
     __syncthreads();
     if (w == 0 && c < 2 * d) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) a += s[i][lane];
+        for (int i = 1; i < 32; ++i) a += s[i][lane];
         if (c < d) dgamma[c] = a;
         else dbeta[c - d] = a;
     }
 }
 
 // ---------------------------------------------------------------- dispatch
-
-constexpr int kFwdMax = 20;              // pieces a thread holds forward (x)
-constexpr int kMaxPartials = 1216;       // partial rows of dgamma, dbeta: 8 CTAs on each of 152 SMs
 
 bool wide(int d, int esz, const void* a, const void* b, const void* c, const void* e)
 {
@@ -343,61 +511,92 @@ struct LnArgs {
     float eps;
     void* y;                 // dx of the backward
     float *mean, *rstd, *part;
-    int nsm, grid;           // grid: CTAs of the backward, 0 forward
+    int nsm, grid;           // grid: most CTAs of the backward (partial rows), set to those launched
     cudaStream_t st;
 };
 
-template <typename T, int V, int TPR, int NV>
+// CTA size, ring depth and grid of rows of `pieces` pieces, NV per thread: a warp per row, or a CTA of the
+// least whole number of warps.  The rings of an SM's CTAs (some 512 threads of them) hold about 160 KB, and no
+// more rows than a group has.
+struct Launch {
+    int threads, grid, depth;
+    size_t smem;
+};
+template <typename K>
+cudaError_t shape_of(K kernel, const LnArgs& a, bool warp, int pieces, int nv, int matrices, size_t row_bytes,
+                     size_t sums, Launch* l)
+{
+    l->threads = warp ? 32 * kWarpGroups : ((pieces + nv - 1) / nv + 31) / 32 * 32;
+    const int groups = warp ? kWarpGroups : 1, ctas = l->threads < 512 ? 512 / l->threads : 1;
+    const long long want = (a.rows + groups - 1) / groups;
+    l->depth = 0;
+    size_t ring = 0;
+    if (row_bytes) {
+        const long long each = (a.rows + (long long)a.nsm * ctas * groups - 1) / ((long long)a.nsm * ctas * groups);
+        long long n = (160 << 10) / (ctas * groups * matrices * (long long)row_bytes);
+        if (n > each) n = each;
+        if (n > kMaxDepth) n = kMaxDepth;
+        l->depth = n < 2 ? 2 : (int)n;
+        ring = (size_t)groups * matrices * l->depth * row_bytes;
+    }
+    l->smem = (size_t)groups * kMaxDepth * 8 + (ring > sums ? ring : sums);
+    cudaError_t e = cudaSuccess;
+    if (l->smem > 48 << 10) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)l->smem);
+    if (e != cudaSuccess) return e;
+    int per_sm = 0;
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, l->threads, l->smem);
+    if (e != cudaSuccess) return e;
+    const long long cap = (long long)a.nsm * (per_sm > 0 ? per_sm : 1);
+    l->grid = (int)(want < cap ? want : cap);
+    return cudaSuccess;
+}
+
+template <typename T, int V, int NV, bool WARP>
 cudaError_t fwd_one(const LnArgs& a)
 {
-    constexpr int kThreads = TPR < kLnThreads ? kLnThreads : TPR, kGroups = kThreads / TPR;
-    const long long want = (a.rows + kGroups - 1) / kGroups, cap = (long long)a.nsm * 16;
-    ln_fwd_kernel<T, V, TPR, NV><<<(int)(want < cap ? want : cap), kThreads, 0, a.st>>>(
-        a.rows, a.d, static_cast<const T*>(a.x), static_cast<const T*>(a.gamma), static_cast<const T*>(a.beta), a.eps,
-        static_cast<T*>(a.y), a.mean, a.rstd);
+    Launch l;
+    auto kernel = ln_fwd_kernel<T, V, NV, WARP>;
+    cudaError_t e = shape_of(kernel, a, WARP, a.d / V, NV, 1, V > 1 ? sizeof(T) * a.d : 0, 0, &l);
+    if (e != cudaSuccess) return e;
+    kernel<<<l.grid, l.threads, l.smem, a.st>>>(a.rows, a.d, static_cast<const T*>(a.x), static_cast<const T*>(a.gamma),
+                                                static_cast<const T*>(a.beta), a.eps, static_cast<T*>(a.y), a.mean,
+                                                a.rstd, l.depth);
     return cudaGetLastError();
 }
-template <typename T, int V, int TPR, int NV>
-cudaError_t bwd_one(const LnArgs& a)
+template <typename T, int V, int NV, bool WARP>
+cudaError_t bwd_one(LnArgs& a)
 {
-    constexpr int kThreads = TPR < kLnThreads ? kLnThreads : TPR;
-    const size_t smem = TPR < kLnThreads && a.part ? sizeof(float) * 2 * a.d : 0;
-    ln_bwd_kernel<T, V, TPR, NV><<<a.grid, kThreads, smem, a.st>>>(
-        a.rows, a.d, static_cast<const T*>(a.x), static_cast<const T*>(a.gamma), a.mean, a.rstd,
-        static_cast<const T*>(a.dy), static_cast<T*>(a.y), a.part);
+    Launch l;
+    auto kernel = ln_bwd_kernel<T, V, NV, WARP>;
+    cudaError_t e = shape_of(kernel, a, WARP, a.d / V, NV, 2, V > 1 ? sizeof(T) * a.d : 0,
+                             WARP && a.part ? sizeof(float) * 2 * a.d : 0, &l);
+    if (e != cudaSuccess) return e;
+    if (a.part && l.grid > a.grid) l.grid = a.grid;
+    a.grid = l.grid;
+    kernel<<<l.grid, l.threads, l.smem, a.st>>>(a.rows, a.d, static_cast<const T*>(a.x), static_cast<const T*>(a.gamma),
+                                                a.mean, a.rstd, static_cast<const T*>(a.dy), static_cast<T*>(a.y),
+                                                a.part, l.depth);
     return cudaGetLastError();
 }
 
-// The instantiation whose TPR x NV pieces hold the row: NV is rounded up along this list.
-template <typename T, int V, int TPR>
-cudaError_t fwd_nv(const LnArgs& a, int nv)
-{
-    if (nv <= 1) return fwd_one<T, V, TPR, 1>(a);
-    if (nv <= 2) return fwd_one<T, V, TPR, 2>(a);
-    if (nv <= 4) return fwd_one<T, V, TPR, 4>(a);
-    if (nv <= 6) return fwd_one<T, V, TPR, 6>(a);
-    if (nv <= 10) return fwd_one<T, V, TPR, 10>(a);
-    return fwd_one<T, V, TPR, kFwdMax>(a);
-}
-template <typename T, int V, int TPR, int MAX>
-cudaError_t bwd_nv(const LnArgs& a, int nv)
-{
-    if (nv <= 1) return bwd_one<T, V, TPR, 1>(a);
-    if (nv <= 2) return bwd_one<T, V, TPR, 2>(a);
-    if (nv <= 4) return bwd_one<T, V, TPR, 4>(a);
-    if constexpr (MAX > 6)
-        if (nv > 6) return bwd_one<T, V, TPR, MAX>(a);
-    return bwd_one<T, V, TPR, 6>(a);
-}
-
+// A warp per row up to two 16-byte pieces a lane (8 elements a lane element by element), then a CTA per
+// row: the pieces a thread holds are bounded by its registers (forward x, gamma and beta as fp32,
+// backward x, dy, gamma and two sums).
 template <typename T, int V>
 cudaError_t fwd(const LnArgs& a)
 {
     const int pieces = a.d / V;
-    auto nv = [&](int tpr) { return (pieces + tpr - 1) / tpr; };
-    if (nv(32) <= kFwdMax) return fwd_nv<T, V, 32>(a, nv(32));
-    if (nv(128) <= kFwdMax) return fwd_nv<T, V, 128>(a, nv(128));
-    if (nv(512) <= kFwdMax) return fwd_nv<T, V, 512>(a, nv(512));
+    if constexpr (V > 1) {
+        if (pieces <= 32) return fwd_one<T, V, 1, true>(a);
+        if (pieces <= 64) return fwd_one<T, V, 2, true>(a);
+        if (pieces <= 2 * 128) return fwd_one<T, V, 2, false>(a);
+        if (pieces <= 4 * kMaxThreads) return fwd_one<T, V, 4, false>(a);
+    } else {
+        if (pieces <= 4 * 32) return fwd_one<T, V, 4, true>(a);
+        if (pieces <= 8 * 32) return fwd_one<T, V, 8, true>(a);
+        if (pieces <= 4 * kMaxThreads) return fwd_one<T, V, 4, false>(a);
+        if (pieces <= 16 * kMaxThreads) return fwd_one<T, V, 16, false>(a);
+    }
     const long long cap = (long long)a.nsm * 4;
     ln_fwd_long_kernel<T><<<(int)(a.rows < cap ? a.rows : cap), 512, 0, a.st>>>(
         a.rows, a.d, static_cast<const T*>(a.x), static_cast<const T*>(a.gamma), static_cast<const T*>(a.beta), a.eps,
@@ -405,20 +604,21 @@ cudaError_t fwd(const LnArgs& a)
     return cudaGetLastError();
 }
 
-template <int V>
-constexpr int bwd_max()                  // pieces a thread holds backward (x, dy and two column sums)
-{
-    return V == 1 ? 16 : 6;
-}
 template <typename T, int V>
-cudaError_t bwd(const LnArgs& a)
+cudaError_t bwd(LnArgs& a)
 {
-    constexpr int MAX = bwd_max<V>();
     const int pieces = a.d / V;
-    auto nv = [&](int tpr) { return (pieces + tpr - 1) / tpr; };
-    if (nv(32) <= MAX) return bwd_nv<T, V, 32, MAX>(a, nv(32));
-    if (nv(128) <= MAX) return bwd_nv<T, V, 128, MAX>(a, nv(128));
-    if (nv(512) <= MAX) return bwd_nv<T, V, 512, MAX>(a, nv(512));
+    if constexpr (V > 1) {
+        if (pieces <= 32) return bwd_one<T, V, 1, true>(a);
+        if (pieces <= 64) return bwd_one<T, V, 2, true>(a);
+        if (pieces <= 2 * kMaxThreads) return bwd_one<T, V, 2, false>(a);
+        if (pieces <= 4 * kMaxThreads) return bwd_one<T, V, 4, false>(a);
+    } else {
+        if (pieces <= 4 * 32) return bwd_one<T, V, 4, true>(a);
+        if (pieces <= 8 * 32) return bwd_one<T, V, 8, true>(a);
+        if (pieces <= 4 * kMaxThreads) return bwd_one<T, V, 4, false>(a);
+        if (pieces <= 16 * kMaxThreads) return bwd_one<T, V, 16, false>(a);
+    }
     if (a.part) {
         const dim3 grid((a.d + 127) / 128, a.grid);
         ln_bwd_long_cols_kernel<T><<<grid, 128, 0, a.st>>>(a.rows, a.d, static_cast<const T*>(a.x), a.mean, a.rstd,
@@ -431,12 +631,12 @@ cudaError_t bwd(const LnArgs& a)
     return cudaGetLastError();
 }
 
-// CTAs of the backward: at most 8 on each SM, and no more than the rows fill with two rows per group,
-// so that a partial row stands for several rows of the sum.
+// Most CTAs of the backward, each of which leaves a partial row: 8 on each of 152 SMs, and no more than
+// leave four rows to a CTA.
 int bwd_grid(long long rows)
 {
-    const long long want = (rows + 7) / 8;
-    return (int)(want < kMaxPartials ? want : kMaxPartials);
+    const long long want = (rows + 3) / 4;
+    return (int)(want < 1216 ? want : 1216);
 }
 
 }  // namespace
@@ -467,7 +667,7 @@ cudaError_t launch_layer_norm_backward(rola_dtype_t dt, long long rows, int d, c
     else
         e = wide(d, 4, x, gamma, dy, dx) ? bwd<float, 4>(a) : bwd<float, 1>(a);
     if (e != cudaSuccess || !dgamma) return e;
-    ln_bwd_reduce_kernel<<<(2 * d + 31) / 32, 256, 0, st>>>(a.grid, d, part, dgamma, dbeta);
+    ln_bwd_reduce_kernel<<<(2 * d + 31) / 32, 1024, 0, st>>>(a.grid, d, part, dgamma, dbeta);
     return cudaGetLastError();
 }
 

@@ -302,11 +302,19 @@ def _dtype_of(t, where: str) -> int:
     return _DTYPES[t.dtype]
 
 
-def _expect(where: str, dtype, **tensors):
-    """Each tensor=(t, shape) is of `dtype` and of that shape; a None tensor is left to the library."""
-    for name, (t, shape) in tensors.items():
-        if t is not None and (t.dtype != dtype or tuple(t.shape) != shape):
-            raise ValueError(f"{where}: {name} must be {dtype} of shape {shape}, not {t.dtype} {tuple(t.shape)}")
+def _a(t, dtype, shape, where: str, name: str):
+    """The address of tensor `t` (None: NULL, which the library judges), checked against its dtype and shape."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{where}: {name} must be a contiguous CUDA tensor, {dtype} of shape {tuple(shape)}, not "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _st(t, stream):
+    """The stream a call on tensor `t` goes to: the given one, or the current one of t's device."""
+    return torch._C._cuda_getCurrentRawStream(t.device.index) if stream is None else stream.cuda_stream
 
 
 def _bytes(n: int, where: str, device) -> torch.Tensor:
@@ -315,36 +323,42 @@ def _bytes(n: int, where: str, device) -> torch.Tensor:
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _rows_of(x):
-    d = x.shape[-1]
-    return (x.numel() // d if d else 0), d
+def _ws(ws, where: str):
+    return _a(ws, torch.uint8, ws.shape, where, "ws"), ws.numel()
+
+
+_F32 = torch.float32
 
 
 def layer_norm(x, gamma, beta, eps: float, y, mean=None, rstd=None, stream=None):
     """y = (x - mean) rstd gamma + beta over the last axis of x; gamma and beta [d] in x's dtype or None.
     mean and rstd (fp32, one per row), if given, receive what layer_norm_backward reads."""
-    w, (rows, d) = "rola_layer_norm", _rows_of(x)
-    dt = _dtype_of(x, w)
-    _expect(w, x.dtype, gamma=(gamma, (d,)), beta=(beta, (d,)), y=(y, tuple(x.shape)))
-    _expect(w, torch.float32, mean=(mean, tuple(x.shape[:-1])), rstd=(rstd, tuple(x.shape[:-1])))
-    _check(_lib.rola_layer_norm(rows, d, dt, _p(x), _p(gamma), _p(beta), eps, _p(y), _p(mean), _p(rstd),
-                                _stream(stream)), w)
+    w, dt, shape = "rola_layer_norm", x.dtype, x.shape
+    d, code = shape[-1], _dtype_of(x, "rola_layer_norm")
+    st = _lib.rola_layer_norm(x.numel() // max(d, 1), d, code, _a(x, dt, shape, w, "x"), _a(gamma, dt, (d,), w, "gamma"),
+                              _a(beta, dt, (d,), w, "beta"), eps, _a(y, dt, shape, w, "y"),
+                              _a(mean, _F32, shape[:-1], w, "mean"), _a(rstd, _F32, shape[:-1], w, "rstd"),
+                              _st(x, stream))
+    if st:
+        raise RolaError(st, w)
 
 
 def layer_norm_backward_workspace(x) -> torch.Tensor:
-    w, (rows, d) = "rola_layer_norm_backward_workspace_bytes", _rows_of(x)
-    return _bytes(_lib.rola_layer_norm_backward_workspace_bytes(rows, d, _dtype_of(x, w)), w, x.device)
+    w, d = "rola_layer_norm_backward_workspace_bytes", x.shape[-1]
+    return _bytes(_lib.rola_layer_norm_backward_workspace_bytes(x.numel() // max(d, 1), d, _dtype_of(x, w)), w, x.device)
 
 
 def layer_norm_backward(x, gamma, mean, rstd, dy, dx, dgamma, dbeta, ws, stream=None):
     """dx of layer_norm, and dgamma, dbeta (fp32 [d], or both None)."""
-    w, (rows, d) = "rola_layer_norm_backward", _rows_of(x)
-    dt = _dtype_of(x, w)
-    _expect(w, x.dtype, gamma=(gamma, (d,)), dy=(dy, tuple(x.shape)), dx=(dx, tuple(x.shape)))
-    _expect(w, torch.float32, mean=(mean, tuple(x.shape[:-1])), rstd=(rstd, tuple(x.shape[:-1])),
-            dgamma=(dgamma, (d,)), dbeta=(dbeta, (d,)))
-    _check(_lib.rola_layer_norm_backward(rows, d, dt, _p(x), _p(gamma), _p(mean), _p(rstd), _p(dy), _p(dx), _p(dgamma),
-                                         _p(dbeta), _p(ws), ws.numel(), _stream(stream)), w)
+    w, dt, shape = "rola_layer_norm_backward", x.dtype, x.shape
+    d, code = shape[-1], _dtype_of(x, "rola_layer_norm_backward")
+    st = _lib.rola_layer_norm_backward(
+        x.numel() // max(d, 1), d, code, _a(x, dt, shape, w, "x"), _a(gamma, dt, (d,), w, "gamma"),
+        _a(mean, _F32, shape[:-1], w, "mean"), _a(rstd, _F32, shape[:-1], w, "rstd"), _a(dy, dt, shape, w, "dy"),
+        _a(dx, dt, shape, w, "dx"), _a(dgamma, _F32, (d,), w, "dgamma"), _a(dbeta, _F32, (d,), w, "dbeta"), *_ws(ws, w),
+        _st(x, stream))
+    if st:
+        raise RolaError(st, w)
 
 
 def make_ffn_config(tokens: int, d_model: int, d_ff: int, act="silu", dtype: int = ROLA_BF16) -> RolaFfnConfig:
@@ -357,43 +371,42 @@ def make_ffn_config(tokens: int, d_model: int, d_ff: int, act="silu", dtype: int
 
 
 def ffn_workspace(c: RolaFfnConfig, device="cuda") -> torch.Tensor:
-    return _bytes(_lib.rola_ffn_workspace_bytes(ctypes.byref(c)), "rola_ffn_workspace_bytes", device)
+    return _bytes(_lib.rola_ffn_workspace_bytes(c), "rola_ffn_workspace_bytes", device)
 
 
 def ffn_backward_workspace(c: RolaFfnConfig, device="cuda") -> torch.Tensor:
-    return _bytes(_lib.rola_ffn_backward_workspace_bytes(ctypes.byref(c)), "rola_ffn_backward_workspace_bytes", device)
-
-
-def _expect_ffn(w, c, X, W_gate, W_up, W_down, **rows):
-    m, d, f = (c.tokens, c.d_model), (c.d_ff, c.d_model), (c.d_model, c.d_ff)
-    _expect(w, _TORCH_DTYPES.get(c.dtype), X=(X, m), W_gate=(W_gate, d), W_up=(W_up, d), W_down=(W_down, f),
-            **{n: (t, m) for n, t in rows.items()})
+    return _bytes(_lib.rola_ffn_backward_workspace_bytes(c), "rola_ffn_backward_workspace_bytes", device)
 
 
 def ffn(c, X, W_gate, W_up, W_down, Y, ws, stream=None):
     """Y = (phi(X W_gate^T) * (X W_up^T)) W_down^T; X, Y [tokens][d_model], weights in the nn.Linear layout."""
-    _expect_ffn("rola_ffn", c, X, W_gate, W_up, W_down, Y=Y)
-    _check(_lib.rola_ffn(ctypes.byref(c), _p(X), _p(W_gate), _p(W_up), _p(W_down), _p(Y), _p(ws), ws.numel(),
-                         _stream(stream)), "rola_ffn")
+    w, dt, m, d, f = "rola_ffn", _TORCH_DTYPES.get(c.dtype), c.tokens, c.d_model, c.d_ff
+    st = _lib.rola_ffn(c, _a(X, dt, (m, d), w, "X"), _a(W_gate, dt, (f, d), w, "W_gate"), _a(W_up, dt, (f, d), w, "W_up"),
+                       _a(W_down, dt, (d, f), w, "W_down"), _a(Y, dt, (m, d), w, "Y"), *_ws(ws, w), _st(X, stream))
+    if st:
+        raise RolaError(st, w)
 
 
 def ffn_train(c, X, W_gate, W_up, W_down, Y, G, U, ws, stream=None):
     """ffn keeping G = X W_gate^T and U = X W_up^T (fp32 [tokens][d_ff]) for ffn_backward."""
-    w, kept = "rola_ffn_train", (c.tokens, c.d_ff)
-    _expect_ffn(w, c, X, W_gate, W_up, W_down, Y=Y)
-    _expect(w, torch.float32, G=(G, kept), U=(U, kept))
-    _check(_lib.rola_ffn_train(ctypes.byref(c), _p(X), _p(W_gate), _p(W_up), _p(W_down), _p(Y), _p(G), _p(U), _p(ws),
-                               ws.numel(), _stream(stream)), w)
+    w, dt, m, d, f = "rola_ffn_train", _TORCH_DTYPES.get(c.dtype), c.tokens, c.d_model, c.d_ff
+    st = _lib.rola_ffn_train(c, _a(X, dt, (m, d), w, "X"), _a(W_gate, dt, (f, d), w, "W_gate"),
+                             _a(W_up, dt, (f, d), w, "W_up"), _a(W_down, dt, (d, f), w, "W_down"), _a(Y, dt, (m, d), w, "Y"),
+                             _a(G, _F32, (m, f), w, "G"), _a(U, _F32, (m, f), w, "U"), *_ws(ws, w), _st(X, stream))
+    if st:
+        raise RolaError(st, w)
 
 
 def ffn_backward(c, X, W_gate, W_up, W_down, G, U, dY, dX, dW_gate, dW_up, dW_down, ws, stream=None):
     """Gradients of ffn_train: dX and the three weights', in the weights' dtype."""
-    w, kept = "rola_ffn_backward", (c.tokens, c.d_ff)
-    _expect_ffn(w, c, X, W_gate, W_up, W_down, dY=dY, dX=dX)
-    _expect_ffn(w, c, X, dW_gate, dW_up, dW_down)
-    _expect(w, torch.float32, G=(G, kept), U=(U, kept))
-    _check(_lib.rola_ffn_backward(ctypes.byref(c), _p(X), _p(W_gate), _p(W_up), _p(W_down), _p(G), _p(U), _p(dY),
-                                  _p(dX), _p(dW_gate), _p(dW_up), _p(dW_down), _p(ws), ws.numel(), _stream(stream)), w)
+    w, dt, m, d, f = "rola_ffn_backward", _TORCH_DTYPES.get(c.dtype), c.tokens, c.d_model, c.d_ff
+    st = _lib.rola_ffn_backward(
+        c, _a(X, dt, (m, d), w, "X"), _a(W_gate, dt, (f, d), w, "W_gate"), _a(W_up, dt, (f, d), w, "W_up"),
+        _a(W_down, dt, (d, f), w, "W_down"), _a(G, _F32, (m, f), w, "G"), _a(U, _F32, (m, f), w, "U"),
+        _a(dY, dt, (m, d), w, "dY"), _a(dX, dt, (m, d), w, "dX"), _a(dW_gate, dt, (f, d), w, "dW_gate"),
+        _a(dW_up, dt, (f, d), w, "dW_up"), _a(dW_down, dt, (d, f), w, "dW_down"), *_ws(ws, w), _st(X, stream))
+    if st:
+        raise RolaError(st, w)
 
 
 def make_attention_config(B: int, H: int, H_kv: int, Lq: int, Lk: int, causal: bool = False, scale: float = 0.0,
@@ -406,37 +419,36 @@ def make_attention_config(B: int, H: int, H_kv: int, Lq: int, Lk: int, causal: b
 
 
 def attention_workspace(c: RolaAttentionConfig, device="cuda") -> torch.Tensor:
-    return _bytes(_lib.rola_attention_workspace_bytes(ctypes.byref(c)), "rola_attention_workspace_bytes", device)
+    return _bytes(_lib.rola_attention_workspace_bytes(c), "rola_attention_workspace_bytes", device)
 
 
 def attention_backward_workspace(c: RolaAttentionConfig, device="cuda") -> torch.Tensor:
-    return _bytes(_lib.rola_attention_backward_workspace_bytes(ctypes.byref(c)),
-                  "rola_attention_backward_workspace_bytes", device)
-
-
-def _expect_attention(w, c, queries, keys, kv_len, lse):
-    rows, cols = (c.B, c.H, c.Lq, c.d_h), (c.B, c.H_kv, c.Lk, c.d_h)
-    _expect(w, _TORCH_DTYPES.get(c.dtype), **{n: (t, rows) for n, t in queries.items()},
-            **{n: (t, cols) for n, t in keys.items()})
-    _expect(w, torch.int32, kv_len=(kv_len, (c.B,)))
-    _expect(w, torch.float32, lse=(lse, rows[:3]))
+    return _bytes(_lib.rola_attention_backward_workspace_bytes(c), "rola_attention_backward_workspace_bytes", device)
 
 
 def attention(c, q, k, v, kv_len, o, lse, ws, stream=None):
     """o = softmax(scale q k^T) v over the first kv_len[b] keys (int32 [B]; None: all), causal if c.causal;
     q, o [B][H][Lq][128], k, v [B][H_kv][Lk][128].  lse (fp32 [B][H][Lq]) is what attention_backward reads."""
-    w = "rola_attention"
-    _expect_attention(w, c, dict(q=q, o=o), dict(k=k, v=v), kv_len, lse)
-    _check(_lib.rola_attention(ctypes.byref(c), _p(q), _p(k), _p(v), _p(kv_len), _p(o), _p(lse), _p(ws), ws.numel(),
-                               _stream(stream)), w)
+    w, dt = "rola_attention", _TORCH_DTYPES.get(c.dtype)
+    rows, keys = (c.B, c.H, c.Lq, c.d_h), (c.B, c.H_kv, c.Lk, c.d_h)
+    st = _lib.rola_attention(c, _a(q, dt, rows, w, "q"), _a(k, dt, keys, w, "k"), _a(v, dt, keys, w, "v"),
+                             _a(kv_len, torch.int32, rows[:1], w, "kv_len"), _a(o, dt, rows, w, "o"),
+                             _a(lse, _F32, rows[:3], w, "lse"), *_ws(ws, w), _st(q, stream))
+    if st:
+        raise RolaError(st, w)
 
 
 def attention_backward(c, q, k, v, kv_len, o, lse, dO, dq, dk, dv, ws, stream=None):
     """Gradients of attention from its o and lse; the probabilities are recomputed."""
-    w = "rola_attention_backward"
-    _expect_attention(w, c, dict(q=q, o=o, dO=dO, dq=dq), dict(k=k, v=v, dk=dk, dv=dv), kv_len, lse)
-    _check(_lib.rola_attention_backward(ctypes.byref(c), _p(q), _p(k), _p(v), _p(kv_len), _p(o), _p(lse), _p(dO),
-                                        _p(dq), _p(dk), _p(dv), _p(ws), ws.numel(), _stream(stream)), w)
+    w, dt = "rola_attention_backward", _TORCH_DTYPES.get(c.dtype)
+    rows, keys = (c.B, c.H, c.Lq, c.d_h), (c.B, c.H_kv, c.Lk, c.d_h)
+    st = _lib.rola_attention_backward(
+        c, _a(q, dt, rows, w, "q"), _a(k, dt, keys, w, "k"), _a(v, dt, keys, w, "v"),
+        _a(kv_len, torch.int32, rows[:1], w, "kv_len"), _a(o, dt, rows, w, "o"), _a(lse, _F32, rows[:3], w, "lse"),
+        _a(dO, dt, rows, w, "dO"), _a(dq, dt, rows, w, "dq"), _a(dk, dt, keys, w, "dk"), _a(dv, dt, keys, w, "dv"),
+        *_ws(ws, w), _st(q, stream))
+    if st:
+        raise RolaError(st, w)
 
 
 def get_device_status(ws, stream=None) -> int:
