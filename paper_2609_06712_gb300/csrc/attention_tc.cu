@@ -5,30 +5,32 @@
 //
 // Rows are the G Lq queries of the heads that share a key head (contiguous in
 // q), so a shared key head is read once for all of them.  An item is 256 rows of
-// a head (two groups of 128) over a range of its key tiles of 128 keys:
-//   S_g  = Q_g (128 rows x 128 d, smem, K-major)  x  K^T (128 keys, smem, K-major)
-//   O_g += P_g (128 rows x 128 keys, TMEM, bf16)  x  V   (128 keys x 128 d, smem, MN-major)
-// TMEM (512 columns): S_0, S_1, O_0, O_1, 128 columns each; P_g overwrites the
-// first 64 columns of S_g.  One thread issues all products in the order
-// PV_0(t) QK_0(t+1) PV_1(t) QK_1(t+1): products of one thread execute in order,
-// so QK_g(t+1) may overwrite S_g / P_g, and S_g(t+1) being complete implies
-// that O_g holds PV_g(t).  While a group's softmax runs, the tensor core does
-// the other group's products; at an item's end the next item's first QK is
-// issued the same way, so items follow one another without a gap.
+// a head (two groups of 128) over a range of its keys, which come in tiles of 128
+// and are worked on in steps of 64:
+//   S_g  = Q_g (128 rows x 128 d, smem, K-major)  x  K^T (64 keys x 128 d, smem, K-major)
+//   O_g += P_g (128 rows x 64 keys, TMEM, bf16)   x  V   (64 keys x 128 d, smem, MN-major)
+// TMEM (512 columns): per group two S buffers of 64 columns and O, 128 columns;
+// P overwrites the first half of its S buffer.  One thread issues all products;
+// after PV_g(n) comes QK_g(n + 2) into the same buffer (products of one thread
+// execute in order), so a group's softmax has its next scores ready when it is
+// done with the present ones, and the two groups' softmax runs under each other's
+// products.  Steps run on across items, so items follow one another without a gap.
+// With steps of 128 TMEM would hold one S buffer per group, and QK(n + 1) would
+// wait for PV(n), and that for the softmax of step n.
 //
 // Softmax (base 2, one thread per row, the whole row of S in registers): each
 // row keeps -m and its sum l in fp32.  With t = s scale log2(e) - m, m is raised
-// only when the tile's largest t exceeds 2^3 (or on the item's first tile); O
+// only when the step's largest t exceeds 2^3 (or on the item's first step); O
 // and l are then scaled by 2^(m_old - m_new).  p = 2^t enters l in fp32 and the
 // product rounded to bf16 (the operand type of the tensor core).  A row sees a
 // prefix of the keys (its length, or its causal limit), so a row that sees
-// nothing in the item's first tile sees nothing in the item: its p stay 0, l = 0.
+// nothing in the item's first step sees nothing in the item: its p stay 0, l = 0.
 // Keys past the length: their scores are replaced by -inf whatever they are, and
 // their rows of V are zeroed in shared memory (0 x NaN would be NaN).
 //
-// Warps (320 threads, one persistent CTA per SM): 0-3 softmax and epilogue of
+// Warps (352 threads, one persistent CTA per SM): 0-3 softmax and epilogue of
 // group 0, 4-7 of group 1, 8 TMA (Q of both groups, and K, V tiles in one ring of
-// five 32 KB slots), 9 products.  Shared memory 64 + 160 KB.  Every mbarrier wait
+// five 32 KB slots), 9 products, 10 the zeroing of V's rows.  Shared memory 64 + 160 KB.  Every mbarrier wait
 // is bounded; a wait that gives up records ROLA_ERR_TIMEOUT and the CTA drains
 // what it issued and frees its TMEM.
 #include "attention_tc.cuh"
@@ -38,15 +40,16 @@ namespace {
 
 using namespace tc;
 
-constexpr int kRows = 128, kKeys = 128, kSlots = 5;
-constexpr int kTmaWarp = 8, kMmaWarp = 9, kThreads = 320;
+constexpr int kRows = 128, kKeys = 128, kStep = 64, kSlots = 5;    // rows of a group, keys of a tile and of a step
+constexpr int kTmaWarp = 8, kMmaWarp = 9, kCutWarp = 10, kThreads = 352;
 constexpr uint32_t kTileBytes = 128 * 128 * 2;               // [d-chunk][128 rows][64]
 constexpr uint32_t kSmemQ = 0, kSmemKV = 2 * kTileBytes, kSmemTiles = kSmemKV + kSlots * kTileBytes;
-constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;   // S_g at 128 g, O_g at 256 + 128 g
+constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;   // S_g,b at 128 g + 64 b, O_g at 256 + 128 g
 constexpr float kRescaleThreshold = 8.0f;                    // log2 units
 
-enum Bar { Q_FULL = 0, Q_EMPTY = 2, S_FULL = 4, P_FULL = 6, O_FULL = 8, O_EMPTY = 10, KV_FULL = 12,
-           KV_EMPTY = KV_FULL + kSlots, DRAIN = KV_EMPTY + kSlots, NUM_BARS = DRAIN + 1 };
+// S_FULL, P_FULL, PV_DONE: 2 g + b
+enum Bar { Q_FULL = 0, Q_EMPTY = 2, S_FULL = 4, P_FULL = 8, PV_DONE = 12, O_FULL = 16, O_EMPTY = 18, KV_FULL = 20,
+           KV_EMPTY = KV_FULL + kSlots, V_CUT = KV_EMPTY + kSlots, DRAIN, NUM_BARS };
 
 struct Ctrl {
     uint64_t bar[NUM_BARS];
@@ -61,6 +64,7 @@ struct Params {
     __nv_bfloat16* o;
     float *lse, *part_o, *part_lse;
     DeviceStatus* status;
+    bool wide;                   // o is 32-byte aligned
     int q_tiles;                 // 256-row tiles of a head
     int items;                   // q_tiles heads splits
 };
@@ -70,19 +74,22 @@ __device__ __forceinline__ void record_timeout(const Params& p, int where)
     if (atomicCAS(&p.status->code, 0, (int)ROLA_ERR_TIMEOUT) == 0) p.status->where = 80 + where;
 }
 
-// One item: rows r0 .. of `head`, key tiles first .. first + T[g] of group g (T[g] 0: the group has no
-// rows, or its rows see nothing there).
+// One item: rows r0 .. of `head`, key tiles from `first`, H0 and H1 steps of the two groups from
+// there (0: the group has no rows, or its rows see nothing there).
 struct Item {
     int head, r0, len, part, first;
-    int T0, T1, T;               // per group, and the larger
+    int H0, H1, H;               // per group, and the larger
     bool has1;
 };
 __device__ __forceinline__ Item item_of(const Params& p, int i)
 {
     const AttnShape& s = p.s;
     Item it;
-    it.part = i % s.splits;
-    i /= s.splits;
+    it.part = 0;
+    if (s.splits > 1) {
+        it.part = i % s.splits;
+        i /= s.splits;
+    }
     int qt;
     if (s.causal) {              // the longest rows of every head first
         qt = p.q_tiles - 1 - i / s.heads;
@@ -94,16 +101,27 @@ __device__ __forceinline__ Item item_of(const Params& p, int i)
     it.r0 = qt * 2 * kRows;
     it.len = attn_len(s, p.kv_len, it.head / s.Hk);
     it.has1 = it.r0 + kRows < s.R;
-    const int last0 = min(it.r0 + kRows, s.R) - 1, last1 = min(it.r0 + 2 * kRows, s.R) - 1;
-    const int n0 = attn_seen_most(s, it.len, it.r0, last0);
-    const int n1 = it.has1 ? attn_seen_most(s, it.len, it.r0 + kRows, last1) : 0;
-    const int t0 = (n0 + kKeys - 1) / kKeys, t1 = (n1 + kKeys - 1) / kKeys, t = max(t0, t1);
-    it.first = (int)((long long)t * it.part / s.splits);
-    const int end = (int)((long long)t * (it.part + 1) / s.splits);
-    it.T0 = max(min(t0, end) - it.first, 0);
-    it.T1 = max(min(t1, end) - it.first, 0);
-    it.T = max(it.T0, it.T1);
+    const int n0 = attn_seen_most(s, it.len, it.r0, min(it.r0 + kRows, s.R) - 1);
+    const int n1 = it.has1 ? attn_seen_most(s, it.len, it.r0 + kRows, min(it.r0 + 2 * kRows, s.R) - 1) : 0;
+    const int t = (max(n0, n1) + kKeys - 1) / kKeys;
+    int end = t;
+    it.first = 0;
+    if (s.splits > 1) {          // tiles x parts stays below 2^31: at most 2^23 tiles and 152 parts
+        it.first = t * it.part / s.splits;
+        end = t * (it.part + 1) / s.splits;
+    }
+    const int from = it.first * 2;
+    it.H0 = max(min((n0 + kStep - 1) / kStep, end * 2) - from, 0);
+    it.H1 = max(min((n1 + kStep - 1) / kStep, end * 2) - from, 0);
+    it.H = max(it.H0, it.H1);
     return it;
+}
+
+// Tile t of the item ends past the sequence's length, where the memory holds other keys (past Lk the copy
+// writes zeros).
+__device__ __forceinline__ bool cut_tile(const AttnShape& s, const Item& it, int t)
+{
+    return (it.first + t + 1) * kKeys > it.len && it.len < s.Lk;
 }
 
 __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_constant__ CUtensorMap map_q,
@@ -128,8 +146,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
         for (int g = 0; g < 2; ++g) {
             mbar_init(bar(Q_FULL + g), 1);
             mbar_init(bar(Q_EMPTY + g), 1);
-            mbar_init(bar(S_FULL + g), 1);
-            mbar_init(bar(P_FULL + g), 4);
+            for (int b = 0; b < 2; ++b) {
+                mbar_init(bar(S_FULL + 2 * g + b), 1);
+                mbar_init(bar(P_FULL + 2 * g + b), 4);
+                mbar_init(bar(PV_DONE + 2 * g + b), 1);
+            }
             mbar_init(bar(O_FULL + g), 1);
             mbar_init(bar(O_EMPTY + g), 4);
         }
@@ -137,6 +158,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
             mbar_init(bar(KV_FULL + i), 1);
             mbar_init(bar(KV_EMPTY + i), 1);
         }
+        mbar_init(bar(V_CUT), 1);
         mbar_init(bar(DRAIN), 1);
         fence_mbar_init();
     }
@@ -175,9 +197,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
         };
         for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
             const Item it = item_of(p, i);
-            if (it.T == 0) continue;
+            if (it.H == 0) continue;
             for (int g = 0; g < 2 && ok; ++g) {
-                if ((g ? it.T1 : it.T0) == 0) continue;
+                if ((g ? it.H1 : it.H0) == 0) continue;
                 if (nq[g] >= 1) ok = mbar_wait(bar(Q_EMPTY + g), (nq[g] - 1) & 1, abort, limit);
                 ok = __shfl_sync(0xffffffffu, ok, 0);
                 if (!ok) break;
@@ -188,7 +210,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
                                 lane * 64, it.r0 + g * kRows, it.head);
                 ++nq[g];
             }
-            for (int t = 0; t < it.T && ok; ++t) {
+            for (int t = 0; t < (it.H + 1) / 2 && ok; ++t) {
                 const int key0 = (it.first + t) * kKeys;
                 // test hook: the CTA's first K tile is never loaded, so the waits on it run out
                 ring(&map_k, key0, it.head, (s.debug_flags & ROLA_DEBUG_SKIP_FIRST_K_COPY) && c == 0);
@@ -206,103 +228,107 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
         }
     } else if (warp == kMmaWarp) {
         // ------------------------------------------------------------ products
-        // The whole warp runs the loop (it zeroes rows of V together); lane 0 issues.
-        const uint32_t id_qk = idesc_bf16(kRows, kKeys, false, false), id_pv = idesc_bf16(kRows, kDh, false, true);
-        const uint64_t dq = smem_desc(sbase + kSmemQ, 16, 1024);                      // A of QK (K-major)
-        const uint64_t dk = smem_desc(sbase + kSmemKV, 16, 1024);                     // B of QK (K-major)
-        const uint64_t dv = smem_desc(sbase + kSmemKV, kTileBytes / 2, 1024);         // B of PV (MN-major)
-        const uint32_t q_lo = (uint32_t)dq, q_hi = (uint32_t)(dq >> 32), k_lo = (uint32_t)dk, k_hi = (uint32_t)(dk >> 32);
-        const uint32_t v_lo = (uint32_t)dv, v_hi = (uint32_t)(dv >> 32);
-        bool ok = true;
-        int u = 0;                                       // tiles whose V was used; K of tile u in slot 2u, V in 2u + 1
-        int np[2] = {0, 0}, nq[2] = {0, 0}, no[2] = {0, 0};   // per group: P tiles, Q tiles, items with O
-        auto wait = [&](int b, int parity) {
-            if (ok) ok = __shfl_sync(0xffffffffu, mbar_wait(bar(b), parity, abort, limit), 0);
-            return ok;
-        };
-        // S_g = Q_g K^T of ring slot ck; `first`: of an item (its Q has to have arrived), `last`: Q is free after it
-        auto qk = [&](int g, int ck, bool first, bool last) {
-            if (first && !wait(Q_FULL + g, nq[g]++ & 1)) return;
-            if (!wait(KV_FULL + ck % kSlots, (ck / kSlots) & 1)) return;
-            fence_after_sync();
-            if (lane == 0) {
-                const uint32_t a = q_lo + g * (kTileBytes >> 4), b = k_lo + (ck % kSlots) * (kTileBytes >> 4);
+        // One elected thread: its own time bounds the kernel (a wait that is over costs it some 150 cycles, 8
+        // products 140), so it waits once per tile for K and V and keeps no more state than the loops need.
+        if (elect_one()) {
+            const uint32_t id_qk = idesc_bf16(kRows, kStep, false, false), id_pv = idesc_bf16(kRows, kDh, false, true);
+            const uint64_t dq = smem_desc(sbase + kSmemQ, 16, 1024);                      // A of QK (K-major)
+            const uint64_t dk = smem_desc(sbase + kSmemKV, 16, 1024);                     // B of QK (K-major)
+            const uint64_t dv = smem_desc(sbase + kSmemKV, kTileBytes / 2, 1024);         // B of PV (MN-major)
+            const uint32_t q_lo = (uint32_t)dq, q_hi = (uint32_t)(dq >> 32), k_lo = (uint32_t)dk, k_hi = (uint32_t)(dk >> 32);
+            const uint32_t v_lo = (uint32_t)dv, v_hi = (uint32_t)(dv >> 32);
+            bool ok = true;
+            auto wait = [&](int b, int parity) {
+                if (ok) ok = mbar_wait(bar(b), parity, abort, limit);
+                return ok;
+            };
+            int nqk0 = 0, nqk1 = 0, npv0 = 0, npv1 = 0, nq0 = 0, nq1 = 0, no0 = 0, no1 = 0, ncut = 0;   // per group; cut tiles
+            // S_g = Q_g K^T of step h of an item, its first tile the CTA's `tile`-th
+            auto qk_group = [&](int g, int h, int H, uint32_t k, int& nqk, int& nq) {
+                if (h == 0 && !wait(Q_FULL + g, nq++ & 1)) return;
+                const int b = nqk++ & 1;
+                const uint32_t a = q_lo + g * (kTileBytes >> 4), d = tmem + kTmemS + g * 128 + b * 64;
+                fence_after_sync();
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk) {
                     const uint32_t o = (kk >> 2) * (kTileBytes >> 5) + (kk & 3) * 2;
-                    mma_ss_split(tmem + kTmemS + g * 128, a + o, q_hi, b + o, k_hi, id_qk, kk > 0 ? 1u : 0u);
+                    mma_ss_split(d, a + o, q_hi, k + o, k_hi, id_qk, kk > 0 ? 1u : 0u);
                 }
-                mma_commit(bar(S_FULL + g));
-                if (last) mma_commit(bar(Q_EMPTY + g));
-            }
-            __syncwarp();
-        };
-        auto free_slot = [&](int c) {
-            if (lane == 0) mma_commit(bar(KV_EMPTY + c % kSlots));
-            __syncwarp();
-        };
-        // the next item that has tiles
-        auto next_item = [&](int i, Item& it) {
-            for (; i < p.items; i += gridDim.x) {
-                it = item_of(p, i);
-                if (it.T) return i;
-            }
-            return i;
-        };
-        Item it{}, nx{};
-        int i = next_item(blockIdx.x, it);
-        if (i < p.items) {
-            if (it.T0) qk(0, 0, true, it.T0 == 1);
-            if (ok && it.T1) qk(1, 0, true, it.T1 == 1);
-            if (ok) free_slot(0);
-        }
-        while (i < p.items && ok) {
-            const int ni = next_item(i + gridDim.x, nx);
-            for (int t = 0; t < it.T && ok; ++t, ++u) {
-                const bool end = t == it.T - 1, more = !end || ni < p.items;
-                const int cv = 2 * u + 1, ck = 2 * u + 2, vs = cv % kSlots;
-                const int valid = it.len - (it.first + t) * kKeys;      // keys of the tile that exist
-                for (int g = 0; g < 2 && ok; ++g) {
-                    const int Tg = g ? it.T1 : it.T0;
-                    if (t < Tg) {
-                        if (!wait(P_FULL + g, np[g]++ & 1)) break;
-                        if (!wait(KV_FULL + vs, (cv / kSlots) & 1)) break;
-                        if (t == 0 && no[g] > 0 && !wait(O_EMPTY + g, (no[g] - 1) & 1)) break;
-                        if (valid < kKeys && (g == 0 || t >= it.T0)) {
-                            // rows of V past the length take no part whatever they hold; the first group to use the tile
-                            // clears them (row r of chunk h: 128 bytes at h 16 KB + r 128; the swizzle stays within a row)
-                            const uint32_t v = sbase + kSmemKV + vs * kTileBytes;
-                            for (int e = lane; e < (kKeys - valid) * 16; e += 32)
-                                asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};\n" ::"r"(
-                                                 v + ((e & 8) ? kTileBytes / 2 : 0) + (valid + (e >> 4)) * 128 + (e & 7) * 16),
-                                             "r"(0)
-                                             : "memory");
-                            fence_proxy_async_smem();
-                            __syncwarp();
-                        }
-                        fence_after_sync();
-                        if (lane == 0) {
-                            const uint32_t a = tmem + kTmemS + g * 128, b = v_lo + vs * (kTileBytes >> 4);
+                mma_commit(bar(S_FULL + 2 * g + b));
+                if (h == H - 1) mma_commit(bar(Q_EMPTY + g));
+            };
+            // O_g += P_g V of step h
+            auto pv_group = [&](int g, int h, int H, uint32_t v, int& npv, int& no) {
+                const int b = npv & 1;
+                if (!wait(P_FULL + 2 * g + b, (npv++ >> 1) & 1)) return;
+                if (h == 0 && no > 0 && !wait(O_EMPTY + g, (no - 1) & 1)) return;
+                const uint32_t a = tmem + kTmemS + g * 128 + b * 64, d = tmem + kTmemO + g * 128;
+                fence_after_sync();
+                mma_ts_split(d, a, v, v_hi, id_pv, h > 0 ? 1u : 0u);
 #pragma unroll
-                            for (int kk = 0; kk < 8; ++kk)          // 16 keys: 8 columns of P, 2 KB of V
-                                mma_ts_split(tmem + kTmemO + g * 128, a + kk * 8, b + kk * 128, v_hi, id_pv,
-                                             (t > 0 || kk > 0) ? 1u : 0u);
-                            if (t == Tg - 1) mma_commit(bar(O_FULL + g));
-                        }
-                        if (t == Tg - 1) ++no[g];
-                        __syncwarp();
-                    }
-                    const int Tn = end ? (ni < p.items ? (g ? nx.T1 : nx.T0) : 0) : Tg;
-                    const int tn = end ? 0 : t + 1;
-                    if (tn < Tn) qk(g, ck, tn == 0, tn == Tn - 1);
+                for (int kk = 1; kk < 4; ++kk)              // 16 keys: 8 columns of P, 2 KB of V
+                    mma_ts_split(d, a + kk * 8, v + kk * 128, v_hi, id_pv, 1u);
+                mma_commit(bar(PV_DONE + 2 * g + b));
+                if (h == H - 1) {
+                    ++no;
+                    mma_commit(bar(O_FULL + g));
                 }
-                if (ok) free_slot(cv);
-                if (ok && more) free_slot(ck);
+            };
+            // both groups' QK of step h; between them what `mid` issues
+            auto qk = [&](const Item& it, int tile, int h, auto mid) {
+                const int c = 2 * (tile + (h >> 1)), slot = c % kSlots;
+                if ((h & 1) == 0) wait(KV_FULL + slot, (c / kSlots) & 1);
+                const uint32_t k = k_lo + slot * (kTileBytes >> 4) + (h & 1) * 512;       // 64 rows of 128 bytes
+                if (ok && h < it.H0) qk_group(0, h, it.H0, k, nqk0, nq0);
+                mid();
+                if (ok && h < it.H1) qk_group(1, h, it.H1, k, nqk1, nq1);
+                if (ok && ((h & 1) || h == it.H - 1)) mma_commit(bar(KV_EMPTY + slot));
+            };
+            auto q_there = [&](const Item& it) {
+                return (it.H0 == 0 || mbar_try_wait(bar(Q_FULL), nq0 & 1)) && (it.H1 == 0 || mbar_try_wait(bar(Q_FULL + 1), nq1 & 1));
+            };
+            // the next item that has steps
+            auto next_item = [&](int i, Item& it) {
+                for (; i < p.items; i += gridDim.x) {
+                    it = item_of(p, i);
+                    if (it.H) break;
+                }
+                return i;
+            };
+            Item it{}, nx{};
+            int i = next_item(blockIdx.x, it), tile = 0, done = 0;      // done: QK steps of `it` issued already
+            while (i < p.items && ok) {
+                const int ni = next_item(i + gridDim.x, nx), ntile = tile + (it.H + 1) / 2;
+                const int nsteps = ni < p.items ? min(nx.H, 2) : 0;
+                int ndone = 0;
+                for (; done < min(it.H, 2) && ok; ++done) qk(it, tile, done, [] {});
+                for (int h = 0; h < it.H && ok; ++h) {
+                    const int c = 2 * (tile + (h >> 1)) + 1, slot = c % kSlots;
+                    if ((h & 1) == 0) {
+                        wait(KV_FULL + slot, (c / kSlots) & 1);
+                        if (cut_tile(s, it, h >> 1)) wait(V_CUT, ncut++ & 1);
+                    }
+                    const uint32_t v = v_lo + slot * (kTileBytes >> 4) + (h & 1) * 512;
+                    auto pv1 = [&] {
+                        if (ok && h < it.H1) pv_group(1, h, it.H1, v, npv1, no1);
+                    };
+                    if (ok && h < it.H0) pv_group(0, h, it.H0, v, npv0, no0);
+                    if (h + 2 < it.H) {
+                        qk(it, tile, h + 2, pv1);
+                    } else if (ndone < nsteps && (ndone > 0 || q_there(nx))) {
+                        // the next item's first steps, once its Q is there
+                        qk(nx, ntile, ndone, pv1);
+                        ++ndone;
+                    } else {
+                        pv1();
+                    }
+                    if (ok && ((h & 1) || h == it.H - 1)) mma_commit(bar(KV_EMPTY + slot));
+                }
+                it = nx;
+                i = ni;
+                tile = ntile;
+                done = ndone;
             }
-            it = nx;
-            i = ni;
-        }
-        if (lane == 0) {
             if (!ok) record_timeout(p, 2);
             // every product issued completes before TMEM is released
             int never = 0;
@@ -310,45 +336,73 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
             mbar_wait(bar(DRAIN), 0, &never, limit);
         }
         __syncwarp();
+    } else if (warp == kCutWarp) {
+        // ------------------------------------------------------------ V past a sequence's length
+        // Those rows take no part whatever they hold: they are cleared in shared memory before the product
+        // reads them (row r of chunk h: 128 bytes at h 16 KB + r 128; the swizzle stays within a row).
+        bool ok = true;
+        int tile = 0;
+        for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
+            const Item it = item_of(p, i);
+            for (int t = 0; t < (it.H + 1) / 2 && ok; ++t, ++tile) {
+                if (!cut_tile(s, it, t)) continue;
+                const int c = 2 * tile + 1, slot = c % kSlots, valid = it.len - (it.first + t) * kKeys;
+                ok = __all_sync(0xffffffffu, mbar_wait(bar(KV_FULL + slot), (c / kSlots) & 1, abort, limit));
+                if (!ok) break;
+                for (int e = lane; e < (kKeys - valid) * 16; e += 32)
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};\n" ::"r"(
+                                     sbase + kSmemKV + slot * kTileBytes + ((e & 8) ? kTileBytes / 2 : 0) +
+                                     (valid + (e >> 4)) * 128 + (e & 7) * 16),
+                                 "r"(0)
+                                 : "memory");
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(V_CUT));
+            }
+        }
+        if (!ok && lane == 0) record_timeout(p, 4);
     } else {
         // ------------------------------------------------------------ softmax + epilogue
         const int g = warp >> 2;
         const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t s_addr = tmem + lane_off + kTmemS + g * 128, o_addr = tmem + lane_off + kTmemO + g * 128;
+        const uint32_t s_base = tmem + lane_off + kTmemS + g * 128, o_addr = tmem + lane_off + kTmemO + g * 128;
         const float c_log2 = s.scale_log2;
         bool ok = true;
-        int n = 0, items = 0;                            // tiles and items of this group
+        int n = 0, items = 0;                            // steps and items of this group
         for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
             const Item it = item_of(p, i);
             if (g == 1 && !it.has1) continue;
             const int r0 = it.r0 + g * kRows, r = r0 + (tid & 127);
-            const int T = g ? it.T1 : it.T0;
+            const int H = g ? it.H1 : it.H0;
             const int seen = r < s.R ? attn_seen(s, it.len, r) : it.len;
-            const int least = T ? attn_seen_least(s, it.len, r0, min(r0 + kRows, s.R) - 1) : 0;
+            const int least = H ? attn_seen_least(s, it.len, r0, min(r0 + kRows, s.R) - 1) : 0;
             float neg_m = 0.0f, l0 = 0.0f, l1 = 0.0f, l2 = 0.0f, l3 = 0.0f;
-            for (int t = 0; t < T; ++t, ++n) {
-                const int key0 = (it.first + t) * kKeys;
-                if (!(ok = mbar_wait(bar(S_FULL + g), n & 1, abort, limit))) break;
+            for (int h = 0; h < H; ++h, ++n) {
+                const int key0 = it.first * kKeys + h * kStep, b = n & 1;
+                const uint32_t s_addr = s_base + b * 64;
+                if (!(ok = mbar_wait(bar(S_FULL + 2 * g + b), (n >> 1) & 1, abort, limit))) break;
                 fence_after_sync();
-                float x[128];
-                row_load128(s_addr, x);
-                if (key0 + kKeys > least) {              // some row of the tile does not see all of its keys
+                float x[64];
+                row_load<64>(s_addr, x);
+                if (key0 + kStep > least) {              // some row of the group does not see all of the step's keys
                     const int m = seen - key0;
 #pragma unroll
-                    for (int j = 0; j < 128; ++j) x[j] = j < m ? x[j] : -INFINITY;
+                    for (int j = 0; j < 64; ++j) x[j] = j < m ? x[j] : -INFINITY;
                 }
                 float mx[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) mx[j] = x[j];
 #pragma unroll
-                for (int j = 8; j < 128; ++j) mx[j & 7] = fmaxf(mx[j & 7], x[j]);
+                for (int j = 8; j < 64; ++j) mx[j & 7] = fmaxf(mx[j & 7], x[j]);
                 const float top = fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
                                         fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7])));
-                const bool need = t == 0 || fmaf(top, c_log2, neg_m) > kRescaleThreshold;
+                const bool need = h == 0 || fmaf(top, c_log2, neg_m) > kRescaleThreshold;
                 if (__any_sync(0xffffffffu, need)) {
                     const float neg_m_new = need ? (top == -INFINITY ? 0.0f : -top * c_log2) : neg_m;
-                    if (t > 0) {
-                        // O holds PV(t - 1): S(t) was issued after it and is complete
+                    if (h > 0) {
+                        // O has to hold PV(n - 1) before it is scaled
+                        if (!(ok = mbar_wait(bar(PV_DONE + 2 * g + (b ^ 1)), ((n - 1) >> 1) & 1, abort, limit))) break;
+                        fence_after_sync();
                         const float alpha = fast_exp2(neg_m_new - neg_m);
 #pragma unroll
                         for (int c = 0; c < 8; ++c) {
@@ -365,11 +419,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
                 }
                 // p = 2^t: row sum in fp32, P packed to bf16 pairs (the lower key in the low half)
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
+                for (int q = 0; q < 2; ++q) {
                     uint32_t pk[16];
 #pragma unroll
                     for (int j = 0; j < 32; j += 4) {
-                        float* y = &x[h * 32 + j];
+                        float* y = &x[q * 32 + j];
                         ffma2(y[0], y[1], c_log2, neg_m);
                         ffma2(y[2], y[3], c_log2, neg_m);
                         const float p0 = fast_exp2(y[0]), p1 = fast_exp2(y[1]);
@@ -379,12 +433,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
                         pk[j >> 1] = pack_bf16(p0, p1);
                         pk[(j >> 1) + 1] = pack_bf16(p2, p3);
                     }
-                    tmem_st16(s_addr + h * 16, *reinterpret_cast<const float(*)[16]>(pk));
+                    tmem_st16(s_addr + q * 16, *reinterpret_cast<const float(*)[16]>(pk));
                 }
                 tmem_st_wait();
                 fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(P_FULL + g));
+                if (lane == 0) mbar_arrive(bar(P_FULL + 2 * g + b));
             }
             if (!ok) break;
             const float l = (l0 + l1) + (l2 + l3);
@@ -396,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
                 if (s.splits > 1) p.part_lse[at] = lse;
                 else if (p.lse) p.lse[at] = lse;
             }
-            if (T) {
+            if (H) {
                 if (!(ok = mbar_wait(bar(O_FULL + g), items & 1, abort, limit))) break;
                 ++items;
                 fence_after_sync();
@@ -404,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
 #pragma unroll
             for (int c = 0; c < 4; ++c) {                // 32 d at a time
                 float ov[32];
-                if (T) {
+                if (H) {
                     tmem_ld16(o_addr + c * 32, *reinterpret_cast<float(*)[16]>(&ov[0]));
                     tmem_ld16(o_addr + c * 32 + 16, *reinterpret_cast<float(*)[16]>(&ov[16]));
                     tmem_ld_wait(*reinterpret_cast<float(*)[16]>(&ov[0]));
@@ -415,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
 #pragma unroll
                     for (int e = 0; e < 32; ++e) ov[e] = 0.0f;
                 }
-                if (c == 3 && T) {
+                if (c == 3 && H) {
                     fence_before_sync();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(O_EMPTY + g));
@@ -424,14 +478,27 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
                 if (s.splits > 1) {
                     float* dst = p.part_o + at * kDh + c * 32;
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<float4*>(dst + e) = make_float4(ov[e], ov[e + 1], ov[e + 2], ov[e + 3]);
-                } else {
-                    uint4* dst = reinterpret_cast<uint4*>(p.o + at * kDh + c * 32);
+                    for (int e = 0; e < 32; e += 8) {
+                        uint32_t y[8];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        dst[e] = make_uint4(pack_bf16(ov[8 * e], ov[8 * e + 1]), pack_bf16(ov[8 * e + 2], ov[8 * e + 3]),
-                                            pack_bf16(ov[8 * e + 4], ov[8 * e + 5]), pack_bf16(ov[8 * e + 6], ov[8 * e + 7]));
+                        for (int j = 0; j < 8; ++j) y[j] = __float_as_uint(ov[e + j]);
+                        st_global32(dst + e, y);
+                    }
+                } else {
+                    // 32 bytes (a whole sector) of the lane's row at a time
+                    __nv_bfloat16* dst = p.o + at * kDh + c * 32;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 16) {
+                        uint32_t y[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) y[j] = pack_bf16(ov[e + 2 * j], ov[e + 2 * j + 1]);
+                        if (p.wide) {
+                            st_global32(dst + e, y);
+                        } else {
+                            *reinterpret_cast<uint4*>(dst + e) = make_uint4(y[0], y[1], y[2], y[3]);
+                            *reinterpret_cast<uint4*>(dst + e + 8) = make_uint4(y[4], y[5], y[6], y[7]);
+                        }
+                    }
                 }
             }
         }
@@ -457,6 +524,7 @@ cudaError_t launch_attention_tc(const AttnShape& s, const AttnArgs& a, cudaStrea
     p.o = static_cast<__nv_bfloat16*>(a.o);
     p.lse = a.lse; p.part_o = a.part_o; p.part_lse = a.part_lse;
     p.status = a.status;
+    p.wide = (reinterpret_cast<uintptr_t>(a.o) & 31u) == 0;
     p.q_tiles = (s.R + 2 * kRows - 1) / (2 * kRows);
     p.items = p.q_tiles * s.heads * s.splits;
     int dev = 0, nsm = 0;

@@ -15,6 +15,14 @@ bool encode_rows(CUtensorMap* m, const void* ptr, int64_t rows, int64_t heads, i
 
 namespace tc {
 
+// True in one lane of the (converged) warp.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+    return p != 0;
+}
+
 // D[tmem] (+)= A[tmem] * B[smem]: A is M rows of K 16-bit values in TMEM,
 // two per 32-bit column (the lower K index in the low half).
 __device__ __forceinline__ void mma_ts_split(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi,
@@ -39,7 +47,13 @@ __device__ __forceinline__ void row_load(uint32_t taddr, float (&v)[NC])
 #pragma unroll
     for (int c = 1; c < NC / 16; ++c) reg_fence(*reinterpret_cast<float(*)[16]>(&v[c * 16]));
 }
-__device__ __forceinline__ void row_load128(uint32_t taddr, float (&v)[128]) { row_load<128>(taddr, v); }
+// 32 bytes at a 32-byte aligned address, one access
+__device__ __forceinline__ void st_global32(void* p, const uint32_t (&y)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n" ::"l"(p), "r"(y[0]), "r"(y[1]), "r"(y[2]),
+                 "r"(y[3]), "r"(y[4]), "r"(y[5]), "r"(y[6]), "r"(y[7])
+                 : "memory");
+}
 
 // (a, b) = (a * m + c, b * m + c), one packed f32x2 instruction (each element an IEEE fma)
 __device__ __forceinline__ void ffma2(float& a, float& b, float m, float c)
