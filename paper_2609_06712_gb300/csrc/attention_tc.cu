@@ -10,9 +10,9 @@
 //   S_g  = Q_g (128 rows x 128 d, smem, K-major)  x  K^T (64 keys x 128 d, smem, K-major)
 //   O_g += P_g (128 rows x 64 keys, TMEM, bf16)   x  V   (64 keys x 128 d, smem, MN-major)
 // TMEM (512 columns): per group two S buffers of 64 columns and O, 128 columns;
-// P overwrites the first half of its S buffer.  One thread issues all products;
-// after PV_g(n) comes QK_g(n + 2) into the same buffer (products of one thread
-// execute in order), so a group's softmax has its next scores ready when it is
+// P overwrites the first half of its S buffer.  One thread issues a group's
+// products: after PV_g(n) comes QK_g(n + 2) into the same buffer (products of one
+// thread execute in order), so a group's softmax has its next scores ready when it is
 // done with the present ones, and the two groups' softmax runs under each other's
 // products.  Steps run on across items, so items follow one another without a gap.
 // With steps of 128 TMEM would hold one S buffer per group, and QK(n + 1) would
@@ -28,9 +28,9 @@
 // Keys past the length: their scores are replaced by -inf whatever they are, and
 // their rows of V are zeroed in shared memory (0 x NaN would be NaN).
 //
-// Warps (352 threads, one persistent CTA per SM): 0-3 softmax and epilogue of
+// Warps (384 threads, one persistent CTA per SM): 0-3 softmax and epilogue of
 // group 0, 4-7 of group 1, 8 TMA (Q of both groups, and K, V tiles in one ring of
-// five 32 KB slots), 9 products, 10 the zeroing of V's rows.  Shared memory 64 + 160 KB.  Every mbarrier wait
+// five 32 KB slots), 9 and 10 products, 11 the zeroing of V's rows.  Shared memory 64 + 160 KB.  Every mbarrier wait
 // is bounded; a wait that gives up records ROLA_ERR_TIMEOUT and the CTA drains
 // what it issued and frees its TMEM.
 #include "attention_tc.cuh"
@@ -41,15 +41,15 @@ namespace {
 using namespace tc;
 
 constexpr int kRows = 128, kKeys = 128, kStep = 64, kSlots = 5;    // rows of a group, keys of a tile and of a step
-constexpr int kTmaWarp = 8, kMmaWarp = 9, kCutWarp = 10, kThreads = 352;
+constexpr int kTmaWarp = 8, kMmaWarp = 9, kCutWarp = 11, kThreads = 384;
 constexpr uint32_t kTileBytes = 128 * 128 * 2;               // [d-chunk][128 rows][64]
 constexpr uint32_t kSmemQ = 0, kSmemKV = 2 * kTileBytes, kSmemTiles = kSmemKV + kSlots * kTileBytes;
 constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemO = 256;   // S_g,b at 128 g + 64 b, O_g at 256 + 128 g
 constexpr float kRescaleThreshold = 8.0f;                    // log2 units
 
-// S_FULL, P_FULL, PV_DONE: 2 g + b
-enum Bar { Q_FULL = 0, Q_EMPTY = 2, S_FULL = 4, P_FULL = 8, PV_DONE = 12, O_FULL = 16, O_EMPTY = 18, KV_FULL = 20,
-           KV_EMPTY = KV_FULL + kSlots, V_CUT = KV_EMPTY + kSlots, DRAIN, NUM_BARS };
+// S_FULL, P_FULL: 2 g + b; the others g, or a slot
+enum Bar { Q_FULL = 0, Q_EMPTY = 2, S_FULL = 4, P_FULL = 8, PV_DONE = 12, O_FULL = 14, O_EMPTY = 16, KV_FULL = 18,
+           KV_EMPTY = KV_FULL + kSlots, V_CUT = KV_EMPTY + kSlots, DRAIN, NUM_BARS = DRAIN + 2 };
 
 struct Ctrl {
     uint64_t bar[NUM_BARS];
@@ -149,17 +149,17 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
             for (int b = 0; b < 2; ++b) {
                 mbar_init(bar(S_FULL + 2 * g + b), 1);
                 mbar_init(bar(P_FULL + 2 * g + b), 4);
-                mbar_init(bar(PV_DONE + 2 * g + b), 1);
             }
+            mbar_init(bar(PV_DONE + g), 1);
+            mbar_init(bar(DRAIN + g), 1);
             mbar_init(bar(O_FULL + g), 1);
             mbar_init(bar(O_EMPTY + g), 4);
         }
         for (int i = 0; i < kSlots; ++i) {
             mbar_init(bar(KV_FULL + i), 1);
-            mbar_init(bar(KV_EMPTY + i), 1);
+            mbar_init(bar(KV_EMPTY + i), 2);      // both groups
         }
         mbar_init(bar(V_CUT), 1);
-        mbar_init(bar(DRAIN), 1);
         fence_mbar_init();
     }
     if (warp == kMmaWarp) {
@@ -226,66 +226,51 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
             for (int u = c > kSlots ? c - kSlots : 0; u < c; ++u)
                 mbar_wait(bar(KV_FULL + u % kSlots), (u / kSlots) & 1, &never, limit);
         }
-    } else if (warp == kMmaWarp) {
-        // ------------------------------------------------------------ products
-        // One elected thread: its own time bounds the kernel (a wait that is over costs it some 150 cycles, 8
-        // products 140), so it waits once per tile for K and V and keeps no more state than the loops need.
+    } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
+        // ------------------------------------------------------------ products of group g
+        // One elected thread per group.  A wait that is over costs it some 150 cycles, 8 products 140, a commit 50
+        // to 150: one thread for both groups took 2000 cycles a step where the tensor core needs 1280.
+        const int g = warp - kMmaWarp;
         if (elect_one()) {
             const uint32_t id_qk = idesc_bf16(kRows, kStep, false, false), id_pv = idesc_bf16(kRows, kDh, false, true);
-            const uint64_t dq = smem_desc(sbase + kSmemQ, 16, 1024);                      // A of QK (K-major)
+            const uint64_t dq = smem_desc(sbase + kSmemQ + g * kTileBytes, 16, 1024);     // A of QK (K-major)
             const uint64_t dk = smem_desc(sbase + kSmemKV, 16, 1024);                     // B of QK (K-major)
             const uint64_t dv = smem_desc(sbase + kSmemKV, kTileBytes / 2, 1024);         // B of PV (MN-major)
             const uint32_t q_lo = (uint32_t)dq, q_hi = (uint32_t)(dq >> 32), k_lo = (uint32_t)dk, k_hi = (uint32_t)(dk >> 32);
             const uint32_t v_lo = (uint32_t)dv, v_hi = (uint32_t)(dv >> 32);
+            const uint32_t t_s = tmem + kTmemS + g * 128, t_o = tmem + kTmemO + g * 128;
             bool ok = true;
             auto wait = [&](int b, int parity) {
                 if (ok) ok = mbar_wait(bar(b), parity, abort, limit);
                 return ok;
             };
-            int nqk0 = 0, nqk1 = 0, npv0 = 0, npv1 = 0, nq0 = 0, nq1 = 0, no0 = 0, no1 = 0, ncut = 0;   // per group; cut tiles
-            // S_g = Q_g K^T of step h of an item, its first tile the CTA's `tile`-th
-            auto qk_group = [&](int g, int h, int H, uint32_t k, int& nqk, int& nq) {
-                if (h == 0 && !wait(Q_FULL + g, nq++ & 1)) return;
-                const int b = nqk++ & 1;
-                const uint32_t a = q_lo + g * (kTileBytes >> 4), d = tmem + kTmemS + g * 128 + b * 64;
-                fence_after_sync();
-#pragma unroll
-                for (int kk = 0; kk < 8; ++kk) {
-                    const uint32_t o = (kk >> 2) * (kTileBytes >> 5) + (kk & 3) * 2;
-                    mma_ss_split(d, a + o, q_hi, k + o, k_hi, id_qk, kk > 0 ? 1u : 0u);
-                }
-                mma_commit(bar(S_FULL + 2 * g + b));
-                if (h == H - 1) mma_commit(bar(Q_EMPTY + g));
+            int nqk = 0, npv = 0, nq = 0, no = 0, ncut = 0;      // steps, Q tiles, items with O, cut tiles
+            // This group is done with the slot of ring use c: after its products, or, where it had none, once the
+            // tile is there (the slot's uses stay in step that way).
+            auto release = [&](int slot, bool used) {
+                if (!ok) return;
+                if (used) mma_commit(bar(KV_EMPTY + slot));
+                else mbar_arrive(bar(KV_EMPTY + slot));
             };
-            // O_g += P_g V of step h
-            auto pv_group = [&](int g, int h, int H, uint32_t v, int& npv, int& no) {
-                const int b = npv & 1;
-                if (!wait(P_FULL + 2 * g + b, (npv++ >> 1) & 1)) return;
-                if (h == 0 && no > 0 && !wait(O_EMPTY + g, (no - 1) & 1)) return;
-                const uint32_t a = tmem + kTmemS + g * 128 + b * 64, d = tmem + kTmemO + g * 128;
-                fence_after_sync();
-                mma_ts_split(d, a, v, v_hi, id_pv, h > 0 ? 1u : 0u);
-#pragma unroll
-                for (int kk = 1; kk < 4; ++kk)              // 16 keys: 8 columns of P, 2 KB of V
-                    mma_ts_split(d, a + kk * 8, v + kk * 128, v_hi, id_pv, 1u);
-                mma_commit(bar(PV_DONE + 2 * g + b));
-                if (h == H - 1) {
-                    ++no;
-                    mma_commit(bar(O_FULL + g));
-                }
-            };
-            // both groups' QK of step h; between them what `mid` issues
-            auto qk = [&](const Item& it, int tile, int h, auto mid) {
+            // S = Q K^T of step h of an item that starts at the CTA's `tile`-th tile; Hg: the group's steps
+            auto qk = [&](const Item& it, int Hg, int tile, int h) {
                 const int c = 2 * (tile + (h >> 1)), slot = c % kSlots;
                 if ((h & 1) == 0) wait(KV_FULL + slot, (c / kSlots) & 1);
-                const uint32_t k = k_lo + slot * (kTileBytes >> 4) + (h & 1) * 512;       // 64 rows of 128 bytes
-                if (ok && h < it.H0) qk_group(0, h, it.H0, k, nqk0, nq0);
-                mid();
-                if (ok && h < it.H1) qk_group(1, h, it.H1, k, nqk1, nq1);
-                if (ok && ((h & 1) || h == it.H - 1)) mma_commit(bar(KV_EMPTY + slot));
-            };
-            auto q_there = [&](const Item& it) {
-                return (it.H0 == 0 || mbar_try_wait(bar(Q_FULL), nq0 & 1)) && (it.H1 == 0 || mbar_try_wait(bar(Q_FULL + 1), nq1 & 1));
+                const bool mine = h < Hg;
+                if (h == 0 && mine) wait(Q_FULL + g, nq++ & 1);
+                if (mine && ok) {
+                    const int b = nqk++ & 1;
+                    const uint32_t k = k_lo + slot * (kTileBytes >> 4) + (h & 1) * 512;       // 64 rows of 128 bytes
+                    fence_after_sync();
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk) {
+                        const uint32_t o = (kk >> 2) * (kTileBytes >> 5) + (kk & 3) * 2;
+                        mma_ss_split(t_s + b * 64, q_lo + o, q_hi, k + o, k_hi, id_qk, kk > 0 ? 1u : 0u);
+                    }
+                    mma_commit(bar(S_FULL + 2 * g + b));
+                    if (h == Hg - 1) mma_commit(bar(Q_EMPTY + g));
+                }
+                if ((h & 1) || h == it.H - 1) release(slot, (h & ~1) < Hg);
             };
             // the next item that has steps
             auto next_item = [&](int i, Item& it) {
@@ -299,30 +284,40 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
             int i = next_item(blockIdx.x, it), tile = 0, done = 0;      // done: QK steps of `it` issued already
             while (i < p.items && ok) {
                 const int ni = next_item(i + gridDim.x, nx), ntile = tile + (it.H + 1) / 2;
+                const int Hg = g ? it.H1 : it.H0, Hn = ni < p.items ? (g ? nx.H1 : nx.H0) : 0;
                 const int nsteps = ni < p.items ? min(nx.H, 2) : 0;
                 int ndone = 0;
-                for (; done < min(it.H, 2) && ok; ++done) qk(it, tile, done, [] {});
+                for (; done < min(it.H, 2) && ok; ++done) qk(it, Hg, tile, done);
                 for (int h = 0; h < it.H && ok; ++h) {
                     const int c = 2 * (tile + (h >> 1)) + 1, slot = c % kSlots;
                     if ((h & 1) == 0) {
                         wait(KV_FULL + slot, (c / kSlots) & 1);
                         if (cut_tile(s, it, h >> 1)) wait(V_CUT, ncut++ & 1);
                     }
-                    const uint32_t v = v_lo + slot * (kTileBytes >> 4) + (h & 1) * 512;
-                    auto pv1 = [&] {
-                        if (ok && h < it.H1) pv_group(1, h, it.H1, v, npv1, no1);
-                    };
-                    if (ok && h < it.H0) pv_group(0, h, it.H0, v, npv0, no0);
-                    if (h + 2 < it.H) {
-                        qk(it, tile, h + 2, pv1);
-                    } else if (ndone < nsteps && (ndone > 0 || q_there(nx))) {
-                        // the next item's first steps, once its Q is there
-                        qk(nx, ntile, ndone, pv1);
-                        ++ndone;
-                    } else {
-                        pv1();
+                    if (h < Hg) {
+                        const int b = npv & 1;
+                        wait(P_FULL + 2 * g + b, (npv++ >> 1) & 1);
+                        if (h == 0 && no > 0) wait(O_EMPTY + g, (no - 1) & 1);
+                        if (!ok) break;
+                        const uint32_t v = v_lo + slot * (kTileBytes >> 4) + (h & 1) * 512;
+                        fence_after_sync();
+                        mma_ts_split(t_o, t_s + b * 64, v, v_hi, id_pv, h > 0 ? 1u : 0u);
+#pragma unroll
+                        for (int kk = 1; kk < 4; ++kk)              // 16 keys: 8 columns of P, 2 KB of V
+                            mma_ts_split(t_o, t_s + b * 64 + kk * 8, v + kk * 128, v_hi, id_pv, 1u);
+                        if (h == Hg - 2) mma_commit(bar(PV_DONE + g));
+                        if (h == Hg - 1) {
+                            ++no;
+                            mma_commit(bar(O_FULL + g));
+                        }
                     }
-                    if (ok && ((h & 1) || h == it.H - 1)) mma_commit(bar(KV_EMPTY + slot));
+                    if ((h & 1) || h == it.H - 1) release(slot, (h & ~1) < Hg);
+                    if (h + 2 < it.H) {
+                        qk(it, Hg, tile, h + 2);
+                    } else if (ndone < nsteps && (ndone > 0 || Hn == 0 || mbar_try_wait(bar(Q_FULL + g), nq & 1))) {
+                        qk(nx, Hn, ntile, ndone);      // the next item's first steps, once its Q is there
+                        ++ndone;
+                    }
                 }
                 it = nx;
                 i = ni;
@@ -332,8 +327,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
             if (!ok) record_timeout(p, 2);
             // every product issued completes before TMEM is released
             int never = 0;
-            mma_commit(bar(DRAIN));
-            mbar_wait(bar(DRAIN), 0, &never, limit);
+            mma_commit(bar(DRAIN + g));
+            mbar_wait(bar(DRAIN + g), 0, &never, limit);
         }
         __syncwarp();
     } else if (warp == kCutWarp) {
@@ -368,7 +363,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
         const uint32_t s_base = tmem + lane_off + kTmemS + g * 128, o_addr = tmem + lane_off + kTmemO + g * 128;
         const float c_log2 = s.scale_log2;
         bool ok = true;
-        int n = 0, items = 0;                            // steps and items of this group
+        int n = 0, items = 0, pairs = 0;                 // steps and items of this group, items of two steps or more
         for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
             const Item it = item_of(p, i);
             if (g == 1 && !it.has1) continue;
@@ -400,8 +395,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
                 if (__any_sync(0xffffffffu, need)) {
                     const float neg_m_new = need ? (top == -INFINITY ? 0.0f : -top * c_log2) : neg_m;
                     if (h > 0) {
-                        // O has to hold PV(n - 1) before it is scaled
-                        if (!(ok = mbar_wait(bar(PV_DONE + 2 * g + (b ^ 1)), ((n - 1) >> 1) & 1, abort, limit))) break;
+                        // O has to hold PV(n - 1) before it is scaled: S(n + 1) was issued after it; on the
+                        // item's last step there may be no S(n + 1) yet, and PV(n - 1) has a barrier of its own
+                        ok = h < H - 1 ? mbar_wait(bar(S_FULL + 2 * g + (b ^ 1)), ((n + 1) >> 1) & 1, abort, limit)
+                                       : mbar_wait(bar(PV_DONE + g), pairs & 1, abort, limit);
+                        if (!ok) break;
                         fence_after_sync();
                         const float alpha = fast_exp2(neg_m_new - neg_m);
 #pragma unroll
@@ -453,6 +451,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
             if (H) {
                 if (!(ok = mbar_wait(bar(O_FULL + g), items & 1, abort, limit))) break;
                 ++items;
+                if (H > 1) ++pairs;
                 fence_after_sync();
             }
 #pragma unroll
@@ -492,12 +491,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
                         uint32_t y[8];
 #pragma unroll
                         for (int j = 0; j < 8; ++j) y[j] = pack_bf16(ov[e + 2 * j], ov[e + 2 * j + 1]);
-                        if (p.wide) {
-                            st_global32(dst + e, y);
-                        } else {
-                            *reinterpret_cast<uint4*>(dst + e) = make_uint4(y[0], y[1], y[2], y[3]);
-                            *reinterpret_cast<uint4*>(dst + e + 8) = make_uint4(y[4], y[5], y[6], y[7]);
-                        }
+                        store_row32(dst + e, y, p.wide);
                     }
                 }
             }

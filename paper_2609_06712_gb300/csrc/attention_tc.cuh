@@ -55,6 +55,17 @@ __device__ __forceinline__ void st_global32(void* p, const uint32_t (&y)[8])
                  : "memory");
 }
 
+// 16 bf16 at a 16-byte aligned address; `wide`: it is 32-byte aligned
+__device__ __forceinline__ void store_row32(__nv_bfloat16* p, const uint32_t (&y)[8], bool wide)
+{
+    if (wide) {
+        st_global32(p, y);
+    } else {
+        *reinterpret_cast<uint4*>(p) = make_uint4(y[0], y[1], y[2], y[3]);
+        *reinterpret_cast<uint4*>(p + 8) = make_uint4(y[4], y[5], y[6], y[7]);
+    }
+}
+
 // (a, b) = (a * m + c, b * m + c), one packed f32x2 instruction (each element an IEEE fma)
 __device__ __forceinline__ void ffma2(float& a, float& b, float m, float c)
 {
