@@ -49,7 +49,7 @@ constexpr float kRescaleThreshold = 8.0f;                    // log2 units
 
 // S_FULL, P_FULL: 2 g + b; the others g, or a slot
 enum Bar { Q_FULL = 0, Q_EMPTY = 2, S_FULL = 4, P_FULL = 8, PV_DONE = 12, O_FULL = 14, O_EMPTY = 16, KV_FULL = 18,
-           KV_EMPTY = KV_FULL + kSlots, V_CUT = KV_EMPTY + kSlots, DRAIN, NUM_BARS = DRAIN + 2 };
+           KV_EMPTY = KV_FULL + kSlots, V_CUT = KV_EMPTY + kSlots, DRAIN = V_CUT + 4, NUM_BARS = DRAIN + 2 };
 
 struct Ctrl {
     uint64_t bar[NUM_BARS];
@@ -157,9 +157,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
         }
         for (int i = 0; i < kSlots; ++i) {
             mbar_init(bar(KV_FULL + i), 1);
-            mbar_init(bar(KV_EMPTY + i), 2);      // both groups
+            mbar_init(bar(KV_EMPTY + i), p.kv_len ? 3 : 2);      // both groups, and the zeroing warp
         }
-        mbar_init(bar(V_CUT), 1);
+        for (int i = 0; i < 4; ++i) mbar_init(bar(V_CUT + i), 1);
         fence_mbar_init();
     }
     if (warp == kMmaWarp) {
@@ -292,7 +292,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
                     const int c = 2 * (tile + (h >> 1)) + 1, slot = c % kSlots;
                     if ((h & 1) == 0) {
                         wait(KV_FULL + slot, (c / kSlots) & 1);
-                        if (cut_tile(s, it, h >> 1)) wait(V_CUT, ncut++ & 1);
+                        if (cut_tile(s, it, h >> 1)) {
+                            wait(V_CUT + (ncut & 3), (ncut >> 2) & 1);
+                            ++ncut;
+                        }
                     }
                     if (h < Hg) {
                         const int b = npv & 1;
@@ -334,25 +337,40 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
     } else if (warp == kCutWarp) {
         // ------------------------------------------------------------ V past a sequence's length
         // Those rows take no part whatever they hold: they are cleared in shared memory before the product
-        // reads them (row r of chunk h: 128 bytes at h 16 KB + r 128; the swizzle stays within a row).
+        // reads them (row r of chunk h: 128 bytes at h 16 KB + r 128; the swizzle stays within a row).  The warp
+        // follows every tile, so that it knows each slot's turn; V_CUT has four barriers because a group may be up to
+        // two V tiles of the ring behind it.
         bool ok = true;
-        int tile = 0;
-        for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
+        int c = 0, ncut = 0;
+        auto next = [&]() {
+            ok = __all_sync(0xffffffffu, mbar_wait(bar(KV_FULL + c % kSlots), (c / kSlots) & 1, abort, limit));
+            return ok;
+        };
+        auto done = [&]() {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(KV_EMPTY + c % kSlots));
+            ++c;
+        };
+        for (int i = blockIdx.x; i < p.items && ok && p.kv_len; i += gridDim.x) {
             const Item it = item_of(p, i);
-            for (int t = 0; t < (it.H + 1) / 2 && ok; ++t, ++tile) {
-                if (!cut_tile(s, it, t)) continue;
-                const int c = 2 * tile + 1, slot = c % kSlots, valid = it.len - (it.first + t) * kKeys;
-                ok = __all_sync(0xffffffffu, mbar_wait(bar(KV_FULL + slot), (c / kSlots) & 1, abort, limit));
-                if (!ok) break;
-                for (int e = lane; e < (kKeys - valid) * 16; e += 32)
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};\n" ::"r"(
-                                     sbase + kSmemKV + slot * kTileBytes + ((e & 8) ? kTileBytes / 2 : 0) +
-                                     (valid + (e >> 4)) * 128 + (e & 7) * 16),
-                                 "r"(0)
-                                 : "memory");
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(V_CUT));
+            for (int t = 0; t < (it.H + 1) / 2; ++t) {
+                if (!next()) break;                      // K
+                done();
+                if (!next()) break;                      // V
+                if (cut_tile(s, it, t)) {
+                    const int slot = c % kSlots, valid = it.len - (it.first + t) * kKeys;
+                    for (int e = lane; e < (kKeys - valid) * 16; e += 32)
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};\n" ::"r"(
+                                         sbase + kSmemKV + slot * kTileBytes + ((e & 8) ? kTileBytes / 2 : 0) +
+                                         (valid + (e >> 4)) * 128 + (e & 7) * 16),
+                                     "r"(0)
+                                     : "memory");
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(V_CUT + (ncut & 3)));
+                    ++ncut;
+                }
+                done();
             }
         }
         if (!ok && lane == 0) record_timeout(p, 4);

@@ -99,7 +99,7 @@ rola_status_t ffn_forward(const rola_ffn_config_t* cfg, const void* X, const voi
     const FfnShape s = make_shape(*cfg);
     void* H = at<void>(ws, w.H);
     ROLA_TRY(cudaMemsetAsync(at<uint8_t>(ws, w.status), 0, sizeof(DeviceStatus), st));
-    if (cfg->dtype == ROLA_BF16 && s.M <= kFfnFewTokens) {
+    if (cfg->dtype == ROLA_BF16 && ffn_few(s)) {
         ROLA_TRY(launch_ffn_few(s, X, Wg, Wu, Wd, H, G, U, Y, at<DeviceStatus>(ws, w.status), st));
     } else if (cfg->dtype == ROLA_BF16) {
         ROLA_TRY(launch_ffn_up_tc(s, X, Wg, Wu, H, G, U, at<DeviceStatus>(ws, w.status), st));
@@ -132,17 +132,23 @@ rola_status_t validate(const rola_attention_config_t* c)
     return ROLA_OK;
 }
 
-// Parts of the key axis.  With fewer (head, row tile) items than SMs the key
-// axis is split so that all SMs read keys, but no part has fewer than two
-// tiles of keys: below that a part's fixed costs (its Q, its epilogue, its
-// share of the join) outweigh its keys.
-int attn_splits(int64_t items, int64_t key_tiles)
+// Parts of an axis of `tiles` tiles, for `items` items without splitting.  One
+// CTA runs on each of 152 SMs, so `items` items in n parts take
+// ceil(items n / 152) turns of tiles / n steps; with parts, their `bytes` (of fp32
+// output, each) are written and read once more at some 5 TB/s, and the second
+// kernel costs 4 us.  step_us: a step's measured time.  The n of least cost is
+// taken, among those whose parts keep two tiles at least.
+int attn_splits(int64_t items, int64_t tiles, double step_us, double bytes)
 {
     constexpr int64_t kSMs = 152;
-    if (items >= kSMs) return 1;
-    int64_t n = kSMs / items;
-    if (n > key_tiles / 2) n = key_tiles / 2;
-    return n > 1 ? (int)n : 1;
+    auto cost = [&](int64_t n) {
+        const double turns = (double)((items * n + kSMs - 1) / kSMs);
+        return turns * (double)tiles / (double)n * step_us + (n > 1 ? (double)n * 2.0 * bytes / 5e6 + 4.0 : 0.0);
+    };
+    int64_t best = 1;
+    for (int64_t n = 2; n <= tiles / 2 && n <= kSMs; ++n)
+        if (cost(n) < cost(best)) best = n;
+    return (int)best;
 }
 
 AttnShape make_shape(const rola_attention_config_t& c)
@@ -155,15 +161,24 @@ AttnShape make_shape(const rola_attention_config_t& c)
     const double scale = c.scale > 0.0f ? (double)c.scale : 1.0 / sqrt((double)kDh);
     s.scale = (float)scale;
     s.scale_log2 = (float)(scale * 1.4426950408889634);
-    const int rows = c.dtype == ROLA_BF16 ? 256 : 64, keys = c.dtype == ROLA_BF16 ? 128 : 64;   // of an item, of a tile
-    s.splits = attn_splits((int64_t)s.heads * ((s.R + rows - 1) / rows), (s.Lk + keys - 1) / keys);
+    auto tiles = [](int64_t n, int of) { return (n + of - 1) / of; };
+    const double rows = 4.0 * kDh * s.heads * s.R, keys = 4.0 * kDh * s.heads * s.Lk;
+    const double part = s.causal ? 0.5 : 1.0;    // of the tiles that a row sees
+    if (c.dtype == ROLA_BF16) {          // items of 256 rows forward, of 128 rows or keys backward; tiles of 128
+        s.splits = attn_splits(s.heads * tiles(s.R, 256), tiles(s.Lk, 128), 1.7 * part, rows);
+        s.splits_dq = attn_splits(s.heads * tiles(s.R, 128), tiles(s.Lk, 128), 1.0 * part, rows);
+        s.splits_dkv = attn_splits(s.heads * tiles(s.Lk, 128), tiles(s.R, 128), 1.3 * part, 2.0 * keys);
+    } else {
+        s.splits = attn_splits(s.heads * tiles(s.R, 64), tiles(s.Lk, 64), 8.0 * part, rows);
+        s.splits_dq = s.splits_dkv = 1;
+    }
     s.wait_limit_ns = wait_limit_ns(c.wait_limit_ms);
     s.debug_flags = c.debug_flags;
     return s;
 }
 
 struct AttnWorkspace {
-    size_t status, part_o, part_lse, D, total;
+    size_t status, part_o, part_lse, D, part_dq, part_dk, part_dv, total;
 };
 AttnWorkspace attn_layout(const AttnShape& s, bool backward)
 {
@@ -174,6 +189,11 @@ AttnWorkspace attn_layout(const AttnShape& s, bool backward)
     w.part_o = off; off = align_up(off + 4 * parts * rows * kDh);
     w.part_lse = off; off = align_up(off + 4 * parts * rows);
     w.D = off; off = align_up(off + (backward ? 4 * rows : 0));
+    const size_t dq = backward && s.splits_dq > 1 ? 4 * s.splits_dq * rows * kDh : 0;
+    const size_t dkv = backward && s.splits_dkv > 1 ? 4 * (size_t)s.splits_dkv * s.heads * s.Lk * kDh : 0;
+    w.part_dq = off; off = align_up(off + dq);
+    w.part_dk = off; off = align_up(off + dkv);
+    w.part_dv = off; off = align_up(off + dkv);
     w.total = off;
     return w;
 }
@@ -325,10 +345,12 @@ rola_status_t rola_attention_backward(const rola_attention_config_t* cfg, const 
     a.q = q; a.k = k; a.v = v; a.kv_len = kv_len; a.o_in = o; a.lse_in = lse; a.dO = dO;
     a.dq = dq; a.dk = dk; a.dv = dv;
     a.D = at<float>(ws, w.D);
+    a.part_dq = at<float>(ws, w.part_dq); a.part_dk = at<float>(ws, w.part_dk); a.part_dv = at<float>(ws, w.part_dv);
     a.status = at<DeviceStatus>(ws, w.status);
     ROLA_TRY(cudaMemsetAsync(a.status, 0, sizeof(DeviceStatus), st));
     if (cfg->dtype == ROLA_BF16) {
-        ROLA_TRY(launch_attention_rowdot<__nv_bfloat16>(s, a, st));
+        // over one stage of keys the dq kernel forms D itself
+        if (s.Lk > 128) ROLA_TRY(launch_attention_rowdot<__nv_bfloat16>(s, a, st));
         ROLA_TRY(launch_attention_backward_tc(s, a, st));
     } else {
         ROLA_TRY(launch_attention_rowdot<float>(s, a, st));

@@ -93,6 +93,36 @@ __device__ __forceinline__ void gate_act_grad(int kind, float g, float& a, float
     }
 }
 
+// The same for results that are rounded to bf16 (the fast exponential and
+// quotient are within some 2^-19 of silu's value), one type per map, so that the choice is
+// made once for a whole loop and not once per element.
+struct FastSilu {
+    static __device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
+    static __device__ __forceinline__ float phi(float g) { return g * sigmoid(g); }
+    static __device__ __forceinline__ void grad(float g, float& a, float& da)
+    {
+        const float s = sigmoid(g);
+        a = g * s;
+        da = fmaf(a, 1.0f - s, s);
+    }
+};
+template <int KIND>
+struct PlainAct {
+    static __device__ __forceinline__ float phi(float g) { return gate_act(KIND, g); }
+    static __device__ __forceinline__ void grad(float g, float& a, float& da) { gate_act_grad(KIND, g, a, da); }
+};
+template <typename F>
+__device__ __forceinline__ void with_act(int kind, F f)
+{
+    switch (kind) {
+        case ROLA_LOWRANK_ACT_SILU: f(FastSilu()); break;
+        case ROLA_LOWRANK_ACT_IDENTITY: f(PlainAct<ROLA_LOWRANK_ACT_IDENTITY>()); break;
+        case ROLA_LOWRANK_ACT_TANH: f(PlainAct<ROLA_LOWRANK_ACT_TANH>()); break;
+        case ROLA_LOWRANK_ACT_RELU: f(PlainAct<ROLA_LOWRANK_ACT_RELU>()); break;
+        default: f(PlainAct<ROLA_LOWRANK_ACT_GELU>()); break;
+    }
+}
+
 // ---------------------------------------------------------------- feed-forward
 
 struct FfnShape {
@@ -110,7 +140,8 @@ struct AttnShape {
     int heads;                   // B Hk
     int causal;
     float scale, scale_log2;     // of the scores, and times log2 e
-    int splits;                  // parts of the key axis (1: none)
+    int splits;                  // parts of the key axis forward (1: none)
+    int splits_dq, splits_dkv;   // bf16 backward: of the key axis for dq, of the row axis for dk and dv
     uint64_t wait_limit_ns;
     int debug_flags;
 };
@@ -146,6 +177,7 @@ struct AttnArgs {
     const int32_t* kv_len;
     void *o, *dq, *dk, *dv;
     float *lse, *part_o, *part_lse;
+    float *part_dq, *part_dk, *part_dv;      // backward with splits: [splits][heads][rows or keys][128]
     const float* lse_in;
     float* D;                    // rowsum(dO o), [heads R]
     DeviceStatus* status;
@@ -170,7 +202,8 @@ cudaError_t launch_ffn_down_simt(const FfnShape& s, const void* H, const void* W
 cudaError_t launch_ffn_down_tc(const FfnShape& s, const void* H, const void* Wd, void* Y, DeviceStatus* status,
                                cudaStream_t st);
 // Few tokens: both products of the forward (and G, U where given); H, dG, dU and dX of the backward.
-constexpr int kFfnFewTokens = 96;    // their sums of two accumulators fit a CTA's shared memory
+constexpr int kFfnFewTokens = 96;    // of one tile; the backward's form up to there
+bool ffn_few(const FfnShape& s);     // whether it is the forward's form for these sizes
 cudaError_t launch_ffn_few(const FfnShape& s, const void* X, const void* Wg, const void* Wu, const void* Wd, void* H,
                            float* G, float* U, void* Y, DeviceStatus* status, cudaStream_t st);
 cudaError_t launch_ffn_few_grad(const FfnShape& s, const void* Wg, const void* Wu, const void* Wd, const float* G,

@@ -1,7 +1,8 @@
 // The gated feed-forward's products for few tokens (bf16 operands, tcgen05):
 // every weight is read once for all of them, and that is what bounds the work
 // (one token at widths 5120 x 13824: 425 MB of weights, 63 us at the measured
-// 6.8 TB/s; its 0.4 GFLOP are nothing).
+// 6.8 TB/s; its 0.4 GFLOP are nothing).  More than 96 tokens go in tiles of at most
+// 96 side by side, which read the weights from L2.
 //
 // The tokens are the N axis and 128 weight rows the M axis of the tensor core,
 // so that a single token costs a tile of 16 columns instead of 128 rows:
@@ -39,6 +40,7 @@ constexpr int kTileM = 128, kStepK = 64, kThreads = 192, kMaxStages = 8;
 constexpr uint32_t kABytes = kTileM * kStepK * 2;
 constexpr uint32_t kSmemBudget = 112 * 1024;                 // two CTAs of an SM's 227 KB
 constexpr int kMaxCluster = 8;
+constexpr int kMaxTokens = kFfnFewTokens;                    // of a tile: its two sums fit the 112 KB
 
 enum Bar { FULL = 0, EMPTY = FULL + kMaxStages, ACC_FULL = EMPTY + kMaxStages, DRAIN, NUM_BARS };
 struct Ctrl {
@@ -50,7 +52,7 @@ struct Ctrl {
 struct Params {
     CUtensorMap a[2], b[2];          // weights (kUp: gate and up; kDX: the two sources), tokens
     int M, rows;                     // tokens; weight rows of the output (d_ff or d_model)
-    int nt;                          // tokens rounded up to a multiple of 16: the N of the products
+    int nt;                          // tokens of a tile, a multiple of 16: the N of the products
     int k_steps, sources;            // K steps of 64 of one source
     int stages, act, skip_first;
     uint32_t stage_bytes, tiles_bytes;   // of a stage; of the tiles in front of the control block
@@ -126,6 +128,7 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_few_kernel(const __grid_const
     volatile int* abort = &cb.abort;
     const uint64_t limit = p.wait_limit_ns;
     const int s = (int)cluster_size(), rank = (int)cluster_rank();
+    const int first_token = blockIdx.y * p.nt, tokens = min(p.M - first_token, p.nt);
     const int tile = blockIdx.x / s, total = p.k_steps * p.sources;
     const int k_begin = (int)((long long)total * rank / s), k_end = (int)((long long)total * (rank + 1) / s);
     const int steps = k_end - k_begin;
@@ -154,7 +157,8 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_few_kernel(const __grid_const
             int src, k0;
             coords(i, src, k0);
             if (lane == 2)
-                tma_load_2d(sbase + (i % p.stages) * p.stage_bytes + b_off, &p.b[src], bar(FULL + i % p.stages), k0, 0);
+                tma_load_2d(sbase + (i % p.stages) * p.stage_bytes + b_off, &p.b[src], bar(FULL + i % p.stages), k0,
+                            first_token);
         };
         // test hook: the first stage is never announced nor loaded, so the waits on it run out
         const int first = p.skip_first && steps > 0 ? 1 : 0, ahead = min(p.stages, steps);
@@ -237,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_few_kernel(const __grid_const
     if (warp == 1) tmem_dealloc(tmem, 128 * ACCS);
     if (warp >= 2) {
         const int row = (warp & 3) * 32 + lane, f = tile * kTileM + row;
-        const int m0 = p.M * rank / s, m1 = p.M * (rank + 1) / s;
+        const int m0 = tokens * rank / s, m1 = tokens * (rank + 1) / s;
         uint32_t from[kMaxCluster];
 #pragma unroll
         for (int r = 0; r < kMaxCluster; ++r) from[r] = r < s ? peer(sbase + (uint32_t)row * 4, r) : 0;
@@ -256,11 +260,13 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_few_kernel(const __grid_const
                 return x;
             };
             const float x = sum(0);
-            const size_t at = (size_t)m * p.rows + f;
+            const size_t at = (size_t)(first_token + m) * p.rows + f;
             if constexpr (MODE == kUp) {
                 const float u = sum(1);
                 if (f < p.rows) {
-                    p.c0[at] = __float2bfloat16_rn(gate_act(p.act, x) * u);
+                    float a = 0.0f;
+                    with_act(p.act, [&](auto act) { a = act.phi(x); });
+                    p.c0[at] = __float2bfloat16_rn(a * u);
                     if (p.G) {
                         p.G[at] = x;
                         p.U[at] = u;
@@ -268,8 +274,8 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_few_kernel(const __grid_const
                 }
             } else if (f < p.rows) {
                 if constexpr (MODE == kGrad) {
-                    float a, da;
-                    gate_act_grad(p.act, p.G[at], a, da);
+                    float a = 0.0f, da = 0.0f;
+                    with_act(p.act, [&](auto act) { act.grad(p.G[at], a, da); });
                     const float u = p.U[at];
                     p.c0[at] = __float2bfloat16_rn(a * u);
                     p.c1[at] = __float2bfloat16_rn(x * u * da);
@@ -301,7 +307,8 @@ cudaError_t launch(const FfnShape& s, Params& p, bool dependent, DeviceStatus* s
     p.skip_first = s.debug_flags & ROLA_DEBUG_SKIP_FIRST_K_COPY ? 1 : 0;
     const int tiles = (p.rows + kTileM - 1) / kTileM, total = p.k_steps * p.sources;
     // as many CTAs as two per SM hold, each with two K steps at least
-    int cluster = 304 / tiles;
+    const int token_tiles = (s.M + p.nt - 1) / p.nt;
+    int cluster = 304 / (tiles * token_tiles);
     if (cluster > total / 2) cluster = total / 2;
     if (cluster > kMaxCluster) cluster = kMaxCluster;
     if (cluster < 1) cluster = 1;
@@ -317,7 +324,7 @@ cudaError_t launch(const FfnShape& s, Params& p, bool dependent, DeviceStatus* s
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(tiles * cluster);
+    cfg.gridDim = dim3(tiles * cluster, token_tiles);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
@@ -337,11 +344,20 @@ int steps(int k) { return (k + kStepK - 1) / kStepK; }
 Params params(const FfnShape& s)
 {
     Params p{};
-    p.nt = (s.M + 15) / 16 * 16;
+    const int tiles = (s.M + kMaxTokens - 1) / kMaxTokens;
+    p.nt = ((s.M + tiles - 1) / tiles + 15) / 16 * 16;
     return p;
 }
 
 }  // namespace
+
+// Up to 96 tokens, and beyond while the down product's tiles of 128 x 256 would leave half of the 152 SMs idle
+// (130 tokens at widths 5120 x 13824: 134 us against 172 in such tiles).  The backward's products read their
+// weights MN-major and gain nothing from tokens side by side (dX of 300 tokens at 1536 x 4096: 71 us against 46).
+bool ffn_few(const FfnShape& s)
+{
+    return s.M <= kMaxTokens || (int64_t)((s.M + 127) / 128) * ((s.D + 255) / 256) < 76;
+}
 
 cudaError_t launch_ffn_few(const FfnShape& s, const void* X, const void* Wg, const void* Wu, const void* Wd, void* H,
                            float* G, float* U, void* Y, DeviceStatus* status, cudaStream_t st)

@@ -5,40 +5,44 @@
 //   dG, dU, H from dH = dY Wd;  dX = dG Wg + dU Wu;  dWg = dG^T X,  dWu = dU^T X,  dWd = dY^T H
 //
 // One persistent warp-specialised kernel computes C(m, n) = sum_k A(m, k) B(n, k)
-// in tiles of 128 x NT, one CTA per SM.  Per K step of 64, A (16 KB) and B
-// (128 NT bytes) arrive by TMA in 128-byte-swizzled shared memory, four stages
-// deep, and four tcgen05.mma M = 128, N = NT, K = 16 accumulate in TMEM.  The
+// in tiles of 128 x 256, one CTA per SM.  Per K step of 64, A (16 KB) and B
+// (32 KB) arrive by TMA in 128-byte-swizzled shared memory, four stages deep,
+// and four tcgen05.mma M = 128, N = 256, K = 16 accumulate in TMEM.  The
 // accumulator is double-buffered, so a tile's epilogue runs under the next
 // tile's products.  An operand is contiguous along k (K-major, one box of 64 k)
 // or along m / n (MN-major, boxes of 64 x 64 k); the tensor core reads either,
 // so no operand is transposed in memory.  Ragged edges are TMA zero fill on
-// loads (a zero adds nothing to the sum) and TMA clipping on stores.
+// loads (a zero adds nothing to the sum).
 //
 // Forms (Epilogue):
-//   kStore     NT = 256: C rounded to bf16.  Y, the weights' gradients (three
+//   kStore     C rounded to bf16.  Y, the weights' gradients (three
 //              products in one launch: 192 tiles each at widths 1536 x 4096
 //              would be 1.3 waves of 152 SMs, 576 together are 3.8), and dX,
 //              whose K axis is d_ff twice (dG Wg, then dU Wu, in one accumulator).
-//   kGateUp    NT = 256 = 128 rows of Wg and the same 128 rows of Wu: a thread
+//   kGateUp    B = 128 rows of Wg and the same 128 rows of Wu: a thread
 //              holds g and u of its row's features, so phi and the product
 //              need no exchange.  H is stored once, G and U when training.
-//   kGateGrad  NT = 128: dH stays in TMEM; G and U arrive by TMA in the
-//              epilogue, dG, dU and H leave by TMA.  The narrower tile leaves
-//              room for that traffic beside the four stages.
+//   kGateGrad  dH stays in TMEM; G and U arrive by TMA beside it, a piece of 32
+//              rows x 16 columns ahead of each epilogue warp.  (Tiles of 128 x 128 leave
+//              room for larger pieces, but four stages of theirs cover 1000 cycles of
+//              loads instead of 2000: 149 us against 121 at 8190 tokens x 1536 x 4096.)
 //
 // Tiles are taken in groups of kGroupM row tiles, column tiles outside, row
 // tiles inside: the CTAs in flight share a few column tiles of B and the
 // group's rows of A, which stay in L2 (129 MB), and B is read once per group.
 //
-// Warp roles (192 threads): warp 0 TMA producer, warp 1 MMA issuer and TMEM
-// owner, warps 2-5 epilogue (warp w reads TMEM lanes 32 (w mod 4) .. +31, its
-// 32 rows).  Every mbarrier wait is bounded; a wait that gives up records
-// ROLA_ERR_TIMEOUT in the status word, and the CTA stops issuing, lets what it
-// issued complete and frees its TMEM.
+// Epilogue: eight warps, two for each quarter of the TMEM lanes (32 rows), half
+// of the columns each, 32 columns at a time; a lane stores whole 32-byte sectors of its
+// row.  (Four warps that staged each piece in shared memory for TMA stores took
+// 371 us for dH at 8190 tokens x 1536 x 4096 where the products need 55.)
+//
+// Warp roles (320 threads): warp 0 TMA producer, warp 1 MMA issuer and TMEM
+// owner, warps 2-9 epilogue.  Every mbarrier wait is bounded; a wait that gives
+// up records ROLA_ERR_TIMEOUT in the status word, and the CTA stops issuing, lets
+// what it issued complete and frees its TMEM.
 #include <cudaTypedefs.h>
 
-#include "block_ops.cuh"
-#include "tcgen05.cuh"
+#include "attention_tc.cuh"
 #include "tma_2d.cuh"
 
 namespace rola {
@@ -48,23 +52,20 @@ using namespace tc;
 
 enum Epilogue { kStore, kGateUp, kGateGrad };
 
-constexpr int kTileM = 128, kStepK = 64, kStages = 4, kGroupM = 16;
+constexpr int kTileM = 128, kStepK = 64, kGroupM = 16;
 constexpr uint32_t kABytes = kTileM * kStepK * 2;
-constexpr int kThreads = 192, kEpiWarps = 4;
-constexpr uint32_t kStoreBytes = 4096;                       // 32 rows of 128 bytes
+constexpr int kThreads = 320, kEpiWarps = 8;
+constexpr int NT = 256, kStages = 4;
+constexpr uint32_t kBBytes = NT * kStepK * 2, kStageBytes = kABytes + kBBytes;
+constexpr uint32_t kPieceBytes = 2048;                       // 32 rows x 16 columns, fp32
 
 template <int E>
 struct Cfg {
-    static constexpr int NT = E == kGateGrad ? 128 : 256;
-    static constexpr uint32_t kBBytes = NT * kStepK * 2;
-    static constexpr uint32_t kStageBytes = kABytes + kBBytes;
     static constexpr uint32_t kSmemEpi = kStages * kStageBytes;
-    // an epilogue warp's shared memory: two store buffers; or two slots of G and U, and H, dG, dU
-    // (32 features in bf16: 2 KB each)
-    static constexpr uint32_t kEpiBytes = E == kGateGrad ? 4 * kStoreBytes + 3 * 2048 : 2 * kStoreBytes;
+    static constexpr uint32_t kEpiBytes = E == kGateGrad ? 2 * kPieceBytes : 0;      // a warp's piece of G and of U
     static constexpr uint32_t kSmemTiles = kSmemEpi + kEpiWarps * kEpiBytes;
     static constexpr int FULL = 0, EMPTY = FULL + kStages, ACC_FULL = EMPTY + kStages, ACC_EMPTY = ACC_FULL + 2,
-                         DRAIN = ACC_EMPTY + 2, GU_FULL = DRAIN + 1, NUM_BARS = GU_FULL + 2 * kEpiWarps;
+                         DRAIN = ACC_EMPTY + 2, GU_FULL = DRAIN + 1, NUM_BARS = GU_FULL + kEpiWarps;
 };
 
 template <int E>
@@ -78,10 +79,12 @@ static_assert(Cfg<kStore>::kSmemTiles + sizeof(Ctrl<kStore>) <= 232448 &&
               "tiles and control block fit the 227 KB a CTA may have");
 
 // One product.  b[1] of kGateUp is W_up; a[1], b[1] with sources = 2 are the second product of the sum.
-// c: C, or H; c[1], c[2]: G and U (kGateUp, fp32) or dG and dU (kGateGrad); in: G and U of kGateGrad.
+// c: C, or H; for kGateGrad dG and dU too.  Every output row is a multiple of 16 bytes long.
 struct Problem {
-    CUtensorMap a[2], b[2], c[3];
+    CUtensorMap a[2], b[2];
+    __nv_bfloat16* c[3];
     int M, N;
+    int wide;                        // the outputs' rows are 32-byte aligned
     int m_tiles, n_tiles, tile0;     // tiles [tile0, tile0 + m_tiles n_tiles) of the launch are this product's
     int k_steps, sources;            // K steps of 64 of one source
 };
@@ -89,8 +92,9 @@ struct Problem {
 template <int E>
 struct Params {
     Problem pr[E == kStore ? 3 : 1];
-    CUtensorMap in[E == kGateGrad ? 2 : 1];
-    int problems, tiles, act, keep;  // keep: kGateUp writes G and U
+    CUtensorMap in[E == kGateGrad ? 2 : 1];      // kGateGrad: G and U
+    float *G, *U;                    // kGateUp: out, or NULL
+    int problems, tiles, act;
     int skip_first;                  // test hook: a CTA's first load is never issued
     DeviceStatus* status;
     uint64_t wait_limit_ns;
@@ -119,46 +123,44 @@ __device__ __forceinline__ const Problem& tile_of(const Params<E>& p, int t, int
     return r;
 }
 
-// 32 bf16 of this lane's row into a 32 x 32 tile of 64-byte rows (64-byte swizzle)
-__device__ __forceinline__ void stage_row32(uint32_t buf, int lane, const float (&v)[32])
+// W values of a row from column f0 of N (a multiple of 8) on: in bf16, and in fp32
+template <int W>
+__device__ __forceinline__ void store_row(__nv_bfloat16* row, int f0, int N, const float (&v)[W], bool wide)
 {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        const uint32_t w0 = pack_bf16(v[8 * c], v[8 * c + 1]), w1 = pack_bf16(v[8 * c + 2], v[8 * c + 3]);
-        const uint32_t w2 = pack_bf16(v[8 * c + 4], v[8 * c + 5]), w3 = pack_bf16(v[8 * c + 6], v[8 * c + 7]);
-        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};\n" ::"r"(buf + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)),
-                     "r"(w0), "r"(w1), "r"(w2), "r"(w3)
-                     : "memory");
+    for (int e = 0; e < W; e += 16) {
+        uint32_t y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = pack_bf16(v[e + 2 * j], v[e + 2 * j + 1]);
+        if (f0 + e + 16 <= N) store_row32(row + f0 + e, y, wide);
+        else if (f0 + e < N) *reinterpret_cast<uint4*>(row + f0 + e) = make_uint4(y[0], y[1], y[2], y[3]);
     }
 }
-// the same 32 columns starting at 16-byte chunk c0 of a row of 128 bytes (128-byte swizzle)
-__device__ __forceinline__ void stage_half_row64(uint32_t buf, int lane, int c0, const float (&v)[32])
+template <int W>
+__device__ __forceinline__ void store_row(float* row, int f0, int N, const float (&v)[W], bool wide)
 {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        const uint32_t w0 = pack_bf16(v[8 * c], v[8 * c + 1]), w1 = pack_bf16(v[8 * c + 2], v[8 * c + 3]);
-        const uint32_t w2 = pack_bf16(v[8 * c + 4], v[8 * c + 5]), w3 = pack_bf16(v[8 * c + 6], v[8 * c + 7]);
-        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};\n" ::"r"(buf + lane * 128 + (((c0 + c) ^ (lane & 7)) << 4)),
-                     "r"(w0), "r"(w1), "r"(w2), "r"(w3)
-                     : "memory");
+    for (int e = 0; e < W; e += 8) {
+        if (f0 + e >= N) break;
+        uint32_t y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = __float_as_uint(v[e + j]);
+        if (wide) {
+            st_global32(row + f0 + e, y);
+        } else {
+            *reinterpret_cast<uint4*>(row + f0 + e) = make_uint4(y[0], y[1], y[2], y[3]);
+            *reinterpret_cast<uint4*>(row + f0 + e + 4) = make_uint4(y[4], y[5], y[6], y[7]);
+        }
     }
 }
-// 32 fp32 of this lane's row, a row of 128 bytes (128-byte swizzle)
-__device__ __forceinline__ void stage_row_f32(uint32_t buf, int lane, const float (&v)[32])
+// 16 fp32 of this lane's row of a piece, a row of 64 bytes (64-byte swizzle)
+__device__ __forceinline__ void read_row(uint32_t buf, int lane, float (&v)[16])
 {
 #pragma unroll
-    for (int c = 0; c < 8; ++c)
-        asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};\n" ::"r"(buf + lane * 128 + ((c ^ (lane & 7)) << 4)),
-                     "f"(v[4 * c]), "f"(v[4 * c + 1]), "f"(v[4 * c + 2]), "f"(v[4 * c + 3])
-                     : "memory");
-}
-__device__ __forceinline__ void read_row_f32(uint32_t buf, int lane, float (&v)[32])
-{
-#pragma unroll
-    for (int c = 0; c < 8; ++c)
+    for (int c = 0; c < 4; ++c)
         asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];\n"
                      : "=f"(v[4 * c]), "=f"(v[4 * c + 1]), "=f"(v[4 * c + 2]), "=f"(v[4 * c + 3])
-                     : "r"(buf + lane * 128 + ((c ^ (lane & 7)) << 4))
+                     : "r"(buf + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4))
                      : "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32])
@@ -173,8 +175,6 @@ template <bool AMn, bool BMn, int E>
 __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_constant__ Params<E> p)
 {
     using C = Cfg<E>;
-    constexpr int NT = C::NT;
-    constexpr uint32_t kStageBytes = C::kStageBytes;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     if (smem_u32(smem_raw) & 1023u) {     // the 128-byte swizzle atoms need a 1024-byte aligned base
         if (threadIdx.x == 0) atomicCAS(&p.status->code, 0, (int)ROLA_ERR_UNSUPPORTED);
@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
             mbar_init(bar(C::ACC_EMPTY + i), kEpiWarps);
         }
         mbar_init(bar(C::DRAIN), 1);
-        for (int i = 0; i < 2 * kEpiWarps; ++i) mbar_init(bar(C::GU_FULL + i), 1);
+        for (int i = 0; i < kEpiWarps; ++i) mbar_init(bar(C::GU_FULL + i), 1);
         fence_mbar_init();
     }
     if (warp == 1) {
@@ -293,146 +293,108 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
         }
     } else {
         // ------------------------------------------------------------ epilogue
-        const int q = warp & 3;                          // TMEM lane quarter: rows 32 q .. +31 of the tile
+        const int q = warp & 3, ew = warp - 2;           // TMEM lane quarter: rows 32 q .. +31 of the tile
+        const int half = ew >> 2;                        // of the columns
         const uint32_t lane_off = (uint32_t)(q * 32) << 16;
-        const uint32_t epi = sbase + C::kSmemEpi + (warp - 2) * C::kEpiBytes;
+        const uint32_t piece = sbase + C::kSmemEpi + ew * C::kEpiBytes;
+        constexpr int kCols = E == kGateGrad ? 16 : 32;              // columns of a chunk
+        constexpr int kHalf = (E == kGateUp ? 128 : NT) / 2, kChunks = kHalf / kCols;
         bool ok = true;
-        int it = 0, chunk = 0;
-        // a store buffer is free once the store issued two chunks ago has read it
-        auto next_buffer = [&]() {
-            if (lane == 0 && chunk >= 2) bulk_wait_read_1();
-            __syncwarp();
-            return epi + (chunk++ & 1) * kStoreBytes;
-        };
-        auto send = [&](const CUtensorMap* map, uint32_t buf, int x, int y, bool in) {
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                if (in) tma_store_2d(map, buf, x, y);
-                bulk_commit();                           // an empty group where nothing is stored
-            }
-        };
-        // kGateGrad: the 32 x 32 pieces of G and U of chunk c of tile t, into slot `slot`
-        auto fetch = [&](int t, int c, int slot) {
+        int it = 0;
+        // kGateGrad: G and U of chunk c of tile t
+        int fetched = 0, used = 0;
+        auto fetch = [&](int t, int c) {
+            if (t >= p.tiles) return;
             int mt, nt;
             tile_of(p, t, mt, nt);
             if (lane == 0) {
-                const uint32_t b = bar(C::GU_FULL + (warp - 2) * 2 + slot), dst = epi + slot * 2 * kStoreBytes;
-                mbar_expect_tx(b, 2 * kStoreBytes);
-                tma_load_2d(dst, &p.in[0], b, nt * NT + c * 32, mt * kTileM + q * 32);
-                tma_load_2d(dst + kStoreBytes, &p.in[E == kGateGrad ? 1 : 0], b, nt * NT + c * 32, mt * kTileM + q * 32);
+                const uint32_t b = bar(C::GU_FULL + ew);
+                const int x = nt * NT + half * kHalf + c * kCols, y = mt * kTileM + q * 32;
+                mbar_expect_tx(b, 2 * kPieceBytes);
+                tma_load_2d(piece, &p.in[0], b, x, y);
+                tma_load_2d(piece + kPieceBytes, &p.in[E == kGateGrad ? 1 : 0], b, x, y);
             }
+            ++fetched;
         };
-        int fetched = 0, used = 0;
-        if constexpr (E == kGateGrad)
-            if ((int)blockIdx.x < p.tiles) fetch(blockIdx.x, 0, fetched++ & 1);
+        if constexpr (E == kGateGrad) fetch(blockIdx.x, 0);
         for (int t = blockIdx.x; t < p.tiles && ok; t += gridDim.x, ++it) {
             int mt, nt;
             const Problem& r = tile_of(p, t, mt, nt);
             const int ab = it & 1;
             if (!(ok = mbar_wait(bar(C::ACC_FULL + ab), (it >> 1) & 1, abort, limit))) break;
             fence_after_sync();
-            const int row0 = mt * kTileM + q * 32;       // first row of this warp
+            const int row = mt * kTileM + q * 32 + lane;
+            const bool in = row < r.M;
+            const size_t at = (size_t)row * r.N;
             const uint32_t acc = tmem + lane_off + ab * NT;
-            auto release = [&]() {                       // the accumulator buffer is free for the tile after next
-                fence_before_sync();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(C::ACC_EMPTY + ab));
-            };
-            if constexpr (E == kStore) {
-                for (int c = 0; c < NT / 64; ++c) {
-                    const int f0 = nt * NT + c * 64;
-                    float v[64];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) tmem_ld16(acc + c * 64 + j * 16, *reinterpret_cast<float(*)[16]>(&v[j * 16]));
-                    tmem_ld_wait(*reinterpret_cast<float(*)[16]>(&v[0]));
-#pragma unroll
-                    for (int j = 1; j < 4; ++j) reg_fence(*reinterpret_cast<float(*)[16]>(&v[j * 16]));
-                    if (c == NT / 64 - 1) release();
-                    const uint32_t buf = next_buffer();
-                    stage_half_row64(buf, lane, 0, *reinterpret_cast<float(*)[32]>(&v[0]));
-                    stage_half_row64(buf, lane, 4, *reinterpret_cast<float(*)[32]>(&v[32]));
-                    send(&r.c[0], buf, f0, row0, row0 < r.M && f0 < r.N);
-                }
-            } else if constexpr (E == kGateUp) {
-                for (int c = 0; c < 2; ++c) {            // 64 of the tile's 128 features
-                    const int f0 = nt * 128 + c * 64;
-                    float h[64];
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const int col = c * 64 + half * 32, f = f0 + half * 32;
-                        float gv[32], uv[32];
-                        tmem_ld32(acc + col, gv);
-                        tmem_ld32(acc + 128 + col, uv);
-                        if (col == 96) release();
-                        if (p.keep) {
-                            const bool in = row0 < r.M && f < r.N;
-                            uint32_t buf = next_buffer();
-                            stage_row_f32(buf, lane, gv);
-                            send(&r.c[1], buf, f, row0, in);
-                            buf = next_buffer();
-                            stage_row_f32(buf, lane, uv);
-                            send(&r.c[2], buf, f, row0, in);
-                        }
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) h[half * 32 + j] = gate_act(p.act, gv[j]) * uv[j];
-                    }
-                    const uint32_t buf = next_buffer();
-                    stage_half_row64(buf, lane, 0, *reinterpret_cast<float(*)[32]>(&h[0]));
-                    stage_half_row64(buf, lane, 4, *reinterpret_cast<float(*)[32]>(&h[32]));
-                    send(&r.c[0], buf, f0, row0, row0 < r.M && f0 < r.N);
-                }
-            } else {
-                for (int c = 0; c < NT / 32; ++c, ++used) {
-                    // the next piece is on its way while this one is used
-                    const int tn = c + 1 < NT / 32 ? t : t + (int)gridDim.x;
-                    __syncwarp();                        // its slot was read by every lane
-                    if (tn < p.tiles) fetch(tn, c + 1 < NT / 32 ? c + 1 : 0, fetched++ & 1);
-                    const int slot = used & 1;
-                    if (!(ok = mbar_wait(bar(C::GU_FULL + (warp - 2) * 2 + slot), (used >> 1) & 1, abort, limit))) break;
-                    float dh[32], gv[32], uv[32];
-                    tmem_ld32(acc + c * 32, dh);
-                    if (c == NT / 32 - 1) release();
-                    read_row_f32(epi + slot * 2 * kStoreBytes, lane, gv);
-                    read_row_f32(epi + slot * 2 * kStoreBytes + kStoreBytes, lane, uv);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        float a, da;
-                        gate_act_grad(p.act, gv[j], a, da);
-                        const float d = dh[j], u = uv[j];
-                        gv[j] = a * u;                   // H
-                        uv[j] = d * u * da;              // dG
-                        dh[j] = d * a;                   // dU
-                    }
-                    const uint32_t buf = epi + 4 * kStoreBytes;
-                    if (lane == 0) bulk_wait_read_all();
+            for (int c = 0; c < kChunks && ok; ++c) {
+                // the last piece is in registers: the accumulator buffer is free for the tile after next
+                auto release = [&]() {
+                    if (c != kChunks - 1) return;
+                    fence_before_sync();
                     __syncwarp();
-                    stage_row32(buf, lane, gv);
-                    stage_row32(buf + 2048, lane, uv);
-                    stage_row32(buf + 4096, lane, dh);
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    const int f0 = nt * NT + c * 32;
-                    if (lane == 0) {
-                        if (row0 < r.M && f0 < r.N) {
-                            tma_store_2d(&r.c[0], buf, f0, row0);
-                            tma_store_2d(&r.c[1], buf + 2048, f0, row0);
-                            tma_store_2d(&r.c[2], buf + 4096, f0, row0);
+                    if (lane == 0) mbar_arrive(bar(C::ACC_EMPTY + ab));
+                };
+                if constexpr (E == kStore) {
+                    const int col = half * kHalf + c * kCols;
+                    float v[32];
+                    tmem_ld32(acc + col, v);
+                    release();
+                    if (in) store_row(r.c[0] + at, nt * NT + col, r.N, v, r.wide);
+                } else if constexpr (E == kGateUp) {
+                    const int col = half * kHalf + c * kCols, f0 = nt * 128 + col;
+                    float gv[32], uv[32];
+                    tmem_ld32(acc + col, gv);
+                    tmem_ld32(acc + 128 + col, uv);
+                    release();
+                    if (in && p.G) {
+                        store_row(p.G + at, f0, r.N, gv, r.wide);
+                        store_row(p.U + at, f0, r.N, uv, r.wide);
+                    }
+                    with_act(p.act, [&](auto act) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) gv[j] = act.phi(gv[j]) * uv[j];
+                    });
+                    if (in) store_row(r.c[0] + at, f0, r.N, gv, r.wide);
+                } else {
+                    const int col = half * kHalf + c * kCols, f0 = nt * NT + col;
+                    float dh[16], gv[16], uv[16];
+                    tmem_ld16(acc + col, dh);
+                    tmem_ld_wait(dh);
+                    release();
+                    if (!(ok = mbar_wait(bar(C::GU_FULL + ew), used & 1, abort, limit))) break;
+                    ++used;
+                    read_row(piece, lane, gv);
+                    read_row(piece + kPieceBytes, lane, uv);
+                    __syncwarp();                        // every lane has read its rows
+                    // the next piece comes under this one's work
+                    if (c + 1 < kChunks) fetch(t, c + 1);
+                    else fetch(t + (int)gridDim.x, 0);
+                    with_act(p.act, [&](auto act) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            float a, da;
+                            act.grad(gv[j], a, da);
+                            const float d = dh[j], u = uv[j];
+                            gv[j] = a * u;               // H
+                            uv[j] = d * u * da;          // dG
+                            dh[j] = d * a;               // dU
                         }
-                        bulk_commit();
+                    });
+                    if (in) {
+                        store_row(r.c[0] + at, f0, r.N, gv, r.wide);
+                        store_row(r.c[1] + at, f0, r.N, uv, r.wide);
+                        store_row(r.c[2] + at, f0, r.N, dh, r.wide);
                     }
                 }
             }
         }
         if (!ok) record_timeout(p, 3);
-        if (lane == 0) {
-            if constexpr (E == kGateGrad) {              // the pieces still in flight land before the CTA exits
+        if constexpr (E == kGateGrad)                    // the pieces still in flight land before the CTA exits
+            if (lane == 0) {
                 int never = 0;
-                for (; used < fetched; ++used)
-                    mbar_wait(bar(C::GU_FULL + (warp - 2) * 2 + (used & 1)), (used >> 1) & 1, &never, limit);
+                for (; used < fetched; ++used) mbar_wait(bar(C::GU_FULL + ew), used & 1, &never, limit);
             }
-            bulk_wait_all();                             // the stores have left shared memory
-        }
     }
     fence_before_sync();
     __syncthreads();
@@ -461,7 +423,9 @@ cudaError_t launch(const FfnShape& s, Params<E>& p, DeviceStatus* status, cudaSt
     for (int i = 0; i < p.problems; ++i) {
         Problem& r = p.pr[i];
         r.m_tiles = (r.M + kTileM - 1) / kTileM;
-        r.n_tiles = (r.N + (E == kGateUp ? 127 : C::NT - 1)) / (E == kGateUp ? 128 : C::NT);
+        r.n_tiles = (r.N + (E == kGateUp ? 127 : NT - 1)) / (E == kGateUp ? 128 : NT);
+        r.wide = r.N % 16 == 0 && ((reinterpret_cast<uintptr_t>(p.G) | reinterpret_cast<uintptr_t>(p.U)) & 31u) == 0;
+        for (const __nv_bfloat16* c : r.c) r.wide = r.wide && (reinterpret_cast<uintptr_t>(c) & 31u) == 0;
         r.tile0 = p.tiles;
         p.tiles += r.m_tiles * r.n_tiles;
     }
@@ -480,6 +444,40 @@ cudaError_t launch(const FfnShape& s, Params<E>& p, DeviceStatus* status, cudaSt
 
 int steps(int k) { return (k + kStepK - 1) / kStepK; }
 
+// dH = dY Wd, and from it H, dG, dU
+cudaError_t launch_dh(const FfnShape& s, const void* Wd, const float* G, const float* U, const void* dY, void* H,
+                      void* dG, void* dU, DeviceStatus* status, cudaStream_t st)
+{
+    Params<kGateGrad> p{};
+    Problem& r = p.pr[0];
+    p.problems = 1;
+    r.M = s.M; r.N = s.F; r.k_steps = steps(s.D); r.sources = 1;
+    r.c[0] = static_cast<__nv_bfloat16*>(H);
+    r.c[1] = static_cast<__nv_bfloat16*>(dG);
+    r.c[2] = static_cast<__nv_bfloat16*>(dU);
+    const auto f32 = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+    if (!operand_map(&r.a[0], dY, s.M, s.D, true, kTileM) || !operand_map(&r.b[0], Wd, s.D, s.F, false, 0) ||
+        !encode_2d(&p.in[0], f32, 4, G, s.M, s.F, 16, 32, CU_TENSOR_MAP_SWIZZLE_64B) ||
+        !encode_2d(&p.in[1], f32, 4, U, s.M, s.F, 16, 32, CU_TENSOR_MAP_SWIZZLE_64B))
+        return cudaErrorInvalidValue;
+    return launch<false, true, kGateGrad>(s, p, status, st);
+}
+
+// dX = dG Wg + dU Wu
+cudaError_t launch_dx(const FfnShape& s, const void* Wg, const void* Wu, const void* dG, const void* dU, void* dX,
+                      DeviceStatus* status, cudaStream_t st)
+{
+    Params<kStore> p{};
+    Problem& r = p.pr[0];
+    p.problems = 1;
+    r.M = s.M; r.N = s.D; r.k_steps = steps(s.F); r.sources = 2;
+    if (!operand_map(&r.a[0], dG, s.M, s.F, true, kTileM) || !operand_map(&r.a[1], dU, s.M, s.F, true, kTileM) ||
+        !operand_map(&r.b[0], Wg, s.F, s.D, false, 0) || !operand_map(&r.b[1], Wu, s.F, s.D, false, 0))
+        return cudaErrorInvalidValue;
+    r.c[0] = static_cast<__nv_bfloat16*>(dX);
+    return launch<false, true, kStore>(s, p, status, st);
+}
+
 }  // namespace
 
 cudaError_t launch_ffn_up_tc(const FfnShape& s, const void* X, const void* Wg, const void* Wu, void* H, float* G,
@@ -488,15 +486,13 @@ cudaError_t launch_ffn_up_tc(const FfnShape& s, const void* X, const void* Wg, c
     Params<kGateUp> p{};
     Problem& r = p.pr[0];
     p.problems = 1;
-    p.keep = G != nullptr;
+    p.G = G;
+    p.U = U;
+    r.c[0] = static_cast<__nv_bfloat16*>(H);
     r.M = s.M; r.N = s.F; r.k_steps = steps(s.D); r.sources = 1;
-    bool ok = operand_map(&r.a[0], X, s.M, s.D, true, kTileM) && operand_map(&r.b[0], Wg, s.F, s.D, true, 128) &&
-              operand_map(&r.b[1], Wu, s.F, s.D, true, 128) &&
-              encode_2d(&r.c[0], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, H, s.M, s.F, 64, 32, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (G)
-        ok = ok && encode_2d(&r.c[1], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, G, s.M, s.F, 32, 32, CU_TENSOR_MAP_SWIZZLE_128B) &&
-             encode_2d(&r.c[2], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, U, s.M, s.F, 32, 32, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (!ok) return cudaErrorInvalidValue;
+    if (!operand_map(&r.a[0], X, s.M, s.D, true, kTileM) || !operand_map(&r.b[0], Wg, s.F, s.D, true, 128) ||
+        !operand_map(&r.b[1], Wu, s.F, s.D, true, 128))
+        return cudaErrorInvalidValue;
     return launch<false, false, kGateUp>(s, p, status, st);
 }
 
@@ -507,8 +503,8 @@ cudaError_t launch_ffn_down_tc(const FfnShape& s, const void* H, const void* Wd,
     Problem& r = p.pr[0];
     p.problems = 1;
     r.M = s.M; r.N = s.D; r.k_steps = steps(s.F); r.sources = 1;
-    if (!operand_map(&r.a[0], H, s.M, s.F, true, kTileM) || !operand_map(&r.b[0], Wd, s.D, s.F, true, 256) ||
-        !encode_2d(&r.c[0], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, Y, s.M, s.D, 64, 32, CU_TENSOR_MAP_SWIZZLE_128B))
+    r.c[0] = static_cast<__nv_bfloat16*>(Y);
+    if (!operand_map(&r.a[0], H, s.M, s.F, true, kTileM) || !operand_map(&r.b[0], Wd, s.D, s.F, true, 256))
         return cudaErrorInvalidValue;
     return launch<false, false, kStore>(s, p, status, st);
 }
@@ -517,38 +513,13 @@ cudaError_t launch_ffn_backward_tc(const FfnShape& s, const void* X, const void*
                                    const float* G, const float* U, const void* dY, void* H, void* dG, void* dU,
                                    void* dX, void* dWg, void* dWu, void* dWd, DeviceStatus* status, cudaStream_t st)
 {
-    const auto bf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-    const auto f32 = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
-    const auto sw128 = CU_TENSOR_MAP_SWIZZLE_128B, sw64 = CU_TENSOR_MAP_SWIZZLE_64B;
     if (s.M <= kFfnFewTokens) {
         cudaError_t e = launch_ffn_few_grad(s, Wg, Wu, Wd, G, U, dY, H, dG, dU, dX, status, st);
         if (e != cudaSuccess) return e;
     } else {
-    {   // dH = dY Wd, and from it H, dG, dU
-        Params<kGateGrad> p{};
-        Problem& r = p.pr[0];
-        p.problems = 1;
-        r.M = s.M; r.N = s.F; r.k_steps = steps(s.D); r.sources = 1;
-        if (!operand_map(&r.a[0], dY, s.M, s.D, true, kTileM) || !operand_map(&r.b[0], Wd, s.D, s.F, false, 0) ||
-            !encode_2d(&r.c[0], bf16, 2, H, s.M, s.F, 32, 32, sw64) || !encode_2d(&r.c[1], bf16, 2, dG, s.M, s.F, 32, 32, sw64) ||
-            !encode_2d(&r.c[2], bf16, 2, dU, s.M, s.F, 32, 32, sw64) || !encode_2d(&p.in[0], f32, 4, G, s.M, s.F, 32, 32, sw128) ||
-            !encode_2d(&p.in[1], f32, 4, U, s.M, s.F, 32, 32, sw128))
-            return cudaErrorInvalidValue;
-        cudaError_t e = launch<false, true, kGateGrad>(s, p, status, st);
+        cudaError_t e = launch_dh(s, Wd, G, U, dY, H, dG, dU, status, st);
+        if (e == cudaSuccess) e = launch_dx(s, Wg, Wu, dG, dU, dX, status, st);
         if (e != cudaSuccess) return e;
-    }
-    {   // dX = dG Wg + dU Wu
-        Params<kStore> p{};
-        Problem& r = p.pr[0];
-        p.problems = 1;
-        r.M = s.M; r.N = s.D; r.k_steps = steps(s.F); r.sources = 2;
-        if (!operand_map(&r.a[0], dG, s.M, s.F, true, kTileM) || !operand_map(&r.a[1], dU, s.M, s.F, true, kTileM) ||
-            !operand_map(&r.b[0], Wg, s.F, s.D, false, 0) || !operand_map(&r.b[1], Wu, s.F, s.D, false, 0) ||
-            !encode_2d(&r.c[0], bf16, 2, dX, s.M, s.D, 64, 32, sw128))
-            return cudaErrorInvalidValue;
-        cudaError_t e = launch<false, true, kStore>(s, p, status, st);
-        if (e != cudaSuccess) return e;
-    }
     }
     // dWg = dG^T X, dWu = dU^T X, dWd = dY^T H: K is the token
     Params<kStore> p{};
@@ -558,8 +529,8 @@ cudaError_t launch_ffn_backward_tc(const FfnShape& s, const void* X, const void*
     for (int i = 0; i < 3; ++i) {
         Problem& r = p.pr[i];
         r.M = w[i].m; r.N = w[i].n; r.k_steps = steps(s.M); r.sources = 1;
-        if (!operand_map(&r.a[0], w[i].a, s.M, w[i].m, false, 0) || !operand_map(&r.b[0], w[i].b, s.M, w[i].n, false, 0) ||
-            !encode_2d(&r.c[0], bf16, 2, w[i].c, w[i].m, w[i].n, 64, 32, sw128))
+        r.c[0] = static_cast<__nv_bfloat16*>(w[i].c);
+        if (!operand_map(&r.a[0], w[i].a, s.M, w[i].m, false, 0) || !operand_map(&r.b[0], w[i].b, s.M, w[i].n, false, 0))
             return cudaErrorInvalidValue;
     }
     return launch<true, true, kStore>(s, p, status, st);

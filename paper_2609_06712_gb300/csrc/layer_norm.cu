@@ -63,6 +63,60 @@ __device__ __forceinline__ void store_piece(T* p, const float (&x)[V])
     else store16(p, x);
 }
 
+// Two elements an instruction (packed fp32, each element an IEEE operation): the rows of d = 1536 leave an SM
+// 430 cycles a row, fewer than one instruction per element and operation would take.
+__device__ __forceinline__ void fma2(float* d, const float* a, const float* b, const float* c)
+{
+    asm("{\n.reg .b64 ra, rb, rc;\nmov.b64 ra, {%2, %3};\nmov.b64 rb, {%4, %5};\nmov.b64 rc, {%6, %7};\n"
+        "fma.rn.f32x2 ra, ra, rb, rc;\nmov.b64 {%0, %1}, ra;\n}\n"
+        : "=f"(d[0]), "=f"(d[1]) : "f"(a[0]), "f"(a[1]), "f"(b[0]), "f"(b[1]), "f"(c[0]), "f"(c[1]));
+}
+// d = a b + c of a piece; b and c may be one value for all elements
+template <int V>
+__device__ __forceinline__ void fma_piece(float (&d)[V], const float (&a)[V], const float (&b)[V], const float (&c)[V])
+{
+    if constexpr (V == 1) d[0] = fmaf(a[0], b[0], c[0]);
+    else
+#pragma unroll
+        for (int e = 0; e < V; e += 2) fma2(d + e, a + e, b + e, c + e);
+}
+template <int V>
+__device__ __forceinline__ void fma_piece(float (&d)[V], const float (&a)[V], float b, float c)
+{
+    const float bb[2] = {b, b}, cc[2] = {c, c};
+    if constexpr (V == 1) d[0] = fmaf(a[0], b, c);
+    else
+#pragma unroll
+        for (int e = 0; e < V; e += 2) fma2(d + e, a + e, bb, cc);
+}
+// s (two partial sums) += a b, or += a
+template <int V>
+__device__ __forceinline__ void dot_piece(float (&s)[2], const float (&a)[V], const float (&b)[V])
+{
+    if constexpr (V == 1) s[0] = fmaf(a[0], b[0], s[0]);
+    else
+#pragma unroll
+        for (int e = 0; e < V; e += 2) fma2(s, a + e, b + e, s);
+}
+template <int V>
+__device__ __forceinline__ void add_piece(float (&d)[V], const float (&a)[V])
+{
+    const float one[2] = {1.0f, 1.0f};
+    if constexpr (V == 1) d[0] += a[0];
+    else
+#pragma unroll
+        for (int e = 0; e < V; e += 2) fma2(d + e, a + e, one, d + e);
+}
+template <int V>
+__device__ __forceinline__ void sum_piece(float (&s)[2], const float (&a)[V])
+{
+    const float one[2] = {1.0f, 1.0f};
+    if constexpr (V == 1) s[0] += a[0];
+    else
+#pragma unroll
+        for (int e = 0; e < V; e += 2) fma2(s, a + e, one, s);
+}
+
 // Sum of (a, b) over the threads of a group, the same bits in every thread.  A
 // group of more than one warp is the whole CTA; `turn` alternates between two
 // buffers, so that one barrier separates a sum's writes from its reads and the
@@ -81,13 +135,24 @@ __device__ __forceinline__ float2 group_sum(float a, float b, float2 (*red)[32],
         turn ^= 1;
         if (lane == 0) buf[threadIdx.x >> 5] = make_float2(a, b);
         __syncthreads();
-        const float2 t = lane < (int)(blockDim.x >> 5) ? buf[lane] : make_float2(0.0f, 0.0f);
-        a = t.x;
-        b = t.y;
+        const int warps = blockDim.x >> 5;
+        if (warps <= 4) {
+            a = b = 0.0f;
 #pragma unroll
-        for (int off = 16; off >= 1; off >>= 1) {
-            a += __shfl_xor_sync(0xffffffffu, a, off);
-            b += __shfl_xor_sync(0xffffffffu, b, off);
+            for (int w = 0; w < 4; ++w)
+                if (w < warps) {
+                    a += buf[w].x;
+                    b += buf[w].y;
+                }
+        } else {
+            const float2 t = lane < warps ? buf[lane] : make_float2(0.0f, 0.0f);
+            a = t.x;
+            b = t.y;
+#pragma unroll
+            for (int off = 16; off >= 1; off >>= 1) {
+                a += __shfl_xor_sync(0xffffffffu, a, off);
+                b += __shfl_xor_sync(0xffffffffu, b, off);
+            }
         }
     }
     return make_float2(a, b);
@@ -241,24 +306,19 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : kMaxThreads)
         float v[1][NV][V];
         q.read(v);
         q.ahead(r);
-        float s = 0.0f;
+        float s[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < V; ++e) s += v[0][i][e];
-        const float mu = group_sum<WARP>(s, 0.0f, red, turn).x * inv_d;
+        for (int i = 0; i < NV; ++i) sum_piece<V>(s, v[0][i]);
+        const float mu = group_sum<WARP>(s[0] + s[1], 0.0f, red, turn).x * inv_d;
         q.refill();
-        float sq = 0.0f;
+        float sq[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (q.gt + i * q.tpr < q.pieces) {
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    v[0][i][e] -= mu;
-                    sq = fmaf(v[0][i][e], v[0][i][e], sq);
-                }
+                fma_piece<V>(v[0][i], v[0][i], 1.0f, -mu);
+                dot_piece<V>(sq, v[0][i], v[0][i]);
             }
-        const float rs = 1.0f / sqrtf(group_sum<WARP>(sq, 0.0f, red, turn).x * inv_d + eps);
+        const float rs = 1.0f / sqrtf(group_sum<WARP>(sq[0] + sq[1], 0.0f, red, turn).x * inv_d + eps);
         if (mean && q.gt == 0) {
             mean[r] = mu;
             rstd[r] = rs;
@@ -268,16 +328,16 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : kMaxThreads)
         for (int i = 0; i < NV; ++i) {
             const int c = q.gt + i * q.tpr;
             if (c < q.pieces) {
-#pragma unroll
-                for (int e = 0; e < V; ++e) v[0][i][e] = fmaf(v[0][i][e] * rs, g[i][e], b[i][e]);
+                fma_piece<V>(v[0][i], v[0][i], rs, 0.0f);
+                fma_piece<V>(v[0][i], v[0][i], g[i], b[i]);
                 store_piece<T, V>(yr + (size_t)c * V, v[0][i]);
             }
         }
     }
 }
 
-template <typename T, int V, int NV, bool WARP>
-__global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : kMaxThreads)
+template <typename T, int V, int NV, bool WARP, int TH = kMaxThreads, int MIN = 1>
+__global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
     ln_bwd_kernel(long long rows, int d, const T* __restrict__ x, const T* __restrict__ gamma,
                   const float* __restrict__ mean, const float* __restrict__ rstd, const T* dy, T* dx,
                   float* __restrict__ part, int depth)
@@ -314,20 +374,18 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : kMaxThreads)
         float v[2][NV][V];               // xh, a
         q.read(v);
         q.ahead(r);
-        float s1 = 0.0f, s2 = 0.0f;
+        float s1[2] = {0.0f, 0.0f}, s2[2] = {0.0f, 0.0f}, zero[V] = {};
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (q.gt + i * q.tpr < q.pieces) {
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    float &xh = v[0][i][e], &a = v[1][i][e];
-                    xh = (xh - mu) * rs;
-                    dg[i][e] = fmaf(a, xh, dg[i][e]);
-                    db[i][e] += a;
-                    a *= g[i][e];
-                    s1 += a;
-                    s2 = fmaf(a, xh, s2);
-                }
+                float (&xh)[V] = v[0][i], (&a)[V] = v[1][i];
+                fma_piece<V>(xh, xh, 1.0f, -mu);         // centred first: mu may be far larger than x - mu
+                fma_piece<V>(xh, xh, rs, 0.0f);
+                fma_piece<V>(dg[i], a, xh, dg[i]);
+                add_piece<V>(db[i], a);
+                fma_piece<V>(a, a, g[i], zero);
+                sum_piece<V>(s1, a);
+                dot_piece<V>(s2, a, xh);
             }
         }
         const float rs0 = rs;
@@ -335,7 +393,7 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : kMaxThreads)
             mu = mean[r + q.stride];
             rs = rstd[r + q.stride];
         }
-        const float2 m = group_sum<WARP>(s1, s2, red, turn);
+        const float2 m = group_sum<WARP>(s1[0] + s1[1], s2[0] + s2[1], red, turn);
         q.refill();
         const float m1 = m.x * inv_d, m2 = m.y * inv_d;
         T* dxr = dx + r * d;
@@ -343,8 +401,9 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : kMaxThreads)
         for (int i = 0; i < NV; ++i) {
             const int c = q.gt + i * q.tpr;
             if (c < q.pieces) {
-#pragma unroll
-                for (int e = 0; e < V; ++e) v[1][i][e] = rs0 * (v[1][i][e] - m1 - v[0][i][e] * m2);
+                fma_piece<V>(v[0][i], v[0][i], -m2, -m1);        // rs (a - (m1 + xh m2))
+                add_piece<V>(v[1][i], v[0][i]);
+                fma_piece<V>(v[1][i], v[1][i], rs0, 0.0f);
                 store_piece<T, V>(dxr + (size_t)c * V, v[1][i]);
             }
         }
@@ -516,8 +575,8 @@ struct LnArgs {
 };
 
 // CTA size, ring depth and grid of rows of `pieces` pieces, NV per thread: a warp per row, or a CTA of the
-// least whole number of warps.  The rings of an SM's CTAs (some 512 threads of them) hold about 160 KB, and no
-// more rows than a group has.
+// least whole number of warps.  The rings of an SM's CTAs (as many as their registers allow, up to 1024
+// threads) hold about 160 KB, and no more rows than a group has.
 struct Launch {
     int threads, grid, depth;
     size_t smem;
@@ -527,7 +586,11 @@ cudaError_t shape_of(K kernel, const LnArgs& a, bool warp, int pieces, int nv, i
                      size_t sums, Launch* l)
 {
     l->threads = warp ? 32 * kWarpGroups : ((pieces + nv - 1) / nv + 31) / 32 * 32;
-    const int groups = warp ? kWarpGroups : 1, ctas = l->threads < 512 ? 512 / l->threads : 1;
+    int ctas = 0;
+    cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, kernel, l->threads, 0);
+    if (e != cudaSuccess) return e;
+    if (ctas > 1024 / l->threads) ctas = 1024 / l->threads;
+    const int groups = warp ? kWarpGroups : 1;
     const long long want = (a.rows + groups - 1) / groups;
     l->depth = 0;
     size_t ring = 0;
@@ -540,7 +603,6 @@ cudaError_t shape_of(K kernel, const LnArgs& a, bool warp, int pieces, int nv, i
         ring = (size_t)groups * matrices * l->depth * row_bytes;
     }
     l->smem = (size_t)groups * kMaxDepth * 8 + (ring > sums ? ring : sums);
-    cudaError_t e = cudaSuccess;
     if (l->smem > 48 << 10) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)l->smem);
     if (e != cudaSuccess) return e;
     int per_sm = 0;
@@ -563,11 +625,11 @@ cudaError_t fwd_one(const LnArgs& a)
                                                 a.rstd, l.depth);
     return cudaGetLastError();
 }
-template <typename T, int V, int NV, bool WARP>
+template <typename T, int V, int NV, bool WARP, int TH = kMaxThreads, int MIN = 1>
 cudaError_t bwd_one(LnArgs& a)
 {
     Launch l;
-    auto kernel = ln_bwd_kernel<T, V, NV, WARP>;
+    auto kernel = ln_bwd_kernel<T, V, NV, WARP, TH, MIN>;
     cudaError_t e = shape_of(kernel, a, WARP, a.d / V, NV, 2, V > 1 ? sizeof(T) * a.d : 0,
                              WARP && a.part ? sizeof(float) * 2 * a.d : 0, &l);
     if (e != cudaSuccess) return e;
@@ -611,6 +673,8 @@ cudaError_t bwd(LnArgs& a)
     if constexpr (V > 1) {
         if (pieces <= 32) return bwd_one<T, V, 1, true>(a);
         if (pieces <= 64) return bwd_one<T, V, 2, true>(a);
+        // up to 320 threads two CTAs an SM: with one, the barriers of a row (d = 5120) leave HBM idle
+        if (pieces <= 2 * 320) return bwd_one<T, V, 2, false, 320, 2>(a);
         if (pieces <= 2 * kMaxThreads) return bwd_one<T, V, 2, false>(a);
         if (pieces <= 4 * kMaxThreads) return bwd_one<T, V, 4, false>(a);
     } else {
