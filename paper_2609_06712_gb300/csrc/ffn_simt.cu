@@ -13,6 +13,12 @@
 // and the same 64 rows of Wu, so that a thread holds g and u of the same
 // features (columns tx*4 .. and 64 + tx*4 ..) and phi and the product need no
 // exchange.  Bound by fp32 FMA issue.
+//
+// Up to 32 tokens that tile would be mostly empty rows, and the weights are what
+// has to be read.  Then a warp takes whole weight rows against 8 tokens (up and
+// down, whose weights lie along k), or a CTA 64 weight columns against 8 tokens, its 32
+// warps sharing the K axis (dH and dX, whose weights lie across it); the parts
+// meet in a fixed order.
 #include "block_ops.cuh"
 
 namespace rola {
@@ -172,9 +178,152 @@ __global__ void __launch_bounds__(256, 2) simt_gemm_kernel(Operand a0, Operand b
     }
 }
 
+// ---------------------------------------------------------------- few tokens
+
+constexpr int kFewTokens = 32, kChunk = 8;       // most tokens; of a CTA
+
+// Outputs n .. n + R - 1 of a warp for the 8 tokens from 8 blockIdx.y on: sum_k a(m, k) b(n, k), both
+// contiguous along k.  kGateUp: R / 2 features, W_gate rows first.
+template <int R, int E>
+__global__ void __launch_bounds__(256) few_rows_kernel(Operand a, Operand b0, Operand b1, const Args p)
+{
+    constexpr int FEATURES = E == kGateUp ? R / 2 : R;
+    const int lane = threadIdx.x & 31;
+    const int n0 = (blockIdx.x * 8 + (threadIdx.x >> 5)) * FEATURES, m0 = blockIdx.y * kChunk;
+    if (n0 >= p.N) return;
+    float acc[R][kChunk] = {};
+    for (int k = lane * 4; k < p.K; k += 128) {
+        float4 w[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int n = min(n0 + r % FEATURES, p.N - 1);
+            w[r] = load4((r < FEATURES ? b0.p : b1.p) + (size_t)n * b0.ld + k);
+        }
+#pragma unroll
+        for (int m = 0; m < kChunk; ++m) {
+            const float4 x = load4(a.p + (size_t)min(m0 + m, p.M - 1) * a.ld + k);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                acc[r][m] = fmaf(x.x, w[r].x, fmaf(x.y, w[r].y, fmaf(x.z, w[r].z, fmaf(x.w, w[r].w, acc[r][m]))));
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int m = 0; m < kChunk; ++m)
+#pragma unroll
+            for (int off = 16; off >= 1; off >>= 1) acc[r][m] += __shfl_xor_sync(0xffffffffu, acc[r][m], off);
+    // lane m writes token m
+#pragma unroll
+    for (int m = 0; m < kChunk; ++m) {
+        if (lane != m || m0 + m >= p.M) continue;
+#pragma unroll
+        for (int f = 0; f < FEATURES; ++f) {
+            if (n0 + f >= p.N) continue;
+            const size_t at = (size_t)(m0 + m) * p.ldc + n0 + f;
+            if constexpr (E == kGateUp) {
+                const float g = acc[f][m], u = acc[f + FEATURES][m];
+                static_cast<float*>(p.C)[at] = gate_act(p.act, g) * u;
+                if (p.G) {
+                    p.G[at] = g;
+                    p.U[at] = u;
+                }
+            } else {
+                static_cast<float*>(p.C)[at] = acc[f][m];
+            }
+        }
+    }
+}
+
+// Columns 64 blockIdx.x .. of 8 tokens: sum_k a(m, k) b(k, n), b contiguous along n; `sources` such products.
+template <int E>
+__global__ void __launch_bounds__(1024) few_columns_kernel(Operand a0, Operand b0, Operand a1, Operand b1, const Args p)
+{
+    constexpr int kPart = 512;                   // of the K axis staged at a time
+    __shared__ __align__(16) float as[kChunk][kPart];
+    __shared__ __align__(16) float part[32][64];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int n = blockIdx.x * 64 + (lane & 15) * 4, m0 = blockIdx.y * kChunk;
+    const bool in = n < p.N;                     // N is a multiple of 8
+    float acc[kChunk][4] = {};
+    for (int s = 0; s < p.sources; ++s) {
+        const Operand &a = s ? a1 : a0, &b = s ? b1 : b0;
+        for (int k0 = 0; k0 < p.K; k0 += kPart) {
+            __syncthreads();
+            for (int e = threadIdx.x; e < kChunk * kPart; e += 1024) {
+                const int m = e / kPart, k = k0 + e % kPart;
+                as[m][e % kPart] = k < p.K && m0 + m < p.M ? a.p[(size_t)(m0 + m) * a.ld + k] : 0.0f;
+            }
+            __syncthreads();
+            const int end = min(kPart, p.K - k0);
+#pragma unroll 4
+            for (int k = warp * 2 + (lane >> 4); k < end; k += 64) {
+                const float4 w = in ? load4(b.p + (size_t)(k0 + k) * b.ld + n) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int m = 0; m < kChunk; ++m) {
+                    const float x = as[m][k];
+                    acc[m][0] = fmaf(x, w.x, acc[m][0]);
+                    acc[m][1] = fmaf(x, w.y, acc[m][1]);
+                    acc[m][2] = fmaf(x, w.z, acc[m][2]);
+                    acc[m][3] = fmaf(x, w.w, acc[m][3]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < kChunk; ++m) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[m][e] += __shfl_xor_sync(0xffffffffu, acc[m][e], 16);
+        __syncthreads();
+        if (lane < 16)
+            *reinterpret_cast<float4*>(&part[warp][lane * 4]) = make_float4(acc[m][0], acc[m][1], acc[m][2], acc[m][3]);
+        __syncthreads();
+        const int c = threadIdx.x, col = blockIdx.x * 64 + c;
+        if (c < 64 && col < p.N && m0 + m < p.M) {
+            float x = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 32; ++w) x += part[w][c];
+            const size_t at = (size_t)(m0 + m) * p.ldc + col;
+            if constexpr (E == kStore) {
+                static_cast<float*>(p.C)[at] = x;
+            } else {
+                float ph, dph;
+                gate_act_grad(p.act, p.G_in[at], ph, dph);
+                const float u = p.U_in[at];
+                static_cast<float*>(p.C)[at] = ph * u;
+                static_cast<float*>(p.C2)[at] = x * u * dph;
+                static_cast<float*>(p.C3)[at] = x * ph;
+            }
+        }
+    }
+}
+
+// Rows per warp: four (the tokens' words are read once for them) where that still leaves 8 warps for each SM.
+template <int E>
+cudaError_t few_rows(Operand a, Operand b0, Operand b1, const Args& p, cudaStream_t st)
+{
+    const int chunks = (p.M + kChunk - 1) / kChunk, per = E == kGateUp ? 2 : 1;      // rows of a feature
+    auto go = [&](auto kernel, int rows) {
+        const int features = 8 * rows / per;                                         // of a CTA
+        kernel<<<dim3((p.N + features - 1) / features, chunks), 256, 0, st>>>(a, b0, b1, p);
+        return cudaGetLastError();
+    };
+    return (int64_t)p.N * per * chunks / 4 >= 8 * 152 ? go(few_rows_kernel<4, E>, 4) : go(few_rows_kernel<per, E>, per);
+}
+template <int E>
+cudaError_t few_columns(Operand a0, Operand b0, Operand a1, Operand b1, const Args& p, cudaStream_t st)
+{
+    few_columns_kernel<E><<<dim3((p.N + 63) / 64, (p.M + kChunk - 1) / kChunk), 1024, 0, st>>>(a0, b0, a1, b1, p);
+    return cudaGetLastError();
+}
+
 template <bool AK, bool BK, int E>
 cudaError_t gemm(Operand a0, Operand b0, Operand a1, Operand b1, const Args& p, cudaStream_t st)
 {
+    if (p.M <= kFewTokens && AK) {               // (a weight's gradient has its token along k)
+        if constexpr (BK) return few_rows<E>(a0, b0, b1, p, st);
+        else if constexpr (AK) return few_columns<E>(a0, b0, a1, b1, p, st);
+    }
     const int nt = E == kGateUp ? 64 : kTile;
     const dim3 grid((p.N + nt - 1) / nt, (p.M + kTile - 1) / kTile);
     simt_gemm_kernel<AK, BK, E><<<grid, 256, 0, st>>>(a0, b0, a1, b1, p);
