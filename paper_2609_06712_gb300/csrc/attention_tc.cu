@@ -92,7 +92,7 @@ __device__ __forceinline__ Item item_of(const Params& p, int i)
     }
     int qt;
     if (s.causal) {              // the longest rows of every head first
-        qt = p.q_tiles - 1 - i / s.heads;
+        qt = falling_tile(i / s.heads, p.q_tiles, s.H / s.Hk);
         it.head = i % s.heads;
     } else {                     // head by head: the CTAs in flight share few heads' keys
         it.head = i / p.q_tiles;
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
                             lane * 64, key0, head);
             ++c;
         };
-        for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
+        for (int turn = 0, i; (i = turn_item(turn, p.items)) < p.items && ok; ++turn) {
             const Item it = item_of(p, i);
             if (it.H == 0) continue;
             for (int g = 0; g < 2 && ok; ++g) {
@@ -272,20 +272,24 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
                 }
                 if ((h & 1) || h == it.H - 1) release(slot, (h & ~1) < Hg);
             };
-            // the next item that has steps
-            auto next_item = [&](int i, Item& it) {
-                for (; i < p.items; i += gridDim.x) {
+            // the next item that has steps, from the turn on
+            auto next_item = [&](int& turn, Item& it) {
+                int i;
+                for (; (i = turn_item(turn, p.items)) < p.items; ++turn) {
                     it = item_of(p, i);
                     if (it.H) break;
                 }
-                return i;
+                return i < p.items;
             };
             Item it{}, nx{};
-            int i = next_item(blockIdx.x, it), tile = 0, done = 0;      // done: QK steps of `it` issued already
-            while (i < p.items && ok) {
-                const int ni = next_item(i + gridDim.x, nx), ntile = tile + (it.H + 1) / 2;
-                const int Hg = g ? it.H1 : it.H0, Hn = ni < p.items ? (g ? nx.H1 : nx.H0) : 0;
-                const int nsteps = ni < p.items ? min(nx.H, 2) : 0;
+            int turn = 0, tile = 0, done = 0;      // done: QK steps of `it` issued already
+            bool have = next_item(turn, it);
+            while (have && ok) {
+                ++turn;
+                const bool more = next_item(turn, nx);
+                const int ntile = tile + (it.H + 1) / 2;
+                const int Hg = g ? it.H1 : it.H0, Hn = more ? (g ? nx.H1 : nx.H0) : 0;
+                const int nsteps = more ? min(nx.H, 2) : 0;
                 int ndone = 0;
                 for (; done < min(it.H, 2) && ok; ++done) qk(it, Hg, tile, done);
                 for (int h = 0; h < it.H && ok; ++h) {
@@ -323,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
                     }
                 }
                 it = nx;
-                i = ni;
+                have = more;
                 tile = ntile;
                 done = ndone;
             }
@@ -351,7 +355,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
             if (lane == 0) mbar_arrive(bar(KV_EMPTY + c % kSlots));
             ++c;
         };
-        for (int i = blockIdx.x; i < p.items && ok && p.kv_len; i += gridDim.x) {
+        for (int turn = 0, i; (i = turn_item(turn, p.items)) < p.items && ok && p.kv_len; ++turn) {
             const Item it = item_of(p, i);
             for (int t = 0; t < (it.H + 1) / 2; ++t) {
                 if (!next()) break;                      // K
@@ -382,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
         const float c_log2 = s.scale_log2;
         bool ok = true;
         int n = 0, items = 0, pairs = 0;                 // steps and items of this group, items of two steps or more
-        for (int i = blockIdx.x; i < p.items && ok; i += gridDim.x) {
+        for (int turn = 0, i; (i = turn_item(turn, p.items)) < p.items && ok; ++turn) {
             const Item it = item_of(p, i);
             if (g == 1 && !it.has1) continue;
             const int r0 = it.r0 + g * kRows, r = r0 + (tid & 127);

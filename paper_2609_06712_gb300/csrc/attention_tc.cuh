@@ -13,6 +13,31 @@ namespace rola {
 // rows in 128-byte swizzle: a d-chunk of a tile.  Rows past `rows` read as zero.
 bool encode_rows(CUtensorMap* m, const void* ptr, int64_t rows, int64_t heads, int box_rows);
 
+// dk and dv from D, in one launch (or their parts)
+cudaError_t launch_attention_dkdv_tc(const AttnShape& s, const AttnArgs& a, cudaStream_t st);
+
+// The item of a persistent CTA's turn: turns of gridDim.x items run forwards and backwards in turn, so that with
+// items sorted by length (causal: the longest first) the CTAs' sums stay close; items or more when there is none.
+// (4095 causal rows x 3 shared heads, 8 key heads: dk and dv 343 us in plain turns, 240 so; dq 138 and 118, the
+// forward 140 and 96, with the rows in falling_tile's order.)
+__device__ __forceinline__ int turn_item(int turn, int items)
+{
+    const int base = turn * (int)gridDim.x;
+    if (base >= items) return items;
+    return base + ((turn & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+}
+
+// The j-th of `tiles` row tiles of a key head that `sharing` query heads share, by falling position: a head's rows
+// follow the last head's, and each ends at its last position.  Where the heads do not fill whole tiles the order is
+// off by less than a tile a head, which only the balance feels.
+__device__ __forceinline__ int falling_tile(int j, int tiles, int sharing)
+{
+    const int per = tiles / sharing, rest = tiles - per * sharing;
+    if (j < rest) return tiles - 1 - j;
+    j -= rest;
+    return (j % sharing + 1) * per - 1 - j / sharing;
+}
+
 namespace tc {
 
 // True in one lane of the (converged) warp.
@@ -72,6 +97,20 @@ __device__ __forceinline__ void ffma2(float& a, float& b, float m, float c)
     asm("{\n.reg .b64 ra, rm, rc;\nmov.b64 ra, {%0, %1};\nmov.b64 rm, {%2, %2};\nmov.b64 rc, {%3, %3};\n"
         "fma.rn.f32x2 ra, ra, rm, rc;\nmov.b64 {%0, %1}, ra;\n}\n"
         : "+f"(a), "+f"(b) : "f"(m), "f"(c));
+}
+// (a, b) = (a * m + c, b * m + d)
+__device__ __forceinline__ void ffma2(float& a, float& b, float m, float c, float d)
+{
+    asm("{\n.reg .b64 ra, rm, rc;\nmov.b64 ra, {%0, %1};\nmov.b64 rm, {%2, %2};\nmov.b64 rc, {%3, %4};\n"
+        "fma.rn.f32x2 ra, ra, rm, rc;\nmov.b64 {%0, %1}, ra;\n}\n"
+        : "+f"(a), "+f"(b) : "f"(m), "f"(c), "f"(d));
+}
+// (a, b) = ((a + c) * p, (b + d) * q)
+__device__ __forceinline__ void fadd_mul2(float& a, float& b, float c, float d, float p, float q)
+{
+    asm("{\n.reg .b64 ra, rc, rp;\nmov.b64 ra, {%0, %1};\nmov.b64 rc, {%2, %3};\nmov.b64 rp, {%4, %5};\n"
+        "add.rn.f32x2 ra, ra, rc;\nmul.rn.f32x2 ra, ra, rp;\nmov.b64 {%0, %1}, ra;\n}\n"
+        : "+f"(a), "+f"(b) : "f"(c), "f"(d), "f"(p), "f"(q));
 }
 __device__ __forceinline__ void fadd2(float& a, float& b, float p, float q)
 {
