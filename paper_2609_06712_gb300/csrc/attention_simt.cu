@@ -203,19 +203,40 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttnShape s, 
     if (a.lse && lane == 0) a.lse[row] = l > 0.0f ? top + logf(l) : -INFINITY;
 }
 
-// D = rowsum(dO o), one warp per row
+__device__ __forceinline__ void load8(const float* p, float (&x)[8])
+{
+    const float4 a = load4(p), b = load4(p + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8])
+{
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                        // a bf16 is the upper half of the fp32 of its value
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+
+// D = rowsum(dO o), 16 lanes per row, 8 elements each (bf16: 16-byte loads).
 template <typename T>
 __global__ void __launch_bounds__(256) attention_rowdot_kernel(long long rows, const T* __restrict__ dO,
                                                                const T* __restrict__ o, float* __restrict__ D)
 {
-    const int lane = threadIdx.x % 32;
-    const long long row = (long long)blockIdx.x * 8 + threadIdx.x / 32;
-    if (row >= rows) return;
-    const float4 x = load4(dO + row * kDh + lane * 4), y = load4(o + row * kDh + lane * 4);
-    float d = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, x.w * y.w)));
+    const int lane = threadIdx.x % 16;
+    const long long row = (long long)blockIdx.x * 16 + threadIdx.x / 16;
+    float d = 0.0f;
+    if (row < rows) {
+        float x[8], y[8];
+        load8(dO + row * kDh + lane * 8, x);
+        load8(o + row * kDh + lane * 8, y);
 #pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) d += __shfl_xor_sync(0xffffffffu, d, off);
-    if (lane == 0) D[row] = d;
+        for (int e = 0; e < 8; ++e) d = fmaf(x[e], y[e], d);
+    }
+#pragma unroll
+    for (int off = 8; off >= 1; off >>= 1) d += __shfl_xor_sync(0xffffffffu, d, off);
+    if (lane == 0 && row < rows) D[row] = d;
 }
 
 // p and ds of the tile at (rows r0 + .., keys k0 + ..) for this thread's 4 x 4 places; 0 where the row
@@ -363,7 +384,7 @@ template <typename T>
 cudaError_t launch_attention_rowdot(const AttnShape& s, const AttnArgs& a, cudaStream_t st)
 {
     const long long rows = (long long)s.heads * s.R;
-    attention_rowdot_kernel<T><<<(unsigned)((rows + 7) / 8), 256, 0, st>>>(rows, static_cast<const T*>(a.dO),
+    attention_rowdot_kernel<T><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>(rows, static_cast<const T*>(a.dO),
                                                                            static_cast<const T*>(a.o_in), a.D);
     return cudaGetLastError();
 }
