@@ -1,7 +1,7 @@
 // The gated feed-forward's products for few tokens (bf16 operands, tcgen05):
 // every weight is read once for all of them, and that is what bounds the work
 // (one token at widths 5120 x 13824: 425 MB of weights, 63 us at the measured
-// 6.8 TB/s; its 0.4 GFLOP are nothing).  More than 96 tokens go in tiles of at most
+// 6.8 TB/s, and 72 measured; its 0.4 GFLOP are nothing).  More than 96 tokens go in tiles of at most
 // 96 side by side, which read the weights from L2.
 //
 // The tokens are the N axis and 128 weight rows the M axis of the tensor core,
@@ -25,6 +25,8 @@
 //
 // Warps (192 threads): 0 TMA, 1 products and TMEM, 2-5 epilogue.  Every mbarrier
 // wait is bounded; all threads reach the cluster barriers whatever happens.
+#include <algorithm>
+
 #include "block_ops.cuh"
 #include "tcgen05.cuh"
 #include "tma_2d.cuh"
@@ -85,10 +87,10 @@ __device__ __forceinline__ uint32_t peer(uint32_t local, uint32_t rank)
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(a) : "r"(local), "r"(rank));
     return a;
 }
-__device__ __forceinline__ float ld_peer(uint32_t addr)
+__device__ __forceinline__ float4 ld_peer(uint32_t addr)
 {
-    float x;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(x) : "r"(addr));
+    float4 x;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(addr));
     return x;
 }
 
@@ -239,55 +241,68 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_few_kernel(const __grid_const
     cluster_sync();
     fence_after_sync();
     if (warp == 1) tmem_dealloc(tmem, 128 * ACCS);
-    if (warp >= 2) {
-        const int row = (warp & 3) * 32 + lane, f = tile * kTileM + row;
-        const int m0 = tokens * rank / s, m1 = tokens * (rank + 1) / s;
-        uint32_t from[kMaxCluster];
+    // a warp per token of this CTA's share, four neighbouring features a lane (d_model and d_ff are multiples of 8).
+    // (A feature a lane and the tokens one after another on four warps, each a round trip to the peers:
+    // their gradients of 77 tokens at widths 1536 x 4096 15.3 and 18.5 us, 10.1 and 13.8 so.)
+    const int f = tile * kTileM + lane * 4, m1 = tokens * (rank + 1) / s;
+    for (int m = tokens * rank / s + warp; m < m1 && f < p.rows; m += kThreads / 32) {
+        // all parts are on their way before the first is added
+        float4 part[ACCS][kMaxCluster];
 #pragma unroll
-        for (int r = 0; r < kMaxCluster; ++r) from[r] = r < s ? peer(sbase + (uint32_t)row * 4, r) : 0;
-        for (int m = m0; m < m1; ++m) {
-            // all parts are on their way before the first is added
-            float part[ACCS][kMaxCluster];
+        for (int acc = 0; acc < ACCS; ++acc)
 #pragma unroll
-            for (int acc = 0; acc < ACCS; ++acc)
+            for (int r = 0; r < kMaxCluster; ++r)
+                part[acc][r] = r < s ? ld_peer(peer(sbase + (uint32_t)((acc * p.nt + m) * kTileM + lane * 4) * 4, r))
+                                     : make_float4(0.f, 0.f, 0.f, 0.f);
+        auto sum = [&](int acc, float (&x)[4]) {
+            x[0] = part[acc][0].x; x[1] = part[acc][0].y; x[2] = part[acc][0].z; x[3] = part[acc][0].w;
 #pragma unroll
-                for (int r = 0; r < kMaxCluster; ++r)
-                    part[acc][r] = r < s ? ld_peer(from[r] + (uint32_t)((acc * p.nt + m) * kTileM) * 4) : 0.0f;
-            auto sum = [&](int acc) {
-                float x = part[acc][0];
-#pragma unroll
-                for (int r = 1; r < kMaxCluster; ++r) x += part[acc][r];
-                return x;
-            };
-            const float x = sum(0);
-            const size_t at = (size_t)(first_token + m) * p.rows + f;
-            if constexpr (MODE == kUp) {
-                const float u = sum(1);
-                if (f < p.rows) {
-                    float a = 0.0f;
-                    with_act(p.act, [&](auto act) { a = act.phi(x); });
-                    p.c0[at] = __float2bfloat16_rn(a * u);
-                    if (p.G) {
-                        p.G[at] = x;
-                        p.U[at] = u;
-                    }
-                }
-            } else if (f < p.rows) {
-                if constexpr (MODE == kGrad) {
-                    float a = 0.0f, da = 0.0f;
-                    with_act(p.act, [&](auto act) { act.grad(p.G[at], a, da); });
-                    const float u = p.U[at];
-                    p.c0[at] = __float2bfloat16_rn(a * u);
-                    p.c1[at] = __float2bfloat16_rn(x * u * da);
-                    p.c2[at] = __float2bfloat16_rn(x * a);
-                } else {
-                    p.c0[at] = __float2bfloat16_rn(x);
-                }
+            for (int r = 1; r < kMaxCluster; ++r) {
+                x[0] += part[acc][r].x; x[1] += part[acc][r].y; x[2] += part[acc][r].z; x[3] += part[acc][r].w;
             }
+        };
+        float x[4];
+        sum(0, x);
+        const size_t at = (size_t)(first_token + m) * p.rows + f;
+        if constexpr (MODE == kUp) {
+            float u[4], h[4];
+            sum(1, u);
+            with_act(p.act, [&](auto act) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[e] = act.phi(x[e]) * u[e];
+            });
+            store4(p.c0 + at, make_float4(h[0], h[1], h[2], h[3]));
+            if (p.G) {
+                *reinterpret_cast<float4*>(p.G + at) = make_float4(x[0], x[1], x[2], x[3]);
+                *reinterpret_cast<float4*>(p.U + at) = make_float4(u[0], u[1], u[2], u[3]);
+            }
+        } else if constexpr (MODE == kGrad) {
+            const float4 gv = *reinterpret_cast<const float4*>(p.G + at), uv = *reinterpret_cast<const float4*>(p.U + at);
+            const float g[4] = {gv.x, gv.y, gv.z, gv.w}, u[4] = {uv.x, uv.y, uv.z, uv.w};
+            float h[4], dg[4], du[4];
+            with_act(p.act, [&](auto act) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float a = 0.0f, da = 0.0f;
+                    act.grad(g[e], a, da);
+                    h[e] = a * u[e];
+                    dg[e] = x[e] * u[e] * da;
+                    du[e] = x[e] * a;
+                }
+            });
+            store4(p.c0 + at, make_float4(h[0], h[1], h[2], h[3]));
+            store4(p.c1 + at, make_float4(dg[0], dg[1], dg[2], dg[3]));
+            store4(p.c2 + at, make_float4(du[0], du[1], du[2], du[3]));
+        } else {
+            store4(p.c0 + at, make_float4(x[0], x[1], x[2], x[3]));
         }
     }
     cluster_sync();                                      // the peers' shared memory stays until all have read it
 }
+
+// Stands for the kernels below where the occupancy is asked for: of one that allocates tensor memory the runtime
+// counts one CTA an SM, however little it allocates.
+__global__ void __launch_bounds__(kThreads, 2) like_ffn_few_kernel() {}
 
 // ---------------------------------------------------------------- host side
 
@@ -306,12 +321,7 @@ cudaError_t launch(const FfnShape& s, Params& p, bool dependent, DeviceStatus* s
     p.wait_limit_ns = s.wait_limit_ns;
     p.skip_first = s.debug_flags & ROLA_DEBUG_SKIP_FIRST_K_COPY ? 1 : 0;
     const int tiles = (p.rows + kTileM - 1) / kTileM, total = p.k_steps * p.sources;
-    // as many CTAs as two per SM hold, each with two K steps at least
     const int token_tiles = (s.M + p.nt - 1) / p.nt;
-    int cluster = 304 / (tiles * token_tiles);
-    if (cluster > total / 2) cluster = total / 2;
-    if (cluster > kMaxCluster) cluster = kMaxCluster;
-    if (cluster < 1) cluster = 1;
     p.stage_bytes = ACCS * kABytes + p.nt * kStepK * 2;
     p.stages = (int)((kSmemBudget - sizeof(Ctrl)) / p.stage_bytes);
     if (p.stages > kMaxStages) p.stages = kMaxStages;
@@ -323,18 +333,36 @@ cudaError_t launch(const FfnShape& s, Params& p, bool dependent, DeviceStatus* s
     auto kernel = ffn_few_kernel<MODE>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
+    // As many CTAs as two per SM hold, each with two K steps at least, and with twice the weights of the sums that
+    // it takes from its peers (77 tokens at widths 1536 x 4096: 24.7 us, 26.9 with 8 CTAs a tile in the up products).
+    int cluster = 304 / (tiles * token_tiles);
+    cluster = std::min(std::min(cluster, kMaxCluster), std::min(total / 2, total * 16 / p.nt));
+    cluster = std::max(cluster, 1);
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(tiles * cluster, token_tiles);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = cluster;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
+    cfg.numAttrs = 1;
+    // A cluster's CTAs share a GPC, and not every size fills its SMs: 38 clusters of 7 are in flight at once, 46 of 6.
+    // A few tiles left for a second wave cost a whole one (one token at 5120 x 13824, whose 40 down tiles
+    // would take 7: 87 us, with 6 72).
+    e = cudaFuncSetAttribute(like_ffn_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    for (;; --cluster) {
+        at[0].val.clusterDim.x = cluster;
+        cfg.gridDim = dim3(tiles * cluster, token_tiles);
+        if (cluster == 1) break;
+        int fit = 0;
+        e = cudaOccupancyMaxActiveClusters(&fit, like_ffn_few_kernel, &cfg);
+        if (e != cudaSuccess) return e;
+        if (fit >= tiles * token_tiles) break;
+    }
     cfg.numAttrs = dependent ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
