@@ -28,6 +28,7 @@
 #include <algorithm>
 
 #include "block_ops.cuh"
+#include "cluster.cuh"
 #include "tcgen05.cuh"
 #include "tma_2d.cuh"
 
@@ -63,36 +64,6 @@ struct Params {
     DeviceStatus* status;
     uint64_t wait_limit_ns;
 };
-
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_size()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;\n" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;\n" ::: "memory");
-}
-// The address of `local` in the shared memory of CTA `rank` of the cluster, and a load from there.
-__device__ __forceinline__ uint32_t peer(uint32_t local, uint32_t rank)
-{
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(a) : "r"(local), "r"(rank));
-    return a;
-}
-__device__ __forceinline__ float4 ld_peer(uint32_t addr)
-{
-    float4 x;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(addr));
-    return x;
-}
 
 template <int MODE>
 __global__ void __launch_bounds__(kThreads, 2) ffn_few_kernel(const __grid_constant__ Params p)

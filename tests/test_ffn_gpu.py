@@ -127,6 +127,14 @@ def test_every_small_token_count_at_a_long_width(rl, m):
     check("silu", X, Wg, Wu, Wd, run(rl, "silu", X, Wg, Wu, Wd))
 
 
+@pytest.mark.parametrize("m,d,f", [(33, 64, 128), (40, 136, 2056), (94, 328, 1032), (129, 72, 3000), (300, 1544, 64)])
+def test_fp32_products_of_few_tiles_and_a_long_axis(rl, m, d, f):
+    """Tiles whose K axis several CTAs share, by 2 to 8, the last rows and columns of a tile empty."""
+    X, Wg, Wu, Wd, dY = inputs_of(m, d, f, torch.float32, seed=m)
+    check("silu", X, Wg, Wu, Wd, run(rl, "silu", X, Wg, Wu, Wd, dY), dY)
+    assert all(torch.equal(s, t) for s, t in zip(run(rl, "gelu", X, Wg, Wu, Wd, dY), run(rl, "gelu", X, Wg, Wu, Wd, dY)))
+
+
 def test_large_gates_stay_finite(rl):
     """Gates of +-300: phi's exponential over- and underflows, the products do not."""
     for dt in DTYPES.values():
