@@ -17,7 +17,7 @@
 // Where the tiles leave most SMs idle (94 tokens at d_model 1360: 11 tiles for dX)
 // the K axis of a tile is split over a cluster of up to 8 CTAs, whose parts meet in
 // their shared memory and are added in rank order, each CTA a share of the rows.
-// (94 tokens at widths 1360 x 8120, a training pass: 3889 us without, 847 with.)
+// (94 tokens at widths 1360 x 8120, a training pass: 3889 us without, 805 with.)
 //
 // Up to 32 tokens that tile would be mostly empty rows, and the weights are what
 // has to be read.  Then a warp takes whole weight rows against 8 tokens (up and
@@ -129,6 +129,13 @@ __device__ __forceinline__ void finish(const Args& p, int m, int n, float4 c, fl
     }
 }
 
+// acc += a b for a pair of b, each an IEEE fma: one instruction of two leaves issue slots to the loads from
+// shared memory (2048 tokens at widths 1536 x 4096: 1980 us with one fma an instruction, 1790 so; 43 TFLOP/s).
+__device__ __forceinline__ void fma_pair(unsigned long long& acc, float a, unsigned long long b)
+{
+    asm("{\n.reg .b64 aa;\nmov.b64 aa, {%1, %1};\nfma.rn.f32x2 %0, aa, %2, %0;\n}\n" : "+l"(acc) : "f"(a), "l"(b));
+}
+
 constexpr size_t kStageBytes = 2 * 2 * kStep * kPad * 4, kSumBytes = (size_t)kTile * kPad * 4;
 
 // SPLIT: the grid's z axis is a cluster that shares the K axis of a tile; its shared memory holds kSumBytes.
@@ -143,7 +150,7 @@ __global__ void __launch_bounds__(256, 2) simt_gemm_kernel(Operand a0, Operand b
     constexpr int kColumns = E == kGateUp ? 64 : kTile;
     const int m0 = blockIdx.y * kTile, n0 = blockIdx.x * kColumns;
     const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-    float acc[8][8] = {};
+    unsigned long long sum[8][4] = {};                 // pairs of neighbouring columns
     const int steps = (p.K + kStep - 1) / kStep;
     int begin = 0, end = steps * p.sources;
     if constexpr (SPLIT) {
@@ -167,15 +174,18 @@ __global__ void __launch_bounds__(256, 2) simt_gemm_kernel(Operand a0, Operand b
         const int cur = (s - begin) & 1;
 #pragma unroll
         for (int k = 0; k < kStep; ++k) {
-            float a[8], b[8];
+            float a[8];
             *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(&as[cur][k][ty * 4]);
             *reinterpret_cast<float4*>(a + 4) = *reinterpret_cast<const float4*>(&as[cur][k][64 + ty * 4]);
-            *reinterpret_cast<float4*>(b) = *reinterpret_cast<const float4*>(&bs[cur][k][tx * 4]);
-            *reinterpret_cast<float4*>(b + 4) = *reinterpret_cast<const float4*>(&bs[cur][k][64 + tx * 4]);
+            const ulonglong2 b0 = *reinterpret_cast<const ulonglong2*>(&bs[cur][k][tx * 4]);
+            const ulonglong2 b1 = *reinterpret_cast<const ulonglong2*>(&bs[cur][k][64 + tx * 4]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+            for (int i = 0; i < 8; ++i) {
+                fma_pair(sum[i][0], a[i], b0.x);
+                fma_pair(sum[i][1], a[i], b0.y);
+                fma_pair(sum[i][2], a[i], b1.x);
+                fma_pair(sum[i][3], a[i], b1.y);
+            }
         }
         if (s + 1 < end) {
             stage<AK>(as[cur ^ 1], xa);                // last read before the previous barrier
@@ -183,6 +193,12 @@ __global__ void __launch_bounds__(256, 2) simt_gemm_kernel(Operand a0, Operand b
         }
         __syncthreads();
     }
+    float acc[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(acc[i][2 * j]), "=f"(acc[i][2 * j + 1]) : "l"(sum[i][j]));
     if constexpr (SPLIT) {
         // this CTA's part of the tile into shared memory, over the stages, which all have read
 #pragma unroll
@@ -194,7 +210,7 @@ __global__ void __launch_bounds__(256, 2) simt_gemm_kernel(Operand a0, Operand b
         cluster_sync();
         const int parts = gridDim.z, rank = blockIdx.z;
         const uint32_t base = (uint32_t)__cvta_generic_to_shared(sm);
-        auto sum = [&](int row, int column) {
+        auto total = [&](int row, int column) {
             const uint32_t at = base + (uint32_t)(row * kPad + column) * 4;
             float4 c = ld_peer(peer(at, 0));
             for (int r = 1; r < parts; ++r) {
@@ -207,8 +223,8 @@ __global__ void __launch_bounds__(256, 2) simt_gemm_kernel(Operand a0, Operand b
         const int row1 = kTile * (rank + 1) / parts, column = (int)threadIdx.x % kLanes * 4;
         for (int row = kTile * rank / parts + (int)threadIdx.x / kLanes; row < row1; row += 256 / kLanes) {
             if (m0 + row >= p.M) break;
-            const float4 c = sum(row, column);
-            finish<E>(p, m0 + row, n0 + column, c, E == kGateUp ? sum(row, 64 + column) : c);
+            const float4 c = total(row, column);
+            finish<E>(p, m0 + row, n0 + column, c, E == kGateUp ? total(row, 64 + column) : c);
         }
         cluster_sync();                                // the peers' shared memory stays until all have read it
     } else {
