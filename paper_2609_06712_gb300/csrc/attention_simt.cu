@@ -219,24 +219,35 @@ __device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8])
     }
 }
 
-// D = rowsum(dO o), 16 lanes per row, 8 elements each (bf16: 16-byte loads).
+// D = rowsum(dO o), 16 lanes per row, 8 elements each (bf16: 16-byte loads), two rows on their way at once.
+// Bound by HBM (196560 rows: 101 MB in 21 us; one row at a time 25).
 template <typename T>
 __global__ void __launch_bounds__(256) attention_rowdot_kernel(long long rows, const T* __restrict__ dO,
                                                                const T* __restrict__ o, float* __restrict__ D)
 {
+    constexpr int kEach = 2;
     const int lane = threadIdx.x % 16;
-    const long long row = (long long)blockIdx.x * 16 + threadIdx.x / 16;
-    float d = 0.0f;
-    if (row < rows) {
-        float x[8], y[8];
-        load8(dO + row * kDh + lane * 8, x);
-        load8(o + row * kDh + lane * 8, y);
+    const long long row0 = (long long)blockIdx.x * (16 * kEach) + threadIdx.x / 16;
+    float x[kEach][8], y[kEach][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d = fmaf(x[e], y[e], d);
+    for (int i = 0; i < kEach; ++i) {
+        const long long row = row0 + 16 * i;
+        if (row >= rows) continue;
+        load8(dO + row * kDh + lane * 8, x[i]);
+        load8(o + row * kDh + lane * 8, y[i]);
     }
 #pragma unroll
-    for (int off = 8; off >= 1; off >>= 1) d += __shfl_xor_sync(0xffffffffu, d, off);
-    if (lane == 0 && row < rows) D[row] = d;
+    for (int i = 0; i < kEach; ++i) {
+        const long long row = row0 + 16 * i;
+        float d = 0.0f;
+        if (row < rows) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d = fmaf(x[i][e], y[i][e], d);
+        }
+#pragma unroll
+        for (int off = 8; off >= 1; off >>= 1) d += __shfl_xor_sync(0xffffffffu, d, off);
+        if (lane == 0 && row < rows) D[row] = d;
+    }
 }
 
 // p and ds of the tile at (rows r0 + .., keys k0 + ..) for this thread's 4 x 4 places; 0 where the row
@@ -384,7 +395,7 @@ template <typename T>
 cudaError_t launch_attention_rowdot(const AttnShape& s, const AttnArgs& a, cudaStream_t st)
 {
     const long long rows = (long long)s.heads * s.R;
-    attention_rowdot_kernel<T><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>(rows, static_cast<const T*>(a.dO),
+    attention_rowdot_kernel<T><<<(unsigned)((rows + 31) / 32), 256, 0, st>>>(rows, static_cast<const T*>(a.dO),
                                                                            static_cast<const T*>(a.o_in), a.D);
     return cudaGetLastError();
 }
