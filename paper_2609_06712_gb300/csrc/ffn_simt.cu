@@ -14,18 +14,15 @@
 // features (columns tx*4 .. and 64 + tx*4 ..) and phi and the product need no
 // exchange.  Bound by fp32 FMA issue.
 //
-// Where the tiles leave most SMs idle (94 tokens at d_model 1360: 11 tiles for dX)
+// Where the tiles leave SMs idle (94 tokens at d_model 1360: 11 tiles for dX)
 // the K axis of a tile is split over a cluster of up to 8 CTAs, whose parts meet in
 // their shared memory and are added in rank order, each CTA a share of the rows.
-// (94 tokens at widths 1360 x 8120, a training pass: 3889 us without, 805 with.)
 //
 // Up to 32 tokens that tile would be mostly empty rows, and the weights are what
 // has to be read.  Then a warp takes whole weight rows against 8 tokens (up and
 // down, whose weights lie along k), or a CTA 64 weight columns against 8 tokens, its 32
 // warps sharing the K axis (dH and dX, whose weights lie across it); the parts
 // meet in a fixed order.
-#include <algorithm>
-
 #include "block_ops.cuh"
 #include "cluster.cuh"
 
@@ -130,7 +127,7 @@ __device__ __forceinline__ void finish(const Args& p, int m, int n, float4 c, fl
 }
 
 // acc += a b for a pair of b, each an IEEE fma: one instruction of two leaves issue slots to the loads from
-// shared memory (2048 tokens at widths 1536 x 4096: 1980 us with one fma an instruction, 1790 so; 43 TFLOP/s).
+// shared memory (2048 tokens at widths 1536 x 4096: 1980 us with one fma an instruction, 1790 so, both in one part a tile).
 __device__ __forceinline__ void fma_pair(unsigned long long& acc, float a, unsigned long long b)
 {
     asm("{\n.reg .b64 aa;\nmov.b64 aa, {%1, %1};\nfma.rn.f32x2 %0, aa, %2, %0;\n}\n" : "+l"(acc) : "f"(a), "l"(b));
@@ -378,6 +375,22 @@ cudaError_t few_columns(Operand a0, Operand b0, Operand a1, Operand b1, const Ar
     return cudaGetLastError();
 }
 
+// Parts of a tile's K axis of `total` steps, 1, 2, 4 or 8 (the sizes of cluster that fill the SMs best), each of three steps at
+// least: those of least cost in steps.  The SM with the most CTAs has n of them, two at a time; one alone takes
+// 0.65 of the time of two, and the exchange of the parts about two steps.  (Few tiles: 94 tokens at widths 1360 x 8120, training,
+// 3889 us in one part, 805 so.  A last turn of few CTAs: 2048 tokens at 1536 x 4096, 1790 us in one part, 1540 so.)
+int parts_of(int64_t tiles, int64_t total)
+{
+    auto cost = [&](int64_t parts) {
+        const int64_t n = (tiles * parts + 151) / 152;
+        return ((double)(n / 2) + (n % 2 ? 0.65 : 0.0)) * ((double)total / (double)parts + (parts > 1 ? 2.0 : 0.0));
+    };
+    int best = 1;
+    for (int parts = 2; parts <= 8 && total >= 3 * parts; parts *= 2)
+        if (cost(parts) < cost(best)) best = parts;
+    return best;
+}
+
 template <bool AK, bool BK, int E>
 cudaError_t gemm(Operand a0, Operand b0, Operand a1, Operand b1, const Args& p, cudaStream_t st)
 {
@@ -387,9 +400,7 @@ cudaError_t gemm(Operand a0, Operand b0, Operand a1, Operand b1, const Args& p, 
     }
     const int nt = E == kGateUp ? 64 : kTile;
     const dim3 grid((p.N + nt - 1) / nt, (p.M + kTile - 1) / kTile);
-    // as many parts as two CTAs an SM hold, each of four K steps at least
-    const int64_t tiles = (int64_t)grid.x * grid.y, total = (int64_t)(p.K + kStep - 1) / kStep * p.sources;
-    const int parts = (int)std::min<int64_t>(std::min<int64_t>(304 / tiles, total / 4), 8);
+    const int parts = parts_of((int64_t)grid.x * grid.y, (int64_t)((p.K + kStep - 1) / kStep) * p.sources);
     if (parts < 2) {
         simt_gemm_kernel<AK, BK, E, false><<<grid, 256, kStageBytes, st>>>(a0, b0, a1, b1, p);
         return cudaGetLastError();
