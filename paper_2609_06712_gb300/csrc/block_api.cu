@@ -347,10 +347,10 @@ rola_status_t rola_attention_backward(const rola_attention_config_t* cfg, const 
     a.D = at<float>(ws, w.D);
     a.part_dq = at<float>(ws, w.part_dq); a.part_dk = at<float>(ws, w.part_dk); a.part_dv = at<float>(ws, w.part_dv);
     a.status = at<DeviceStatus>(ws, w.status);
-    ROLA_TRY(cudaMemsetAsync(a.status, 0, sizeof(DeviceStatus), st));
     if (cfg->dtype == ROLA_BF16) {
-        // over one stage of keys the dq kernel forms D itself
+        // the row sums' kernel clears the status too; over one stage of keys the dq kernel forms D itself
         if (s.Lk > 128) ROLA_TRY(launch_attention_rowdot<__nv_bfloat16>(s, a, st));
+        else ROLA_TRY(cudaMemsetAsync(a.status, 0, sizeof(DeviceStatus), st));
         ROLA_TRY(launch_attention_backward_tc(s, a, st));
     } else {
         ROLA_TRY(launch_attention_rowdot<float>(s, a, st));
