@@ -28,6 +28,10 @@
 // Keys past the length: their scores are replaced by -inf whatever they are, and
 // their rows of V are zeroed in shared memory (0 x NaN would be NaN).
 //
+// Measured: 40 heads of 75600 rows to 512 keys 684 us (1160 TFLOP/s), 4725 rows to 8192 keys 1440 TFLOP/s; one token, 4
+// x 40 heads on 8, 32760 keys 95 us (5.7 TB/s).  Bound by the tensor pipe, whose 128 x 64 products take 48 cycles instead of
+// 32, and over few keys by the ends of an item (1.6 us); for a single token by HBM.
+//
 // Warps (384 threads, one persistent CTA per SM): 0-3 softmax and epilogue of
 // group 0, 4-7 of group 1, 8 TMA (Q of both groups, and K, V tiles in one ring of
 // five 32 KB slots), 9 and 10 products, 11 the zeroing of V's rows.  Shared memory 64 + 160 KB.  Every mbarrier wait
