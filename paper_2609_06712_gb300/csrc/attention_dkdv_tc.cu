@@ -39,10 +39,11 @@ constexpr uint32_t kABytes = kM * kDh * 2, kBBytes = kN * kDh * 2;        // [d-
 constexpr uint32_t kSmemA = 0, kSmemB = 2 * kABytes, kSmemTiles = kSmemB + kSlots * kBBytes;
 constexpr uint32_t kTmemCols = 512, kTmemS = 0, kTmemP = 128, kTmemV = 256, kTmemK = 384;
 
-// B: a ring of tiles, Q of stage n in use 2n, dO in 2n + 1.  S_FULL .. K_DONE: + g.
+// B: a ring of tiles, Q of stage n in use 2n, dO in 2n + 1.  S_FULL .. K_DONE, COLS: + g.  COLS: a stage's row values
+// are in shared memory (a group's warps meet at no barrier of the CTA, whose wait would have no limit).
 enum Bar { A_FULL = 0, A_EMPTY, B_FULL, B_EMPTY = B_FULL + kSlots, S_FULL = B_EMPTY + kSlots, DP_FULL = S_FULL + 2,
            P_FULL = DP_FULL + 2, DS_FULL = P_FULL + 2, V_DONE = DS_FULL + 2, K_DONE = V_DONE + 2, O_FULL = K_DONE + 2,
-           O_EMPTY, DRAIN, NUM_BARS = DRAIN + 3 };
+           O_EMPTY, COLS, DRAIN = COLS + 2, NUM_BARS = DRAIN + 3 };
 
 struct Cols {                                             // of a stage's rows
     alignas(16) float lse2[kN];
@@ -160,7 +161,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dkdv_tc_kernel(const __
         for (int i = 0; i < NUM_BARS; ++i) {
             int count = 1;
             if (i == A_EMPTY || (i >= B_EMPTY && i < B_EMPTY + kSlots)) count = 2;      // two issuing threads
-            if (i >= P_FULL && i < V_DONE) count = 4;                                   // a group's warps
+            if ((i >= P_FULL && i < V_DONE) || (i >= COLS && i < DRAIN)) count = 4;     // a group's warps
             if (i == O_EMPTY) count = 8;
             mbar_init(bar(i), count);
         }
@@ -331,11 +332,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dkdv_tc_kernel(const __
                 } else {
                     cols.neg_D[gt - 64] = val;
                 }
-                bar_sync(1 + g, 128);                     // (the group's stage before last has been read)
+                // a buffer is written again two stages on, past the next stage's COLS, for which every warp has read this one
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(COLS + g));
                 fetch(it.next(s, nt + 1));                // on their way under this stage's work
                 const int r0 = t * kN, r1 = min(r0 + kN, s.R) - 1;
                 const bool whole = it.x0 + kM <= attn_seen_least(s, it.len, r0, r1);
-                if (!wait(S_FULL + g, k)) break;
+                if (!wait(S_FULL + g, k) || !wait(COLS + g, k)) break;
                 fence_after_sync();
                 float pr[64];
                 // p of 32 rows from their scores; `masked`: some row does not see all of the item's keys

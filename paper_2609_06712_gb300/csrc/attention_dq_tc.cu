@@ -46,12 +46,13 @@ constexpr uint32_t kTmemCols = 512;
 
 constexpr uint32_t kTmemS = 0, kTmemP = 256, kTmemAcc = 384;      // S_b at 128 b
 
-// B: a ring of tiles, K of stage n in use 2n, V in 2n + 1.  READ: dP is in registers; S_FULL, DONE: + b.
+// B: a ring of tiles, K of stage n in use 2n, V in 2n + 1.  READ: dP is in registers; S_FULL, DONE: + b; D_FULL: the
+// groups' parts of D are in shared memory (the warps meet at no barrier of the CTA, whose wait would have no limit).
 enum Bar { A_FULL = 0, A_EMPTY, B_FULL, B_EMPTY = B_FULL + kSlots, S_FULL = B_EMPTY + kSlots, DP_FULL = S_FULL + 2, READ,
-           DS_FULL, DONE, O_FULL = DONE + 2, O_EMPTY, CUT, DRAIN = CUT + 4, NUM_BARS = DRAIN + 2 };
+           DS_FULL, DONE, O_FULL = DONE + 2, O_EMPTY, D_FULL, CUT, DRAIN = CUT + 4, NUM_BARS = DRAIN + 2 };
 
 struct Ctrl {
-    float D[2][kM];                                       // the groups' parts of D
+    float D[2][2][kM];                                    // the groups' parts of D, [single-stage item & 1][group]
     uint64_t bar[NUM_BARS];
     uint32_t tmem_base;
     int abort;
@@ -149,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dq_tc_kernel(const __gr
     if (tid == 0) {
         sm.abort = 0;
         for (int i = 0; i < NUM_BARS; ++i) {
-            const bool groups = i == READ || i == DS_FULL || i == O_EMPTY;
+            const bool groups = i == READ || i == DS_FULL || i == O_EMPTY || i == D_FULL;
             // a tile is followed by the zeroing warp too where there is work for it
             const bool two = i >= B_EMPTY && i < B_EMPTY + kSlots && p.kv_len;
             mbar_init(bar(i), groups ? 8 : (two ? 2 : 1));
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dq_tc_kernel(const __gr
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(b));
         };
-        int n = 0, items = 0;
+        int n = 0, items = 0, singles = 0;                // singles: items of one stage
         for (int turn = 0, i; (i = turn_item(turn, p.items)) < p.items && ok; ++turn) {
             const Item it(p, i);
             const int x = it.x0 + gt;                     // this thread's row
@@ -366,11 +367,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dq_tc_kernel(const __gr
                             if (q1 != 0.0f) d1 = fmaf(q1, dp[j + 1], d1);
                         }
                     }
-                    sm.D[g][gt] = d0 + d1;
-                    bar_sync(1, 256);
-                    D = sm.D[0][gt] + sm.D[1][gt];
+                    // a buffer is written again two such items on, past the next one's D_FULL, for which every
+                    // warp has read this one
+                    float (&part)[2][kM] = sm.D[singles & 1];
+                    part[g][gt] = d0 + d1;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(D_FULL));
+                    if (!wait(D_FULL, singles)) break;
+                    ++singles;
+                    D = part[0][gt] + part[1][gt];
                     if (in && g == 0) p.D[rows + x] = D;
-                    bar_sync(1, 256);                 // read before the next item's are written
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {

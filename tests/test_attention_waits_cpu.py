@@ -1,0 +1,98 @@
+"""The waits between the warps of the dense attention's tensor-core kernels, on the CPU: a model of their mbarriers run
+under random schedules, and what the sources must hold for the model to be theirs.
+
+An mbarrier counts the phases it has completed; a wait for use u of it passes while that number's parity differs from
+u's.  A run is stuck if no actor can go on and not all are done.
+"""
+import os
+import random
+import re
+
+import pytest
+
+from conftest import ROOT
+
+CSRC = os.path.join(ROOT, "paper_2609_06712_gb300", "csrc")
+KERNELS = ["attention_tc.cu", "attention_dq_tc.cu", "attention_dkdv_tc.cu"]
+
+
+class Bar:
+    def __init__(self, count=1):
+        self.count, self.left, self.phases = count, count, 0
+
+    def arrive(self):
+        self.left -= 1
+        if self.left == 0:
+            self.left, self.phases = self.count, self.phases + 1
+
+    def passed(self, use):
+        return (self.phases & 1) != (use & 1)
+
+
+def run(actors, rng):
+    """Actors yield conditions.  Runs them in a random order with random pauses; True if all came to their end."""
+    waiting = [(a, next(a, None)) for a in actors]
+    waiting = [(a, c) for a, c in waiting if c is not None]
+    weight = [rng.choice([1, 1, 4, 30]) for _ in actors]         # some actors far slower than others
+    while waiting:
+        ready = [i for i, (_, c) in enumerate(waiting) if c()]
+        if not ready:
+            return False
+        i = rng.choices(ready, [1 / weight[j % len(weight)] for j in ready])[0]
+        a, _ = waiting[i]
+        c = next(a, None)
+        if c is None:
+            waiting.pop(i)
+        else:
+            waiting[i] = (a, c)
+    return True
+
+
+def source(name):
+    with open(os.path.join(CSRC, name)) as f:
+        return re.sub(r"//.*", "", f.read())
+
+
+# ---------------------------------------------------------------- a wait that gives up
+
+def leaves(barrier, rng):
+    """Four warps through stages of (meet the others, wait for a product), while waits give up from some moment on:
+    a wait whose phase is complete passes all the same.  barrier: they meet at a barrier of the CTA, which has no
+    limit; else at an mbarrier whose wait is one like the others."""
+    stages = 4
+    meet, product, abort, arrived = Bar(4), [Bar() for _ in range(stages)], [], [0]
+
+    def issuer():
+        for k in range(stages):
+            if k == 2:
+                abort.append(1)              # what comes now is late: some waits have given up, some see it complete
+            yield lambda: True
+            product[k].arrive()
+
+    def warp():
+        for k in range(stages):
+            if barrier:
+                arrived[0] += 1
+                yield lambda k=k: arrived[0] >= 4 * (k + 1)
+            else:
+                meet.arrive()
+                yield lambda k=k: meet.passed(k) or abort
+                if not meet.passed(k):
+                    return
+            yield lambda k=k: product[k].passed(0) or abort
+            if not product[k].passed(0):
+                return
+    return run([issuer()] + [warp() for _ in range(4)], rng)
+
+
+def test_a_warp_that_gives_up_leaves_no_other_behind():
+    assert all(leaves(False, random.Random(i)) for i in range(400))
+    assert not all(leaves(True, random.Random(i)) for i in range(400)), "the model does not show the fault"
+
+
+@pytest.mark.parametrize("name", KERNELS)
+def test_warps_meet_at_mbarriers_only(name):
+    text = source(name)
+    assert not re.findall(r"\b(bar_sync|bar_red_or|__syncthreads_\w+)\s*\(", text)
+    # before the roles part and after they have ended
+    assert text.count("__syncthreads()") == 2

@@ -1,0 +1,49 @@
+"""The dense attention's gradients when waits run out and when many items follow one another, on the GPU."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def rl():
+    assert torch.cuda.is_available(), "GPU tests need a CUDA device"
+    from paper_2609_06712_gb300 import build
+    build.build()
+    from paper_2609_06712_gb300 import rola
+    return rola
+
+
+def setup(rl, B, H, Hk, Lq, Lk, causal, lens=None):
+    g = torch.Generator().manual_seed(Lq + Lk)
+
+    def rand(*shape):
+        return torch.randn(shape, generator=g).bfloat16().cuda()
+    q, k, v, dO = rand(B, H, Lq, 128), rand(B, Hk, Lk, 128), rand(B, Hk, Lk, 128), rand(B, H, Lq, 128)
+    kv = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    c = rl.make_attention_config(B, H, Hk, Lq, Lk, causal)
+    o, lse, ws = torch.empty_like(q), torch.empty((B, H, Lq), device="cuda"), rl.attention_workspace(c)
+    rl.attention(c, q, k, v, kv, o, lse, ws)
+    assert rl.get_device_status(ws) == rl.ROLA_OK
+    bws = rl.attention_backward_workspace(c)
+
+    def backward():
+        grads = [torch.full_like(t, float("nan")) for t in (q, k, v)]
+        rl.attention_backward(c, q, k, v, kv, o, lse, dO, *grads, bws)
+        return rl.get_device_status(bws), grads
+    return c, backward
+
+
+# one stage of keys (D exchanged between the groups), few and many stages of rows, items of unequal length
+@pytest.mark.parametrize("B,H,Hk,Lq,Lk,causal,lens", [
+    (1, 2, 2, 500, 100, False, None), (2, 2, 1, 300, 70, True, [70, 33]), (1, 2, 2, 64, 500, False, None),
+    (1, 4, 2, 900, 900, True, None), (2, 2, 2, 700, 300, False, [300, 90]), (1, 12, 12, 2100, 129, False, None)])
+def test_gradients_give_up_and_the_next_call_works(rl, B, H, Hk, Lq, Lk, causal, lens):
+    c, backward = setup(rl, B, H, Hk, Lq, Lk, causal, lens)
+    status, want = backward()
+    assert status == rl.ROLA_OK
+    c.wait_limit_ms, c.debug_flags = 20, rl.ROLA_DEBUG_SKIP_FIRST_K_COPY
+    assert backward()[0] == rl.ROLA_ERR_TIMEOUT
+    c.wait_limit_ms, c.debug_flags = 0, 0
+    status, got = backward()
+    assert status == rl.ROLA_OK and all(torch.equal(a, b) for a, b in zip(got, want))
