@@ -46,10 +46,11 @@ constexpr uint32_t kTmemCols = 512;
 
 constexpr uint32_t kTmemS = 0, kTmemP = 256, kTmemAcc = 384;      // S_b at 128 b
 
-// B: a ring of tiles, K of stage n in use 2n, V in 2n + 1.  READ: dP is in registers; S_FULL, DONE: + b; D_FULL: the
+// B: a ring of tiles, K of stage n in use 2n, V in 2n + 1.  READ: dP is in registers; S_FULL, DS_FULL, DONE: + b, since dS of
+// stage n + 1 may be there before the dQ thread has looked for that of stage n; D_FULL: the
 // groups' parts of D are in shared memory (the warps meet at no barrier of the CTA, whose wait would have no limit).
 enum Bar { A_FULL = 0, A_EMPTY, B_FULL, B_EMPTY = B_FULL + kSlots, S_FULL = B_EMPTY + kSlots, DP_FULL = S_FULL + 2, READ,
-           DS_FULL, DONE, O_FULL = DONE + 2, O_EMPTY, D_FULL, CUT, DRAIN = CUT + 4, NUM_BARS = DRAIN + 2 };
+           DS_FULL, DONE = DS_FULL + 2, O_FULL = DONE + 2, O_EMPTY, D_FULL, CUT, DRAIN = CUT + 4, NUM_BARS = DRAIN + 2 };
 
 struct Ctrl {
     float D[2][2][kM];                                    // the groups' parts of D, [single-stage item & 1][group]
@@ -150,7 +151,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dq_tc_kernel(const __gr
     if (tid == 0) {
         sm.abort = 0;
         for (int i = 0; i < NUM_BARS; ++i) {
-            const bool groups = i == READ || i == DS_FULL || i == O_EMPTY || i == D_FULL;
+            const bool groups = i == READ || (i >= DS_FULL && i < DONE) || i == O_EMPTY || i == D_FULL;
             // a tile is followed by the zeroing warp too where there is work for it
             const bool two = i >= B_EMPTY && i < B_EMPTY + kSlots && p.kv_len;
             mbar_init(bar(i), groups ? 8 : (two ? 2 : 1));
@@ -252,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dq_tc_kernel(const __gr
                             wait(CUT + (ncut & 3), ncut >> 2);
                             ++ncut;
                         }
-                        wait(DS_FULL, n);
+                        wait(DS_FULL + (n & 1), n >> 1);
                         if (first && items >= 1) wait(O_EMPTY, items - 1);
                         if (!ok) break;
                         fence_after_sync();
@@ -397,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dq_tc_kernel(const __gr
                     tmem_st16(s_addr + b * 128 + h * 16, *reinterpret_cast<const float(*)[16]>(pk));
                 }
                 tmem_st_wait();
-                arrive(DS_FULL);
+                arrive(DS_FULL + b);
             }
             if (!ok) break;
             // ---- epilogue: group g writes d 64 g .. +63

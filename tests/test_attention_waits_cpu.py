@@ -96,3 +96,61 @@ def test_warps_meet_at_mbarriers_only(name):
     assert not re.findall(r"\b(bar_sync|bar_red_or|__syncthreads_\w+)\s*\(", text)
     # before the roles part and after they have ended
     assert text.count("__syncthreads()") == 2
+
+
+# ---------------------------------------------------------------- the dq kernel's products and element-wise work
+
+def dq_pipeline(pair, rng, stages=12):
+    """The dq kernel's loop over stages, its tiles loaded: S and dP by one actor, dQ by another, two warps between
+    them.  pair: dS is announced on a barrier for each of the two S buffers; else on one for all stages."""
+    S, dP, read, done = [Bar(), Bar()], Bar(), Bar(2), [Bar(), Bar()]
+    ds = [Bar(2), Bar(2)] if pair else [Bar(2)]
+    holds = [None, None]                             # the stage whose S, then dS, is in each buffer
+
+    def ds_of(n):
+        return (ds[n & 1], n >> 1) if pair else (ds[0], n)
+
+    def s_thread():
+        for n in range(stages):
+            if n >= 2:
+                yield lambda n=n: done[n & 1].passed((n >> 1) - 1)
+            assert holds[n & 1] is None, "S over a buffer that dQ has not read"
+            holds[n & 1] = n
+            S[n & 1].arrive()
+            yield lambda: True
+            if n >= 1:
+                yield lambda n=n: read.passed(n - 1)
+            dP.arrive()
+            yield lambda: True
+
+    def warp():
+        for n in range(stages):
+            yield lambda n=n: S[n & 1].passed(n >> 1)
+            assert holds[n & 1] == n
+            yield lambda n=n: dP.passed(n)
+            read.arrive()
+            yield lambda: True
+            ds_of(n)[0].arrive()
+            yield lambda: True
+
+    def dq_thread():
+        for n in range(stages):
+            b, use = ds_of(n)
+            yield lambda b=b, use=use: b.passed(use)
+            assert holds[n & 1] == n
+            holds[n & 1] = None
+            done[n & 1].arrive()
+            yield lambda: True                       # the next item's sizes, a commit: any time
+    return run([s_thread(), warp(), warp(), dq_thread()], rng)
+
+
+def test_dq_stages_follow_one_another_whatever_the_pace():
+    assert all(dq_pipeline(True, random.Random(i)) for i in range(600))
+    assert not all(dq_pipeline(False, random.Random(i)) for i in range(600)), "the model does not show the fault"
+
+
+def test_dq_announces_ds_per_buffer():
+    text = source("attention_dq_tc.cu")
+    assert re.findall(r"wait\(DS_FULL[^;]*;", text) == ["wait(DS_FULL + (n & 1), n >> 1);"]
+    assert re.findall(r"arrive\(DS_FULL[^;]*;", text) == ["arrive(DS_FULL + b);"] and "const int b = n & 1;" in text
+    assert re.search(r"DS_FULL, DONE = DS_FULL \+ 2", text)

@@ -47,3 +47,14 @@ def test_gradients_give_up_and_the_next_call_works(rl, B, H, Hk, Lq, Lk, causal,
     c.wait_limit_ms, c.debug_flags = 0, 0
     status, got = backward()
     assert status == rl.ROLA_OK and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_many_short_items_in_a_row(rl):
+    """Items of one to three stages, tens on each CTA, their lengths mixed: no wait runs out, and the bits repeat."""
+    lens = [1, 129, 300, 64, 257, 128, 0, 299]
+    _, backward = setup(rl, 8, 24, 12, 1500, 300, False, lens)
+    status, want = backward()
+    assert status == rl.ROLA_OK and all(torch.isfinite(t).all() for t in want)
+    for _ in range(50):
+        status, got = backward()
+        assert status == rl.ROLA_OK and all(torch.equal(a, b) for a, b in zip(got, want))
