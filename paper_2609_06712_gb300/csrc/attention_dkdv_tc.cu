@@ -294,6 +294,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dkdv_tc_kernel(const __
         const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_addr = tmem + lane_off + kTmemS + g * 64, p_addr = tmem + lane_off + kTmemP + g * 64;
         const float c_log2 = s.scale_log2, log2e = 1.4426950408889634f;
+        auto warp_wait = [&](int b, int parity) {
+            if (ok) ok = mbar_wait_warp(bar(b), parity & 1, abort, limit);
+            return ok;
+        };
         auto arrive = [&](int b) {
             fence_before_sync();
             __syncwarp();
@@ -338,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dkdv_tc_kernel(const __
                 fetch(it.next(s, nt + 1));                // on their way under this stage's work
                 const int r0 = t * kN, r1 = min(r0 + kN, s.R) - 1;
                 const bool whole = it.x0 + kM <= attn_seen_least(s, it.len, r0, r1);
-                if (!wait(S_FULL + g, k) || !wait(COLS + g, k)) break;
+                if (!warp_wait(S_FULL + g, k) || !warp_wait(COLS + g, k)) break;
                 fence_after_sync();
                 float pr[64];
                 // p of 32 rows from their scores; `masked`: some row does not see all of the item's keys
@@ -395,7 +399,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dkdv_tc_kernel(const __
                 }
                 tmem_st_wait();
                 arrive(P_FULL + g);
-                if (!wait(DP_FULL + g, k)) break;
+                if (!warp_wait(DP_FULL + g, k)) break;
                 fence_after_sync();
                 if (whole) {
                     grads(0, Flag<false>());
@@ -411,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dkdv_tc_kernel(const __
             if (!ok) break;
             // ---- epilogue: group 0 writes dv, group 1 dk
             if (any) {
-                if (!wait(O_FULL, items)) break;
+                if (!warp_wait(O_FULL, items)) break;
                 fence_after_sync();
                 ++items;
             }

@@ -318,6 +318,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dq_tc_kernel(const __gr
         const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_addr = tmem + lane_off + g * 64, p_addr = tmem + lane_off + kTmemP + g * 64;   // this group's columns
         const float c_log2 = s.scale_log2, log2e = 1.4426950408889634f;
+        auto warp_wait = [&](int b, int parity) {
+            if (ok) ok = mbar_wait_warp(bar(b), parity & 1, abort, limit);
+            return ok;
+        };
         auto arrive = [&](int b) {
             fence_before_sync();
             __syncwarp();
@@ -336,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dq_tc_kernel(const __gr
             float D = in && any && it.all > 1 ? p.D[rows + x] : 0.0f;
             for (int t = it.begin; t < it.end; ++t, ++n) {
                 const int b = n & 1;
-                if (!wait(S_FULL + b, n >> 1)) break;
+                if (!warp_wait(S_FULL + b, n >> 1)) break;
                 fence_after_sync();
                 float pr[64];
                 row_load<64>(s_addr + b * 128, pr);
@@ -353,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dq_tc_kernel(const __gr
                     for (int j = 0; j < 64; ++j)
                         if (j >= m) pr[j] = 0.0f;
                 }
-                if (!wait(DP_FULL, n)) break;
+                if (!warp_wait(DP_FULL, n)) break;
                 fence_after_sync();
                 if (it.all == 1) {                    // D from this stage, the only one
                     float d0 = 0.0f, d1 = 0.0f;
@@ -374,7 +378,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dq_tc_kernel(const __gr
                     part[g][gt] = d0 + d1;
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(D_FULL));
-                    if (!wait(D_FULL, singles)) break;
+                    if (!warp_wait(D_FULL, singles)) break;
                     ++singles;
                     D = part[0][gt] + part[1][gt];
                     if (in && g == 0) p.D[rows + x] = D;
@@ -403,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dq_tc_kernel(const __gr
             if (!ok) break;
             // ---- epilogue: group g writes d 64 g .. +63
             if (any) {
-                if (!wait(O_FULL, items)) break;
+                if (!warp_wait(O_FULL, items)) break;
                 fence_after_sync();
                 ++items;
             }

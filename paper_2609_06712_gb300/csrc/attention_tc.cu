@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
             for (int h = 0; h < H; ++h, ++n) {
                 const int key0 = it.first * kKeys + h * kStep, b = n & 1;
                 const uint32_t s_addr = s_base + b * 64;
-                if (!(ok = mbar_wait(bar(S_FULL + 2 * g + b), (n >> 1) & 1, abort, limit))) break;
+                if (!(ok = mbar_wait_warp(bar(S_FULL + 2 * g + b), (n >> 1) & 1, abort, limit))) break;
                 fence_after_sync();
                 float x[64];
                 row_load<64>(s_addr, x);
@@ -426,8 +426,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
                     if (h > 0) {
                         // O has to hold PV(n - 1) before it is scaled: S(n + 1) was issued after it; on the
                         // item's last step there may be no S(n + 1) yet, and PV(n - 1) has a barrier of its own
-                        ok = h < H - 1 ? mbar_wait(bar(S_FULL + 2 * g + (b ^ 1)), ((n + 1) >> 1) & 1, abort, limit)
-                                       : mbar_wait(bar(PV_DONE + g), pairs & 1, abort, limit);
+                        ok = h < H - 1 ? mbar_wait_warp(bar(S_FULL + 2 * g + (b ^ 1)), ((n + 1) >> 1) & 1, abort, limit)
+                                       : mbar_wait_warp(bar(PV_DONE + g), pairs & 1, abort, limit);
                         if (!ok) break;
                         fence_after_sync();
                         const float alpha = fast_exp2(neg_m_new - neg_m);
@@ -478,7 +478,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
                 else if (p.lse) p.lse[at] = lse;
             }
             if (H) {
-                if (!(ok = mbar_wait(bar(O_FULL + g), items & 1, abort, limit))) break;
+                if (!(ok = mbar_wait_warp(bar(O_FULL + g), items & 1, abort, limit))) break;
                 ++items;
                 if (H > 1) ++pairs;
                 fence_after_sync();

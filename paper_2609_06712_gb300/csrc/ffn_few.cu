@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_few_kernel(const __grid_const
         // this CTA's part of the sums into shared memory: [acc][token][128 rows] over the stages, which
         // every product has read
         const int q = warp & 3, row = q * 32 + lane;
-        const bool ok = mbar_wait(bar(ACC_FULL), 0, abort, limit);
+        const bool ok = mbar_wait_warp(bar(ACC_FULL), 0, abort, limit);
         if (!ok) timeout(3);
         else {
             fence_after_sync();

@@ -325,7 +325,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
             int mt, nt;
             const Problem& r = tile_of(p, t, mt, nt);
             const int ab = it & 1;
-            if (!(ok = mbar_wait(bar(C::ACC_FULL + ab), (it >> 1) & 1, abort, limit))) break;
+            if (!(ok = mbar_wait_warp(bar(C::ACC_FULL + ab), (it >> 1) & 1, abort, limit))) break;
             fence_after_sync();
             const int row = mt * kTileM + q * 32 + lane;
             const bool in = row < r.M;
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, 1) ffn_gemm_kernel(const __grid_cons
                     tmem_ld16(acc + col, dh);
                     tmem_ld_wait(dh);
                     release();
-                    if (!(ok = mbar_wait(bar(C::GU_FULL + ew), used & 1, abort, limit))) break;
+                    if (!(ok = mbar_wait_warp(bar(C::GU_FULL + ew), used & 1, abort, limit))) break;
                     ++used;
                     read_row(piece, lane, gv);
                     read_row(piece + kPieceBytes, lane, uv);

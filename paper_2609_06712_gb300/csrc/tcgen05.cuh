@@ -75,6 +75,13 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
 }
 
+// mbar_wait by all lanes of a warp, which give up together or not at all: what follows reads TMEM, an instruction of
+// the whole warp, and lanes that look at different moments may see the phase complete or *abort set.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort, uint64_t limit_ns)
+{
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort, limit_ns)) != 0;
+}
+
 // ------------------------------------------------------------------ TMA
 
 __device__ __forceinline__ void tma_prefetch_desc(const void* map)

@@ -154,3 +154,22 @@ def test_dq_announces_ds_per_buffer():
     assert re.findall(r"wait\(DS_FULL[^;]*;", text) == ["wait(DS_FULL + (n & 1), n >> 1);"]
     assert re.findall(r"arrive\(DS_FULL[^;]*;", text) == ["arrive(DS_FULL + b);"] and "const int b = n & 1;" in text
     assert re.search(r"DS_FULL, DONE = DS_FULL \+ 2", text)
+
+
+# ---------------------------------------------------------------- lanes of a warp
+
+@pytest.mark.parametrize("name,role", [
+    ("attention_tc.cu", "softmax + epilogue"), ("attention_dq_tc.cu", "element-wise work + epilogue"),
+    ("attention_dkdv_tc.cu", "element-wise work + epilogue"), ("ffn_tc.cu", "-- epilogue"),
+    ("ffn_few.cu", "this CTA's part of the sums")])
+def test_warps_that_read_tensor_memory_give_up_as_a_whole(name, role):
+    """Reading TMEM takes the whole warp, so its lanes must agree on how a wait ended (mbar_wait_warp votes); the wait
+    for a warp's own last copies at its end, by one lane, may be a plain one."""
+    with open(os.path.join(CSRC, name)) as f:
+        text = f.read()
+    assert text.count(role) == 1
+    role_text = re.sub(r"//.*", "", text[text.index(role):text.index("fence_before_sync();\n    ", text.index(role))])
+    waits = [w for w in re.findall(r"\b(?:mbar_wait\w*|(?:warp_)?wait)\([^;]*;", role_text) if "&never" not in w]
+    assert waits and all(w.startswith(("mbar_wait_warp(", "warp_wait(")) for w in waits), waits
+    with open(os.path.join(CSRC, "tcgen05.cuh")) as f:
+        assert re.search(r"bool mbar_wait_warp[^}]*__all_sync\(0xffffffffu, mbar_wait\(", f.read())
