@@ -262,6 +262,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dkdv_tc_kernel(const __
                     } else {
                         const bool first = t == it.begin;
                         wait(P_FULL + g, k);
+                        // P says that Q is there, by way of S; dO, of which it knows nothing, may still be on its way
+                        wait(B_FULL + u1 % kSlots, u1 / kSlots);
                         if (first && items >= 1) wait(O_EMPTY, items - 1);
                         if (!ok) break;
                         fence_after_sync();

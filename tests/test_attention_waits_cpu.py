@@ -173,3 +173,76 @@ def test_warps_that_read_tensor_memory_give_up_as_a_whole(name, role):
     assert waits and all(w.startswith(("mbar_wait_warp(", "warp_wait(")) for w in waits), waits
     with open(os.path.join(CSRC, "tcgen05.cuh")) as f:
         assert re.search(r"bool mbar_wait_warp[^}]*__all_sync\(0xffffffffu, mbar_wait\(", f.read())
+
+
+# ---------------------------------------------------------------- the dk / dv kernel's tiles
+
+def dkdv_pipeline(waits_for_dO, rng, stages=10, slots=4):
+    """The dk / dv kernel's loop over stages: Q and dO of each in a ring of slots, filled in their own time; S and dP
+    by a thread of each of two groups, dV and dK by a third.  True if no product read a slot without its tile."""
+    full, empty = [Bar() for _ in range(slots)], [Bar(2) for _ in range(slots)]
+    S, dP, P, dS, V, K = ([Bar(), Bar()] for _ in range(6))
+    tile, good = [None] * slots, [True]
+
+    def read(use):
+        good[0] &= tile[use % slots] == use
+
+    issued = [0]
+
+    def copies():
+        for use in range(2 * stages):
+            yield lambda: use < slots or empty[use % slots].passed(use // slots - 1)
+            tile[use % slots] = None
+            issued[0] += 1
+
+    def landings(slot):                              # each whenever it likes
+        for use in range(slot, 2 * stages, slots):
+            yield lambda: issued[0] > use
+            tile[slot] = use
+            full[slot].arrive()
+
+    def s_thread(g):
+        for n in range(g, stages, 2):
+            k = n >> 1
+            for use, out, before in ((2 * n, S, V), (2 * n + 1, dP, K)):
+                yield lambda: full[use % slots].passed(use // slots)
+                yield lambda: k < 1 or before[g].passed(k - 1)
+                read(use)
+                out[g].arrive()
+                empty[use % slots].arrive()
+
+    def warp(g):
+        for n in range(g, stages, 2):
+            k = n >> 1
+            yield lambda: S[g].passed(k)
+            P[g].arrive()
+            yield lambda: dP[g].passed(k)
+            dS[g].arrive()
+
+    def grad_thread():
+        for n in range(stages):
+            g, k, u0, u1 = n & 1, n >> 1, 2 * n, 2 * n + 1
+            yield lambda: P[g].passed(k)
+            if waits_for_dO:
+                yield lambda: full[u1 % slots].passed(u1 // slots)
+            read(u1)
+            V[g].arrive()
+            empty[u1 % slots].arrive()
+            yield lambda: dS[g].passed(k)
+            read(u0)
+            K[g].arrive()
+            empty[u0 % slots].arrive()
+    ended = run([copies()] + [landings(i) for i in range(slots)] + [s_thread(0), s_thread(1), warp(0), warp(1), grad_thread()], rng)
+    assert ended, "stuck"
+    return good[0]
+
+
+def test_dkdv_products_read_tiles_that_are_there():
+    assert all(dkdv_pipeline(True, random.Random(i)) for i in range(300))
+    assert not all(dkdv_pipeline(False, random.Random(i)) for i in range(300)), "the model does not show the fault"
+
+
+def test_dv_waits_for_its_tile():
+    text = source("attention_dkdv_tc.cu")
+    grad = text[text.index("wait(P_FULL + g, k);"):text.index("gradient(tmem + kTmemV")]
+    assert "wait(B_FULL + u1 % kSlots, u1 / kSlots);" in grad
