@@ -524,6 +524,8 @@ size_t rola_attention_backward_workspace_bytes(const rola_attention_config_t* cf
  * over j < kv_len[b], and with `causal` j <= i + kv_len[b] - Lq.  A query that
  * sees no key (kv_len 0, or an early causal query) has o = 0 and lse = -inf.
  * Keys past kv_len take no part whatever they hold (NaN and infinities too).
+ * NaN or infinite scores of seen keys give what the formulas give: a NaN or
+ * +inf among them, or -inf alone, makes o NaN (never the 0 of an empty row).
  * The running maximum and sum are fp32; bf16 rounds p once, as the operand of
  * the product with v.  Few queries over many keys: the keys are split over
  * CTAs and the parts joined in a fixed order.

@@ -159,11 +159,12 @@ __global__ void __launch_bounds__(256) attention_simt_kernel(const AttnShape s, 
     for (int i = 0; i < 4; ++i) {
         const int r = r0 + ty + 16 * i;
         if (r >= s.R) continue;
-        const float inv = l[i] > 0.0f ? 1.0f / l[i] : 0.0f;
+        // l is 0 where nothing is seen, and over scores of -inf alone: then p is 0 / 0 (with parts the join says so)
+        const float inv = l[i] == 0.0f ? (seen[i] > 0 && s.splits == 1 ? __int_as_float(0x7fc00000) : 0.0f) : 1.0f / l[i];
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[i][j] *= inv;
         const size_t row = (size_t)head * s.R + r;
-        const float lse = l[i] > 0.0f ? m[i] + logf(l[i]) : -INFINITY;
+        const float lse = l[i] == 0.0f ? -INFINITY : m[i] + logf(l[i]);
         if (s.splits > 1) {
             const size_t at = (size_t)blockIdx.z * s.heads * s.R + row;
             store_row(a.part_o + at * kDh, tx, o[i]);
@@ -175,7 +176,8 @@ __global__ void __launch_bounds__(256) attention_simt_kernel(const AttnShape s, 
     }
 }
 
-// o = sum_z w_z o_z with w_z = exp(lse_z - lse), the parts in order.  One warp per row.
+// o = sum_z w_z o_z with w_z = exp(lse_z - lse), the parts in order; NaN if a part is, or if the row sees keys but
+// every score is -inf.  One warp per row.
 template <typename T>
 __global__ void __launch_bounds__(256) attention_join_kernel(const AttnShape s, const AttnArgs a)
 {
@@ -184,12 +186,18 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttnShape s, 
     const long long row = (long long)blockIdx.x * 8 + threadIdx.x / 32;
     if (row >= rows) return;
     float top = -INFINITY;
-    for (int z = lane; z < s.splits; z += 32) top = fmaxf(top, a.part_lse[z * rows + row]);
+    bool nan = false;
+    for (int z = lane; z < s.splits; z += 32) {
+        const float x = a.part_lse[z * rows + row];
+        top = fmaxf(top, x);
+        nan = nan || x != x;
+    }
+    nan = __any_sync(0xffffffffu, nan);
 #pragma unroll
     for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     float l = 0.0f;
-    if (top > -INFINITY) {
+    if (top > -INFINITY || nan) {
         for (int z = 0; z < s.splits; ++z) {
             const float w = expf(a.part_lse[z * rows + row] - top);
             const float4 x = load4(a.part_o + (z * rows + row) * kDh + lane * 4);
@@ -198,9 +206,13 @@ __global__ void __launch_bounds__(256) attention_join_kernel(const AttnShape s, 
         }
         const float inv = 1.0f / l;
         o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
+    } else {
+        const int head = (int)(row / s.R);
+        if (attn_seen(s, attn_len(s, a.kv_len, head / s.Hk), (int)(row - (long long)head * s.R)) > 0)
+            o.x = o.y = o.z = o.w = __int_as_float(0x7fc00000);
     }
     store4(static_cast<T*>(a.o) + row * kDh + lane * 4, o);
-    if (a.lse && lane == 0) a.lse[row] = l > 0.0f ? top + logf(l) : -INFINITY;
+    if (a.lse && lane == 0) a.lse[row] = l == 0.0f ? -INFINITY : top + logf(l);
 }
 
 __device__ __forceinline__ void load8(const float* p, float (&x)[8])

@@ -471,9 +471,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
             const float l = (l0 + l1) + (l2 + l3);
             const size_t row = (size_t)it.head * s.R + r;
             const size_t at = s.splits > 1 ? (size_t)it.part * s.heads * s.R + row : row;
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+            // l is 0 where nothing is seen, and over scores of -inf alone: then p is 0 / 0 (with parts the join says
+            // so); a NaN sum stays one
+            const float inv = l == 0.0f ? (seen > 0 && s.splits == 1 ? __int_as_float(0x7fc00000) : 0.0f) : 1.0f / l;
             if (r < s.R) {
-                const float lse = l > 0.0f ? (log2f(l) - neg_m) * 0.6931471805599453f : -INFINITY;
+                const float lse = l == 0.0f ? -INFINITY : (log2f(l) - neg_m) * 0.6931471805599453f;
                 if (s.splits > 1) p.part_lse[at] = lse;
                 else if (p.lse) p.lse[at] = lse;
             }

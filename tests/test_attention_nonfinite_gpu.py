@@ -1,0 +1,90 @@
+"""Attention over NaN and infinite queries and keys that are seen: o and lse are NaN exactly where the definition's are,
+whether the key axis is split or not, and the other rows are untouched."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DTYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def rl():
+    assert torch.cuda.is_available(), "GPU tests need a CUDA device"
+    from paper_2609_06712_gb300 import build
+    build.build()
+    from paper_2609_06712_gb300 import rola
+    return rola
+
+
+def tensors(B, H, Hk, Lq, Lk, dt):
+    g = torch.Generator().manual_seed(Lq + Lk)
+    return [torch.randn(s, generator=g).to(dt).cuda() for s in ((B, H, Lq, 128), (B, Hk, Lk, 128), (B, Hk, Lk, 128))]
+
+
+def run(rl, q, k, v, causal=False, lens=None):
+    B, H, Lq, _ = q.shape
+    code = rl.ROLA_BF16 if q.dtype == torch.bfloat16 else rl.ROLA_FP32
+    c = rl.make_attention_config(B, H, k.shape[1], Lq, k.shape[2], causal, dtype=code)
+    o, lse, ws = torch.full_like(q, 7.0), torch.full((B, H, Lq), 7.0, device="cuda"), rl.attention_workspace(c)
+    kv = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    rl.attention(c, q, k, v, kv, o, lse, ws)
+    assert rl.get_device_status(ws) == rl.ROLA_OK
+    return o, lse
+
+
+def definition(q, k, v, causal=False, lens=None):
+    B, H, Lq, _ = q.shape
+    Hk, Lk = k.shape[1], k.shape[2]
+    kk, vv = (t.double().repeat_interleave(H // Hk, 1) for t in (k, v))
+    n = torch.tensor([Lk] * B if lens is None else lens, device="cuda").view(B, 1, 1, 1)
+    j, i = torch.arange(Lk, device="cuda"), torch.arange(Lq, device="cuda").view(Lq, 1)
+    seen = (j < n) & ((j <= i + n - Lq) if causal else torch.ones((), dtype=torch.bool, device="cuda"))
+    s = (q.double() @ kk.transpose(2, 3) / math.sqrt(128)).masked_fill(~seen, float("-inf"))
+    p = torch.softmax(s, 3).masked_fill(~seen, 0.0)              # of an empty row: 0
+    vv = torch.where((j < n).transpose(2, 3), vv, 0.0)
+    # about the row's maximum: inf - inf where that is infinite
+    lse = torch.where((s == float("inf")).any(3), float("nan"), torch.logsumexp(s, 3))
+    return p @ vv, lse
+
+
+def check(got, want):
+    (o, lse), (ref, ref_lse) = got, want
+    assert torch.equal(torch.isnan(o), torch.isnan(ref)) and torch.equal(torch.isnan(lse), torch.isnan(ref_lse))
+    good = ~torch.isnan(ref)
+    # P rounded to bf16 (2^-8 of values that average to |o| or less: |v| is below 6) and o once more
+    tol = 0.06 if o.dtype == torch.bfloat16 else 1e-4
+    assert ((o.double() - ref)[good].abs() <= tol).all()
+    fin = torch.isfinite(ref_lse)
+    assert torch.equal(lse[~fin & ~torch.isnan(ref_lse)].double(), ref_lse[~fin & ~torch.isnan(ref_lse)])
+    assert ((lse.double() - ref_lse)[fin].abs() <= 1e-3).all()
+
+
+# one part, parts of a split key axis, and a batch whose second sequence fits one part
+SHAPES = [(1, 2, 2, 3, 100, False, None), (1, 3, 1, 300, 400, True, None), (1, 2, 2, 1, 6000, False, None),
+          (2, 4, 2, 2, 5000, True, [5000, 90]), (2, 2, 1, 1, 4000, False, [0, 4000])]
+
+
+@pytest.mark.parametrize("B,H,Hk,Lq,Lk,causal,lens", SHAPES)
+@pytest.mark.parametrize("dname", sorted(DTYPES))
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_queries(rl, B, H, Hk, Lq, Lk, causal, lens, dname, bad):
+    q, k, v = tensors(B, H, Hk, Lq, Lk, DTYPES[dname])
+    q[B - 1, 0, Lq - 1, 5] = bad
+    check(run(rl, q, k, v, causal, lens), definition(q, k, v, causal, lens))
+    # every score of the row -inf: 0 / 0
+    k[..., 5] = torch.where(k[..., 5] == 0, 1.0, k[..., 5].abs())
+    q[B - 1, 0, Lq - 1, 5] = float("-inf")
+    check(run(rl, q, k, v, causal, lens), definition(q, k, v, causal, lens))
+
+
+@pytest.mark.parametrize("B,H,Hk,Lq,Lk,causal,lens", SHAPES)
+@pytest.mark.parametrize("dname", sorted(DTYPES))
+@pytest.mark.parametrize("at", [0, 60, -1])
+def test_keys(rl, B, H, Hk, Lq, Lk, causal, lens, dname, at):
+    q, k, v = tensors(B, H, Hk, Lq, Lk, DTYPES[dname])
+    n = Lk if lens is None else lens[-1]
+    for bad in (float("nan"), float("inf")):
+        k[B - 1, 0, at % n, 7] = bad
+        check(run(rl, q, k, v, causal, lens), definition(q, k, v, causal, lens))
