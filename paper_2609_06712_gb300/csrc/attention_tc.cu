@@ -24,7 +24,8 @@
 // and l are then scaled by 2^(m_old - m_new).  p = 2^t enters l in fp32 and the
 // product rounded to bf16 (the operand type of the tensor core).  A row sees a
 // prefix of the keys (its length, or its causal limit), so a row that sees
-// nothing in the item's first step sees nothing in the item: its p stay 0, l = 0.
+// nothing in the item's first step sees nothing in the item: its p stay 0, l = 0.  Where the first
+// scores are -inf (infinite keys) m starts at the lowest number and is raised by the first finite one.
 // Keys past the length: their scores are replaced by -inf whatever they are, and
 // their rows of V are zeroed in shared memory (0 x NaN would be NaN).
 //
@@ -37,6 +38,8 @@
 // five 32 KB slots), 9 and 10 products, 11 the zeroing of V's rows.  Shared memory 64 + 160 KB.  Every mbarrier wait
 // is bounded; a wait that gives up records ROLA_ERR_TIMEOUT and the CTA drains
 // what it issued and frees its TMEM.
+#include <float.h>
+
 #include "attention_tc.cuh"
 
 namespace rola {
@@ -422,7 +425,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const __grid_
                                         fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7])));
                 const bool need = h == 0 || fmaf(top, c_log2, neg_m) > kRescaleThreshold;
                 if (__any_sync(0xffffffffu, need)) {
-                    const float neg_m_new = need ? (top == -INFINITY ? 0.0f : -top * c_log2) : neg_m;
+                    // over scores of -inf alone m is the lowest number, which any finite score to come exceeds
+                    const float neg_m_new = need ? fminf(-top * c_log2, FLT_MAX) : neg_m;
                     if (h > 0) {
                         // O has to hold PV(n - 1) before it is scaled: S(n + 1) was issued after it; on the
                         // item's last step there may be no S(n + 1) yet, and PV(n - 1) has a barrier of its own

@@ -88,3 +88,15 @@ def test_keys(rl, B, H, Hk, Lq, Lk, causal, lens, dname, at):
     for bad in (float("nan"), float("inf")):
         k[B - 1, 0, at % n, 7] = bad
         check(run(rl, q, k, v, causal, lens), definition(q, k, v, causal, lens))
+
+
+@pytest.mark.parametrize("dname", sorted(DTYPES))
+@pytest.mark.parametrize("first", [64, 65, 128, 200])
+def test_a_row_whose_first_scores_are_minus_infinity(rl, dname, first):
+    """Finite scores far below 0 after whole steps of -inf: the running maximum has to start with them."""
+    q, k, v = tensors(1, 2, 1, 130, 300, DTYPES[dname])
+    q.zero_()
+    q[..., 3], q[..., 10] = 1.0, 8.0
+    k[..., 10] -= 200.0                              # scores of -140: 2^-200 of what a maximum of 0 would ask for
+    k[:, :, :first, 3] = float("-inf")
+    check(run(rl, q, k, v), definition(q, k, v))
