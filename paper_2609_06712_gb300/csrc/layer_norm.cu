@@ -36,6 +36,7 @@ namespace {
 
 constexpr int kWarpGroups = 4;           // rows of a CTA whose rows have a warp each
 constexpr int kMaxThreads = 512;         // of a CTA that has one row
+constexpr size_t kStaticSmem = sizeof(float2[2][32]);    // of the row kernels: `red`
 
 // A piece as loaded: 16 bytes (V elements), or one element (V = 1).
 template <typename T, int V>
@@ -606,7 +607,8 @@ cudaError_t shape_of(K kernel, const LnArgs& a, bool warp, int pieces, int nv, i
         ring = (size_t)groups * matrices * l->depth * row_bytes;
     }
     l->smem = (size_t)groups * kMaxDepth * 8 + (ring > sums ? ring : sums);
-    if (l->smem > 48 << 10) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)l->smem);
+    // 48 KB without asking are of static and dynamic shared memory together
+    if (l->smem + kStaticSmem > 48 << 10) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)l->smem);
     if (e != cudaSuccess) return e;
     int per_sm = 0;
     e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, l->threads, l->smem);
