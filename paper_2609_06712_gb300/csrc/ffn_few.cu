@@ -52,6 +52,8 @@ struct Ctrl {
     int abort;
 };
 
+constexpr size_t kSmemMost = kSmemBudget + sizeof(Ctrl);     // of a CTA, whatever the sizes
+
 struct Params {
     CUtensorMap a[2], b[2];          // weights (kUp: gate and up; kDX: the two sources), tokens
     int M, rows;                     // tokens; weight rows of the output (d_ff or d_model)
@@ -302,7 +304,8 @@ cudaError_t launch(const FfnShape& s, Params& p, bool dependent, DeviceStatus* s
     p.tiles_bytes = (p.tiles_bytes + 1023) & ~1023u;
     const size_t smem = p.tiles_bytes + sizeof(Ctrl);
     auto kernel = ffn_few_kernel<MODE>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    // the limit is the kernel's, not the call's: every call sets it to the same, since another thread may be about to launch
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost);
     if (e != cudaSuccess) return e;
     // As many CTAs as two per SM hold, each with two K steps at least, and with twice the weights of the sums that
     // it takes from its peers (77 tokens at widths 1536 x 4096: 24.7 us, 26.9 with 8 CTAs a tile in the up products).
@@ -323,7 +326,7 @@ cudaError_t launch(const FfnShape& s, Params& p, bool dependent, DeviceStatus* s
     // A cluster's CTAs share a GPC, and not every size fills its SMs: 38 clusters of 7 are in flight at once, 46 of 6.
     // A few tiles left for a second wave cost a whole one (one token at 5120 x 13824, whose 40 down tiles
     // would take 7: 87 us, with 6 72).
-    e = cudaFuncSetAttribute(like_ffn_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    e = cudaFuncSetAttribute(like_ffn_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost);
     if (e != cudaSuccess) return e;
     for (;; --cluster) {
         at[0].val.clusterDim.x = cluster;

@@ -163,6 +163,7 @@ __device__ __forceinline__ float2 group_sum(float a, float b, float2 (*red)[32],
 }
 
 constexpr int kMaxDepth = 16;            // rows in a group's ring
+constexpr size_t kRingBytes = 160 << 10;             // of the rings of an SM's CTAs
 constexpr uint64_t kWaitLimitNs = 2000000000ull;     // bound of the wait for a row
 
 // A group's rows r0, r0 + stride, ... of N matrices, brought ahead.  RING: into
@@ -580,7 +581,8 @@ struct LnArgs {
 
 // CTA size, ring depth and grid of rows of `pieces` pieces, NV per thread: a warp per row, or a CTA of the
 // least whole number of warps.  The rings of an SM's CTAs (as many as their registers allow, up to 1024
-// threads) hold about 160 KB, and no more rows than a group has.
+// threads) hold about 160 KB, and no more rows than a group has.  (Two rows at least: of 32 KB and two
+// matrices at most, so a CTA's ring stays within 160 KB, and the warps' sums are far smaller.)
 struct Launch {
     int threads, grid, depth;
     size_t smem;
@@ -600,15 +602,18 @@ cudaError_t shape_of(K kernel, const LnArgs& a, bool warp, int pieces, int nv, i
     size_t ring = 0;
     if (row_bytes) {
         const long long each = (a.rows + (long long)a.nsm * ctas * groups - 1) / ((long long)a.nsm * ctas * groups);
-        long long n = (160 << 10) / (ctas * groups * matrices * (long long)row_bytes);
+        long long n = (long long)kRingBytes / (ctas * groups * matrices * (long long)row_bytes);
         if (n > each) n = each;
         if (n > kMaxDepth) n = kMaxDepth;
         l->depth = n < 2 ? 2 : (int)n;
         ring = (size_t)groups * matrices * l->depth * row_bytes;
     }
     l->smem = (size_t)groups * kMaxDepth * 8 + (ring > sums ? ring : sums);
-    // 48 KB without asking are of static and dynamic shared memory together
-    if (l->smem + kStaticSmem > 48 << 10) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)l->smem);
+    // 48 KB without asking are of static and dynamic shared memory together.  The limit is the kernel's, not the
+    // call's: every call sets it to the same, the most that any needs, since another thread may be about to launch.
+    if (l->smem + kStaticSmem > 48 << 10)
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)(kRingBytes + kWarpGroups * kMaxDepth * 8));
     if (e != cudaSuccess) return e;
     int per_sm = 0;
     e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, l->threads, l->smem);
