@@ -302,19 +302,22 @@ def _dtype_of(t, where: str) -> int:
     return _DTYPES[t.dtype]
 
 
-def _a(t, dtype, shape, where: str, name: str):
-    """The address of tensor `t` (None: NULL, which the library judges), checked against its dtype and shape."""
+def _gpu(t, where: str, name: str) -> int:
+    """The number of the GPU that the call's first tensor is on, where all the others have to be."""
+    dev = -1 if t is None else t.get_device()
+    if dev < 0:
+        raise ValueError(f"{where}: {name} must be a CUDA tensor")
+    return dev
+
+
+def _a(t, dtype, shape, where: str, name: str, dev: int):
+    """The address of tensor `t` (None: NULL, which the library judges), checked against its dtype, shape and GPU."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{where}: {name} must be a contiguous CUDA tensor, {dtype} of shape {tuple(shape)}, not "
-                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{where}: {name} must be a contiguous tensor on GPU {dev}, {dtype} of shape {tuple(shape)}, "
+                         f"not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
-
-
-def _st(t, stream):
-    """The stream a call on tensor `t` goes to: the given one, or the current one of t's device."""
-    return torch._C._cuda_getCurrentRawStream(t.device.index) if stream is None else stream.cuda_stream
 
 
 def _bytes(n: int, where: str, device) -> torch.Tensor:
@@ -323,8 +326,22 @@ def _bytes(n: int, where: str, device) -> torch.Tensor:
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _ws(ws, where: str):
-    return _a(ws, torch.uint8, ws.shape, where, "ws"), ws.numel()
+def _ws(ws, where: str, dev: int):
+    return _a(ws, torch.uint8, ws.shape, where, "ws", dev), ws.numel()
+
+
+def _run(fn, where: str, dev: int, stream, *args):
+    """fn(*args, stream) with GPU `dev` current, which the library launches on; stream None: its current one."""
+    if stream is not None and stream.device_index != dev:
+        raise ValueError(f"{where}: the stream is on GPU {stream.device_index}, the tensors on GPU {dev}")
+    handle = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if torch._C._cuda_getDevice() == dev:
+        st = fn(*args, handle)
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args, handle)
+    if st:
+        raise RolaError(st, where)
 
 
 _F32 = torch.float32
@@ -335,12 +352,10 @@ def layer_norm(x, gamma, beta, eps: float, y, mean=None, rstd=None, stream=None)
     mean and rstd (fp32, one per row), if given, receive what layer_norm_backward reads."""
     w, dt, shape = "rola_layer_norm", x.dtype, x.shape
     d, code = shape[-1], _dtype_of(x, "rola_layer_norm")
-    st = _lib.rola_layer_norm(x.numel() // max(d, 1), d, code, _a(x, dt, shape, w, "x"), _a(gamma, dt, (d,), w, "gamma"),
-                              _a(beta, dt, (d,), w, "beta"), eps, _a(y, dt, shape, w, "y"),
-                              _a(mean, _F32, shape[:-1], w, "mean"), _a(rstd, _F32, shape[:-1], w, "rstd"),
-                              _st(x, stream))
-    if st:
-        raise RolaError(st, w)
+    dev = _gpu(x, w, "x")
+    _run(_lib.rola_layer_norm, w, dev, stream, x.numel() // max(d, 1), d, code, _a(x, dt, shape, w, "x", dev),
+         _a(gamma, dt, (d,), w, "gamma", dev), _a(beta, dt, (d,), w, "beta", dev), eps, _a(y, dt, shape, w, "y", dev),
+         _a(mean, _F32, shape[:-1], w, "mean", dev), _a(rstd, _F32, shape[:-1], w, "rstd", dev))
 
 
 def layer_norm_backward_workspace(x) -> torch.Tensor:
@@ -352,13 +367,12 @@ def layer_norm_backward(x, gamma, mean, rstd, dy, dx, dgamma, dbeta, ws, stream=
     """dx of layer_norm, and dgamma, dbeta (fp32 [d], or both None)."""
     w, dt, shape = "rola_layer_norm_backward", x.dtype, x.shape
     d, code = shape[-1], _dtype_of(x, "rola_layer_norm_backward")
-    st = _lib.rola_layer_norm_backward(
-        x.numel() // max(d, 1), d, code, _a(x, dt, shape, w, "x"), _a(gamma, dt, (d,), w, "gamma"),
-        _a(mean, _F32, shape[:-1], w, "mean"), _a(rstd, _F32, shape[:-1], w, "rstd"), _a(dy, dt, shape, w, "dy"),
-        _a(dx, dt, shape, w, "dx"), _a(dgamma, _F32, (d,), w, "dgamma"), _a(dbeta, _F32, (d,), w, "dbeta"), *_ws(ws, w),
-        _st(x, stream))
-    if st:
-        raise RolaError(st, w)
+    dev = _gpu(x, w, "x")
+    _run(_lib.rola_layer_norm_backward, w, dev, stream, x.numel() // max(d, 1), d, code,
+         _a(x, dt, shape, w, "x", dev), _a(gamma, dt, (d,), w, "gamma", dev),
+         _a(mean, _F32, shape[:-1], w, "mean", dev), _a(rstd, _F32, shape[:-1], w, "rstd", dev),
+         _a(dy, dt, shape, w, "dy", dev), _a(dx, dt, shape, w, "dx", dev), _a(dgamma, _F32, (d,), w, "dgamma", dev),
+         _a(dbeta, _F32, (d,), w, "dbeta", dev), *_ws(ws, w, dev))
 
 
 def make_ffn_config(tokens: int, d_model: int, d_ff: int, act="silu", dtype: int = ROLA_BF16) -> RolaFfnConfig:
@@ -381,32 +395,32 @@ def ffn_backward_workspace(c: RolaFfnConfig, device="cuda") -> torch.Tensor:
 def ffn(c, X, W_gate, W_up, W_down, Y, ws, stream=None):
     """Y = (phi(X W_gate^T) * (X W_up^T)) W_down^T; X, Y [tokens][d_model], weights in the nn.Linear layout."""
     w, dt, m, d, f = "rola_ffn", _TORCH_DTYPES.get(c.dtype), c.tokens, c.d_model, c.d_ff
-    st = _lib.rola_ffn(c, _a(X, dt, (m, d), w, "X"), _a(W_gate, dt, (f, d), w, "W_gate"), _a(W_up, dt, (f, d), w, "W_up"),
-                       _a(W_down, dt, (d, f), w, "W_down"), _a(Y, dt, (m, d), w, "Y"), *_ws(ws, w), _st(X, stream))
-    if st:
-        raise RolaError(st, w)
+    dev = _gpu(X, w, "X")
+    _run(_lib.rola_ffn, w, dev, stream, c, _a(X, dt, (m, d), w, "X", dev), _a(W_gate, dt, (f, d), w, "W_gate", dev),
+         _a(W_up, dt, (f, d), w, "W_up", dev), _a(W_down, dt, (d, f), w, "W_down", dev),
+         _a(Y, dt, (m, d), w, "Y", dev), *_ws(ws, w, dev))
 
 
 def ffn_train(c, X, W_gate, W_up, W_down, Y, G, U, ws, stream=None):
     """ffn keeping G = X W_gate^T and U = X W_up^T (fp32 [tokens][d_ff]) for ffn_backward."""
     w, dt, m, d, f = "rola_ffn_train", _TORCH_DTYPES.get(c.dtype), c.tokens, c.d_model, c.d_ff
-    st = _lib.rola_ffn_train(c, _a(X, dt, (m, d), w, "X"), _a(W_gate, dt, (f, d), w, "W_gate"),
-                             _a(W_up, dt, (f, d), w, "W_up"), _a(W_down, dt, (d, f), w, "W_down"), _a(Y, dt, (m, d), w, "Y"),
-                             _a(G, _F32, (m, f), w, "G"), _a(U, _F32, (m, f), w, "U"), *_ws(ws, w), _st(X, stream))
-    if st:
-        raise RolaError(st, w)
+    dev = _gpu(X, w, "X")
+    _run(_lib.rola_ffn_train, w, dev, stream, c, _a(X, dt, (m, d), w, "X", dev),
+         _a(W_gate, dt, (f, d), w, "W_gate", dev), _a(W_up, dt, (f, d), w, "W_up", dev),
+         _a(W_down, dt, (d, f), w, "W_down", dev), _a(Y, dt, (m, d), w, "Y", dev), _a(G, _F32, (m, f), w, "G", dev),
+         _a(U, _F32, (m, f), w, "U", dev), *_ws(ws, w, dev))
 
 
 def ffn_backward(c, X, W_gate, W_up, W_down, G, U, dY, dX, dW_gate, dW_up, dW_down, ws, stream=None):
     """Gradients of ffn_train: dX and the three weights', in the weights' dtype."""
     w, dt, m, d, f = "rola_ffn_backward", _TORCH_DTYPES.get(c.dtype), c.tokens, c.d_model, c.d_ff
-    st = _lib.rola_ffn_backward(
-        c, _a(X, dt, (m, d), w, "X"), _a(W_gate, dt, (f, d), w, "W_gate"), _a(W_up, dt, (f, d), w, "W_up"),
-        _a(W_down, dt, (d, f), w, "W_down"), _a(G, _F32, (m, f), w, "G"), _a(U, _F32, (m, f), w, "U"),
-        _a(dY, dt, (m, d), w, "dY"), _a(dX, dt, (m, d), w, "dX"), _a(dW_gate, dt, (f, d), w, "dW_gate"),
-        _a(dW_up, dt, (f, d), w, "dW_up"), _a(dW_down, dt, (d, f), w, "dW_down"), *_ws(ws, w), _st(X, stream))
-    if st:
-        raise RolaError(st, w)
+    dev = _gpu(X, w, "X")
+    _run(_lib.rola_ffn_backward, w, dev, stream, c, _a(X, dt, (m, d), w, "X", dev),
+         _a(W_gate, dt, (f, d), w, "W_gate", dev), _a(W_up, dt, (f, d), w, "W_up", dev),
+         _a(W_down, dt, (d, f), w, "W_down", dev), _a(G, _F32, (m, f), w, "G", dev), _a(U, _F32, (m, f), w, "U", dev),
+         _a(dY, dt, (m, d), w, "dY", dev), _a(dX, dt, (m, d), w, "dX", dev),
+         _a(dW_gate, dt, (f, d), w, "dW_gate", dev), _a(dW_up, dt, (f, d), w, "dW_up", dev),
+         _a(dW_down, dt, (d, f), w, "dW_down", dev), *_ws(ws, w, dev))
 
 
 def make_attention_config(B: int, H: int, H_kv: int, Lq: int, Lk: int, causal: bool = False, scale: float = 0.0,
@@ -431,28 +445,28 @@ def attention(c, q, k, v, kv_len, o, lse, ws, stream=None):
     q, o [B][H][Lq][128], k, v [B][H_kv][Lk][128].  lse (fp32 [B][H][Lq]) is what attention_backward reads."""
     w, dt = "rola_attention", _TORCH_DTYPES.get(c.dtype)
     rows, keys = (c.B, c.H, c.Lq, c.d_h), (c.B, c.H_kv, c.Lk, c.d_h)
-    st = _lib.rola_attention(c, _a(q, dt, rows, w, "q"), _a(k, dt, keys, w, "k"), _a(v, dt, keys, w, "v"),
-                             _a(kv_len, torch.int32, rows[:1], w, "kv_len"), _a(o, dt, rows, w, "o"),
-                             _a(lse, _F32, rows[:3], w, "lse"), *_ws(ws, w), _st(q, stream))
-    if st:
-        raise RolaError(st, w)
+    dev = _gpu(q, w, "q")
+    _run(_lib.rola_attention, w, dev, stream, c, _a(q, dt, rows, w, "q", dev), _a(k, dt, keys, w, "k", dev),
+         _a(v, dt, keys, w, "v", dev), _a(kv_len, torch.int32, rows[:1], w, "kv_len", dev),
+         _a(o, dt, rows, w, "o", dev), _a(lse, _F32, rows[:3], w, "lse", dev), *_ws(ws, w, dev))
 
 
 def attention_backward(c, q, k, v, kv_len, o, lse, dO, dq, dk, dv, ws, stream=None):
     """Gradients of attention from its o and lse; the probabilities are recomputed."""
     w, dt = "rola_attention_backward", _TORCH_DTYPES.get(c.dtype)
     rows, keys = (c.B, c.H, c.Lq, c.d_h), (c.B, c.H_kv, c.Lk, c.d_h)
-    st = _lib.rola_attention_backward(
-        c, _a(q, dt, rows, w, "q"), _a(k, dt, keys, w, "k"), _a(v, dt, keys, w, "v"),
-        _a(kv_len, torch.int32, rows[:1], w, "kv_len"), _a(o, dt, rows, w, "o"), _a(lse, _F32, rows[:3], w, "lse"),
-        _a(dO, dt, rows, w, "dO"), _a(dq, dt, rows, w, "dq"), _a(dk, dt, keys, w, "dk"), _a(dv, dt, keys, w, "dv"),
-        *_ws(ws, w), _st(q, stream))
-    if st:
-        raise RolaError(st, w)
+    dev = _gpu(q, w, "q")
+    _run(_lib.rola_attention_backward, w, dev, stream, c, _a(q, dt, rows, w, "q", dev), _a(k, dt, keys, w, "k", dev),
+         _a(v, dt, keys, w, "v", dev), _a(kv_len, torch.int32, rows[:1], w, "kv_len", dev),
+         _a(o, dt, rows, w, "o", dev), _a(lse, _F32, rows[:3], w, "lse", dev), _a(dO, dt, rows, w, "dO", dev),
+         _a(dq, dt, rows, w, "dq", dev), _a(dk, dt, keys, w, "dk", dev), _a(dv, dt, keys, w, "dv", dev),
+         *_ws(ws, w, dev))
 
 
 def get_device_status(ws, stream=None) -> int:
-    return _lib.rola_get_device_status(_p(ws), _stream(stream))
+    p = _p(ws)
+    with torch.cuda.device(ws.device):
+        return _lib.rola_get_device_status(p, _stream(stream))
 
 
 class RoLAAttention:
