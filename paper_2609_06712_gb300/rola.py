@@ -11,6 +11,7 @@ import ctypes
 import os
 
 import torch
+from torch.autograd.function import once_differentiable
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "librola.so")
@@ -515,6 +516,7 @@ class RoLAFunction(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dO):
         q, k, v, P_q, P_k, gate, kv, o_s, lse, C = ctx.saved_tensors
         c = ctx.c
@@ -544,6 +546,7 @@ class LayerNormFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, gamma, mean, rstd = ctx.saved_tensors
         dx, dgamma, dbeta = torch.empty_like(x), None, None
@@ -571,6 +574,7 @@ class FfnFunction(torch.autograd.Function):
         return Y.view(X.shape)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dY):
         x, W_gate, W_up, W_down, G, U = ctx.saved_tensors
         dX, dWg, dWu, dWd = (torch.empty_like(t) for t in (x, W_gate, W_up, W_down))
@@ -595,6 +599,7 @@ class AttentionFunction(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dO):
         q, k, v, kv_len, o, lse = ctx.saved_tensors
         dq, dk, dv = (torch.empty_like(t) for t in (q, k, v))
