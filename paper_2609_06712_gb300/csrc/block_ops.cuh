@@ -68,7 +68,7 @@ __device__ __forceinline__ float gate_act(int kind, float g)
         case ROLA_LOWRANK_ACT_SILU: return g / (1.0f + expf(-g));
         case ROLA_LOWRANK_ACT_IDENTITY: return g;
         case ROLA_LOWRANK_ACT_TANH: return tanhf(g);
-        case ROLA_LOWRANK_ACT_RELU: return fmaxf(g, 0.0f);
+        case ROLA_LOWRANK_ACT_RELU: return g <= 0.0f ? 0.0f : g;         // (fmaxf would make a NaN 0)
         default: return 0.5f * g * erfcf(g * -0.7071067811865476f);
     }
 }
@@ -83,7 +83,10 @@ __device__ __forceinline__ void gate_act_grad(int kind, float g, float& a, float
         }
         case ROLA_LOWRANK_ACT_IDENTITY: a = g; da = 1.0f; return;
         case ROLA_LOWRANK_ACT_TANH: a = tanhf(g); da = fmaf(-a, a, 1.0f); return;
-        case ROLA_LOWRANK_ACT_RELU: a = fmaxf(g, 0.0f); da = g > 0.0f ? 1.0f : 0.0f; return;
+        case ROLA_LOWRANK_ACT_RELU:
+            a = g <= 0.0f ? 0.0f : g;
+            da = g > 0.0f ? 1.0f : a;                                    // 0, or NaN
+            return;
         default: {
             const float cdf = 0.5f * erfcf(g * -0.7071067811865476f);
             a = g * cdf;
