@@ -544,7 +544,9 @@ rola_status_t rola_attention(const rola_attention_config_t* cfg, const void* q, 
  *   D_i = dO_i . o_i,  dp_ij = dO_i . v_j,  ds_ij = scale p_ij (dp_ij - D_i)
  *   dv_j = sum_i p_ij dO_i,  dq_i = sum_j ds_ij k_j,  dk_j = sum_i ds_ij q_i
  * dk and dv are summed over the query heads that share a key head; they are 0 at
- * the keys no query sees, and dq is 0 for a query that sees no key.
+ * the keys no query sees, and dq is 0 for a query that sees no key, whatever dO
+ * holds there.  dk and dv are products over all queries, so q and dO have to be
+ * finite in those rows too.
  *   q, k, v, kv_len, o, lse : as rola_attention read and wrote them
  *   dO : [B][H][Lq][d_h];  dq : out, as q;  dk, dv : out, as k and v; dtype
  */

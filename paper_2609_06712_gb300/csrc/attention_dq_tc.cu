@@ -337,7 +337,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_dq_tc_kernel(const __gr
             const int seen = in ? attn_seen(s, it.len, x) : 0;
             const int least = any && it.x0 + kM <= s.R ? attn_seen_least(s, it.len, it.x0, it.x0 + kM - 1) : 0;
             const float neg_lse = in ? -p.lse[rows + x] * log2e : 0.0f;
-            float D = in && any && it.all > 1 ? p.D[rows + x] : 0.0f;
+            // (a row that sees nothing: its dO may be anything, and 0 x infinity in D would show in dq)
+            float D = seen > 0 && any && it.all > 1 ? p.D[rows + x] : 0.0f;
             for (int t = it.begin; t < it.end; ++t, ++n) {
                 const int b = n & 1;
                 if (!warp_wait(S_FULL + b, n >> 1)) break;

@@ -100,3 +100,27 @@ def test_a_row_whose_first_scores_are_minus_infinity(rl, dname, first):
     k[..., 10] -= 200.0                              # scores of -140: 2^-200 of what a maximum of 0 would ask for
     k[:, :, :first, 3] = float("-inf")
     check(run(rl, q, k, v), definition(q, k, v))
+
+
+@pytest.mark.parametrize("dname", sorted(DTYPES))
+@pytest.mark.parametrize("B,H,Hk,Lq,Lk,lens", [(1, 4, 2, 300, 200, None), (2, 6, 2, 170, 160, [160, 140]), (1, 2, 1, 90, 60, None)])
+def test_dq_of_queries_that_see_nothing(rl, dname, B, H, Hk, Lq, Lk, lens):
+    """It is 0 whatever the incoming gradient holds there: rows in front of a causal sequence, beside the last rows of
+    the head before in the same tile."""
+    q, k, v = tensors(B, H, Hk, Lq, Lk, DTYPES[dname])
+    code = rl.ROLA_BF16 if dname == "bf16" else rl.ROLA_FP32
+    c = rl.make_attention_config(B, H, Hk, Lq, Lk, True, dtype=code)
+    kv = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    o, lse = torch.empty_like(q), torch.empty((B, H, Lq), device="cuda")
+    rl.attention(c, q, k, v, kv, o, lse, rl.attention_workspace(c))
+    dO = torch.randn(q.shape, generator=torch.Generator().manual_seed(1)).to(q.dtype).cuda()
+    clean, grads = ([torch.empty_like(t) for t in (q, k, v)] for _ in range(2))
+    bws = rl.attention_backward_workspace(c)
+    rl.attention_backward(c, q, k, v, kv, o, lse, dO, *clean, bws)
+    empty = [Lq - n for n in (lens or [Lk] * B)]
+    for b, n in enumerate(empty):
+        dO[b, :, :n, 3] = float("inf")
+        dO[b, :, :n, 40] = float("nan")
+    rl.attention_backward(c, q, k, v, kv, o, lse, dO, *grads, bws)
+    for b, n in enumerate(empty):
+        assert (grads[0][b, :, :n] == 0).all() and torch.equal(grads[0][b, :, n:], clean[0][b, :, n:])
