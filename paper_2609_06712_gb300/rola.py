@@ -538,6 +538,8 @@ class LayerNormFunction(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, gamma, beta, eps):
+        if (gamma is None) != (beta is None):
+            raise ValueError("LayerNormFunction: gamma and beta are both tensors or both None")
         x = x.contiguous()
         y = torch.empty_like(x)
         mean, rstd = (torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) for _ in range(2))
