@@ -17,3 +17,16 @@ rl = base.rl
 def test_rings_of_48_kb(rl, rows, d, dname):
     x, gamma, beta, dy = base.inputs_of(rows, d, DTYPES[dname], seed=d)
     base.check(x, gamma, beta, dy, base.run(rl, x, gamma, beta, dy))
+
+
+# every CTA or warp takes tens of rows: warps (64, 512), CTAs with deep and shallow rings, single elements
+@pytest.mark.parametrize("rows,d", [(100000, 64), (60001, 512), (20000, 1536), (6000, 5120), (3000, 12224), (9000, 777), (3000, 4999)])
+@pytest.mark.parametrize("dname", sorted(DTYPES))
+def test_many_rows(rl, rows, d, dname):
+    if dname == "fp32" and d == 12224:
+        d //= 2
+    x, gamma, beta, dy = base.inputs_of(rows, d, DTYPES[dname], seed=d)
+    got = base.run(rl, x, gamma, beta, dy)
+    base.check(x, gamma, beta, dy, got)
+    again = base.run(rl, x, gamma, beta, dy)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
