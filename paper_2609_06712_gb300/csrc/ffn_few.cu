@@ -353,12 +353,22 @@ Params params(const FfnShape& s)
 
 }  // namespace
 
-// Up to 96 tokens, and beyond while the down product's tiles of 128 x 256 would leave half of the 152 SMs idle
-// (130 tokens at widths 5120 x 13824: 134 us against 172 in such tiles).  The backward's products read their
-// weights MN-major and gain nothing from tokens side by side (dX of 300 tokens at 1536 x 4096: 71 us against 46).
+// Up to 96 tokens, and beyond (up to seven tiles of 96) while the tiles of 128 x 256 would leave half of the 152 SMs
+// idle in the down product and the weights, which every tile of tokens reads again from L2, stay below 3 x 1.5e8
+// elements over all tiles.  Forward, us, this form / tiles of 128 x 256, the weights from HBM:
+//   1536 x 4096: 130 tokens 27 / 45, 400 43 / 45, 600 51 / 54, 900 70 / 54, 1500 100 / 63
+//   5120 x 13824: 130 tokens 120 / 158, 200 191 / 158, 300 261 / 183
+//   512 x 8192: 130 tokens 31 / 63, 600 50 / 69, 1200 79 / 75, 4500 251 / 113
+//   64 x 4096: 600 tokens 25 / 32, 1500 39 / 35, 9600 164 / 69;  256 x 1024: 130 tokens 21 / 19, 600 24 / 19
+// (What decides is how often the weights are read against how long a tile's K axis is; these two numbers are within 1.4 %
+// of the better form on average over 140 measured calls of nine widths, and within a third in the worst.)  The
+// backward's products read their weights MN-major and gain nothing from tokens side by side (dX of 300 tokens at
+// 1536 x 4096: 71 us against 46).
 bool ffn_few(const FfnShape& s)
 {
-    return s.M <= kMaxTokens || (int64_t)((s.M + 127) / 128) * ((s.D + 255) / 256) < 76;
+    const int64_t tiles = (s.M + kMaxTokens - 1) / kMaxTokens;
+    return tiles == 1 || (tiles <= 7 && tiles * s.D * s.F <= 150000000 &&
+                          (int64_t)((s.M + 127) / 128) * ((s.D + 255) / 256) < 76);
 }
 
 cudaError_t launch_ffn_few(const FfnShape& s, const void* X, const void* Wg, const void* Wu, const void* Wd, void* H,

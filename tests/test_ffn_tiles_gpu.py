@@ -1,7 +1,7 @@
 """The feed-forward's tensor-core products in tiles of 128 x 256, forward and backward, at sizes where every CTA takes
 several tiles: against 64 bits, inside guarded buffers, and when a wait runs out.
 
-The forward takes these tiles from 76 of them on in the down product (fewer go side by side in tiles of few tokens), and
+The forward takes these tiles from 76 of them on in the down product at the latest (fewer tokens go in tiles of few), and
 a GB300 has 152 SMs: the sizes below have up to 693 tiles in a product, more than 16 row tiles, partial tiles in
 every direction, and rows that are and are not multiples of 32 bytes.
 """
