@@ -48,6 +48,10 @@ class DiTBlock(torch.nn.Module):
 
     def forward(self, x, text, text_len=None):
         """x [B][N][d_model], text [B][L][d_text], text_len int32 [B] (None: the whole text)."""
+        with torch.cuda.device(x.device):            # the module launches on the current device
+            return self._forward(x, text, text_len)
+
+    def _forward(self, x, text, text_len):
         q, k, v = self._heads(linear(self._norm(0, x), self.W_qkv), 3)
         x = x + linear(self._join(rola.RoLAFunction.apply(self.cfg, q, k, v, self.P_q, self.P_k, None)), self.W_o)
         (q,), (k, v) = self._heads(linear(self._norm(1, x), self.W_cq), 1), self._heads(linear(text, self.W_ckv), 2)
