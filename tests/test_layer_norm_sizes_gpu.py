@@ -30,3 +30,20 @@ def test_many_rows(rl, rows, d, dname):
     base.check(x, gamma, beta, dy, got)
     again = base.run(rl, x, gamma, beta, dy)
     assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+@pytest.mark.parametrize("offset", [1000.3, -54321.7])
+@pytest.mark.parametrize("d", [777, 1536])
+def test_offsets_whose_mean_is_rounded(rl, offset, d):
+    """The mean of such rows is not an fp32 number: x - mu carries its rounding, |mu| d 2^-24 at most, which check's bounds
+    hold; the variance, about that mean, does not cancel."""
+    x, gamma, beta, dy = base.inputs_of(200, d, DTYPES["fp32"], seed=d)
+    x = x + offset
+    got = base.run(rl, x, gamma, beta, dy)
+    base.check(x, gamma, beta, dy, got)
+    # a row's sum is at most 18 additions deep (8 or 9 in a thread, 5 in a warp, 3 to 5 across warps), its mean two
+    # roundings more, each within 2^-24 of |mu|; what else happens is within 2^-18 of y
+    rstd = (x.double().var(1, unbiased=False, keepdim=True) + base.EPS).rsqrt()
+    y = (x.double() - x.double().mean(1, keepdim=True)) * rstd * gamma.double() + beta.double()
+    bound = 20 * 2.0 ** -24 * (abs(offset) + 4) * rstd * gamma.double().abs() + 2.0 ** -18 * (1 + y.abs())
+    assert ((got[0].double() - y).abs() <= bound).all()
