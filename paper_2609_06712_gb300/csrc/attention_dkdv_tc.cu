@@ -17,8 +17,9 @@
 // all stages in order.  So each group goes through scores, P, dP, dS at its own
 // pace, under the other's products.  (With stages of 128 rows in which both groups
 // work side by side the four steps form one chain of 4100 cycles, 2048 of them products:
-// 814 us at 12 heads x 8190 x 8190, 700 us so, 1180 TFLOP/s.  The bound now is the tensor
-// pipe with its 128 x 64 products, 48 cycles each where half a 128 x 128 one would take 32.)
+// 814 us at 12 heads x 8190 x 8190, 672 us so, 1230 TFLOP/s.  The tensor pipe is then 63 % busy, its
+// 128 x 64 products taking 48 cycles each where half a 128 x 128 one would take 32; the rest are waits within
+// the groups' chains.  64 bytes a thread are spilled.)
 //
 // A key past the sequence's length has P = dS = 0 by selection whatever it holds.
 // Few items: their rows are split over several (AttnShape::splits_dkv); the parts

@@ -17,7 +17,7 @@
 // each, under the products of the stages beside it.  (One issuing thread and stages
 // of 64 took 1.7 times as long: a 128 x 64 product takes 48 cycles instead of 32, and
 // one thread's waits, products and commits, 150, 17 and 50 to 150 cycles each, were the bound.
-// 427 us at 12 heads x 8190 x 8190, 1450 TFLOP/s.)
+// 430 us at 12 heads x 8190 x 8190, 1440 TFLOP/s.)
 //
 // A key past the sequence's length has P = dS = 0 by selection whatever it
 // holds, and since K is also the other operand of a sum over keys, its rows of K

@@ -232,7 +232,7 @@ __device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8])
 }
 
 // D = rowsum(dO o), 16 lanes per row, 8 elements each (bf16: 16-byte loads), two rows on their way at once.
-// Bound by HBM (196560 rows: 101 MB in 21 us; one row at a time 25).  It clears the status word for the kernels behind it
+// Bound by HBM (196560 rows: 101 MB in 19 us; one row at a time 25).  It clears the status word for the kernels behind it
 // (8 heads x 128 rows: the pass takes 18.2 us to 128 keys, where a memset does that, and 16.2 to 256 keys).
 template <typename T>
 __global__ void __launch_bounds__(256) attention_rowdot_kernel(long long rows, const T* __restrict__ dO,

@@ -29,9 +29,11 @@
 // Keys past the length: their scores are replaced by -inf whatever they are, and
 // their rows of V are zeroed in shared memory (0 x NaN would be NaN).
 //
-// Measured: 40 heads of 75600 rows to 512 keys 684 us (1160 TFLOP/s), 4725 rows to 8192 keys 1440 TFLOP/s; one token, 4
-// x 40 heads on 8, 32760 keys 95 us (5.7 TB/s).  Bound by the tensor pipe, whose 128 x 64 products take 48 cycles instead of
-// 32, and over few keys by the ends of an item (1.6 us); for a single token by HBM.
+// Measured: 40 heads of 75600 rows to 512 keys 680 us (1170 TFLOP/s), of 4725 rows to 8192 keys 530 us (1500 TFLOP/s), 12
+// heads of 8190 rows to 8190 keys 315 us (1310 TFLOP/s); one token, 4 x 40 heads on 8, 32760 keys 94 us (5.7 TB/s).  A
+// single token is bound by HBM.  Else the tensor pipe is 69 % busy (8190 keys), its QK products of 128 x 64 at 3/4 of
+// the full rate; the rest are waits along the chain scores, softmax, PV of each group.  Over 512 keys an
+// item takes 8.7 us: products 5.0, its ends 1.6, and 2.1 that no measurement has placed yet.
 //
 // Warps (384 threads, one persistent CTA per SM): 0-3 softmax and epilogue of
 // group 0, 4-7 of group 1, 8 TMA (Q of both groups, and K, V tiles in one ring of

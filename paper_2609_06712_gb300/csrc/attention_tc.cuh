@@ -18,8 +18,8 @@ cudaError_t launch_attention_dkdv_tc(const AttnShape& s, const AttnArgs& a, cuda
 
 // The item of a persistent CTA's turn: turns of gridDim.x items run forwards and backwards in turn, so that with
 // items sorted by length (causal: the longest first) the CTAs' sums stay close; items or more when there is none.
-// (4095 causal rows x 3 shared heads, 8 key heads: dk and dv 343 us in plain turns, 240 so; dq 138 and 118, the
-// forward 140 and 96, with the rows in falling_tile's order.)
+// (4095 causal rows x 3 shared heads, 8 key heads: dk and dv 343 us in plain turns, 247 so; dq 138 and 123, the
+// forward 140 and 99, with the rows in falling_tile's order.)
 __device__ __forceinline__ int turn_item(int turn, int items)
 {
     const int base = turn * (int)gridDim.x;

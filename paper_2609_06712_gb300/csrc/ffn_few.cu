@@ -2,7 +2,7 @@
 // every weight is read once for all of them, and that is what bounds the work
 // (one token at widths 5120 x 13824: 425 MB of weights, 63 us at the measured
 // 6.8 TB/s, and 72 measured; its 0.4 GFLOP are nothing).  More than 96 tokens go in tiles of at most
-// 96 side by side, which read the weights from L2.
+// 96 side by side, which read the weights from L2 (ffn_few says up to where).
 //
 // The tokens are the N axis and 128 weight rows the M axis of the tensor core,
 // so that a single token costs a tile of 16 columns instead of 128 rows:

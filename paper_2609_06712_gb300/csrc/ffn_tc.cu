@@ -36,9 +36,9 @@
 // row.  (Four warps that staged each piece in shared memory for TMA stores took
 // 371 us for dH at 8190 tokens x 1536 x 4096 where the products need 55.)
 //
-// Measured at 8190 tokens x 1536 x 4096, training: up 171 us (G and U, 268 MB, written beside
-// H), down 72, dH 123 (530 MB through HBM), dX 146, the weights 205; the plain products
-// keep the tensor pipe 70 to 76 % busy (1410 to 1510 TFLOP/s), the last turn of tiles included.
+// Measured at 8190 tokens x 1536 x 4096, training: up 172 us (G and U, 268 MB, written beside
+// H; 125 without them), down 71, dH 120 (530 MB through HBM), dX 143, the weights 200; the plain products
+// keep the tensor pipe 69 to 75 % busy (1440 to 1550 TFLOP/s), the last turn of tiles included.
 //
 // Warp roles (320 threads): warp 0 TMA producer, warp 1 MMA issuer and TMEM
 // owner, warps 2-9 epilogue.  Every mbarrier wait is bounded; a wait that gives

@@ -26,8 +26,12 @@
 // CTA writes one partial row; a second kernel adds the partial rows in a fixed
 // order.  All sums are fp32.
 //
-// Measured, bf16: 75600 x 5120 forward 240 us (6.4 TB/s, 95 % of a copy), backward 381 us
-// (6.1 TB/s); 32760 x 1536 38 and 63 us, where the ramp and the tail count.
+// Measured, bf16: 75600 x 5120 forward 251 us (6.2 TB/s, 91 % of a copy), backward 390 us
+// (6.0 TB/s); 32760 x 1536 39 and 63 us, where the ramp and the tail count.  Rows of 8200 to 16384 elements spill 360
+// bytes a thread in the backward.
+//
+// The variance is taken about the rounded mean, so a common offset of the row does not cancel in it; the mean's own
+// rounding, and with it a shift of x - mu of the order of 2^-24 |mu|, remains.
 #include "block_ops.cuh"
 #include "tcgen05.cuh"
 
