@@ -407,7 +407,8 @@ rola_status_t rola_lowrank_summary_static(const rola_config_t* cfg, const void* 
  * backward pass.  The conventions above hold: device pointers, 16-byte aligned
  * where not said otherwise, densely packed, nothing allocated, asynchronous
  * on `stream`.  Every reduction has a fixed order: the same call gives the same
- * bits.
+ * bits.  Launches go to the current device, where the pointers have to be; calls
+ * of several host threads, each with a workspace of its own, are independent.
  */
 
 /*
