@@ -403,8 +403,8 @@ rola_status_t rola_lowrank_summary_static(const rola_config_t* cfg, const void* 
 /* ------------------------------------------------------------------------
  * The rest of a transformer block around the module: the norm before each
  * sub-layer, softmax attention over a dense key set (cross-attention, a causal
- * sequence, a single new token) and the gated feed-forward, each with its
- * backward pass.  The conventions above hold: device pointers, 16-byte aligned
+ * sequence, a single new token), the gated feed-forward, and the gated residual
+ * sum between two parts of a conditioned block, each with its backward pass.  The conventions above hold: device pointers, 16-byte aligned
  * where not said otherwise, densely packed, nothing allocated, asynchronous
  * on `stream`.  Every reduction has a fixed order: the same call gives the same
  * bits.  Launches go to the current device, where the pointers have to be; calls
@@ -554,6 +554,75 @@ rola_status_t rola_attention(const rola_attention_config_t* cfg, const void* q, 
 rola_status_t rola_attention_backward(const rola_attention_config_t* cfg, const void* q, const void* k, const void* v,
                                       const int32_t* kv_len, const void* o, const float* lse, const void* dO, void* dq,
                                       void* dk, void* dv, void* ws, size_t ws_bytes, void* stream);
+
+/* Which norm, of rola_residual_norm. */
+typedef enum {
+    ROLA_NORM_NONE = 0,
+    ROLA_NORM_LAYER = 1,       /* (v - mean v) / sqrt(mean (v - mean v)^2 + eps) */
+    ROLA_NORM_RMS = 2          /* v / sqrt(mean v^2 + eps) */
+} rola_norm_t;
+
+/* Sizes of a gated residual sum and its norms.  Fill with rola_residual_norm_config_init, then set the sizes. */
+typedef struct {
+    int32_t groups, rows, d;   /* samples, rows (tokens) of each, width; all >= 1, d at most 2^20 */
+    rola_norm_t norm;          /* of the sum, for y; default ROLA_NORM_LAYER.  ROLA_NORM_NONE: no y */
+    rola_norm_t branch_norm;   /* of the branch h; default ROLA_NORM_NONE */
+    int32_t mod_stride;        /* elements from one sample's gate, scale or shift to the next sample's, 0
+                                  (default) or at least d; 0 is d.  They may be slices of one modulation [groups][6 d] */
+    float eps;                 /* of both norms, >= 0; default 1e-6 */
+    rola_dtype_t dtype;        /* ROLA_BF16 (default) or ROLA_FP32 */
+} rola_residual_norm_config_t;
+
+/* Fill *cfg with defaults (sizes zero).  Returns ROLA_ERR_INVALID_ARG on NULL. */
+rola_status_t rola_residual_norm_config_init(rola_residual_norm_config_t* cfg);
+
+/*
+ * The step between two parts of a block: a branch's output joins the residual
+ * stream through its gate, and the sum's norm, scaled and shifted by the sample's
+ * conditioning, is the next part's input.  For row r of sample s:
+ *   a = h, or with branch_norm  a = norm_b(h) gamma_h
+ *   out = x + gate_s a
+ *   y = (norm(out) gamma + beta) (1 + scale_s) + shift_s
+ * in fp32; out and y are rounded once each, y from the sum before its rounding.
+ *   x     : [groups][rows][d], dtype;  h : as x, or NULL: the norm of x alone (out, gate, gamma_h NULL, no branch_norm)
+ *   gate, scale, shift : [groups][d] with mod_stride between the samples, dtype, or NULL (1, 0, 0)
+ *   gamma_h, gamma, beta : [d], dtype, or NULL (1, 1, 0); gamma_h with branch_norm only
+ *   out   : out, as x; may be x or h
+ *   y     : out, as x; may be x or h (not out).  NULL with norm = ROLA_NORM_NONE, as gamma, beta, scale and shift
+ *   stats : out, fp32 [groups][rows][4], 16-byte aligned, or NULL: mean and 1 / size of each row's sum, then of its branch
+ *           (0 where there is no such norm), what the backward pass reads
+ * Tensors need their element's alignment only (with d and mod_stride multiples of 16 bytes and 16-byte aligned
+ * pointers the wide path runs).
+ */
+rola_status_t rola_residual_norm(const rola_residual_norm_config_t* cfg, const void* x, const void* h, const void* gate,
+                                 const void* gamma_h, const void* gamma, const void* beta, const void* scale,
+                                 const void* shift, void* out, void* y, float* stats, void* stream);
+
+/* Bytes of workspace rola_residual_norm_backward needs (256-byte aligned); 0 if cfg is invalid. */
+size_t rola_residual_norm_backward_workspace_bytes(const rola_residual_norm_config_t* cfg);
+
+/*
+ * Gradients of rola_residual_norm from those of out and y.  With hh = norm_b(h) or h, v = norm(out),
+ * a = dy gamma (1 + scale_s), and mean over the row (the terms in brackets belong to the layer norm):
+ *   dx = dout + rstd (a [- mean a] - v mean(a v)),   e = dx gate_s gamma_h
+ *   dh = e, or with branch_norm  rstd_h (e [- mean e] - hh mean(e hh))
+ *   A_s = sum_r dy v,  B_s = sum_r dy,  E_s = sum_r dx hh
+ *   dscale_s = gamma A_s + beta B_s,  dshift_s = B_s,  dgate_s = gamma_h E_s
+ *   dgamma = sum_s (1 + scale_s) A_s,  dbeta = sum_s (1 + scale_s) B_s,  dgamma_h = sum_s gate_s E_s
+ * The sum is formed again from x and h, so nothing is lost to the rounding of out.
+ *   x .. scale, stats : as rola_residual_norm read and wrote them (x and h have to be unchanged)
+ *   dout  : as x, or NULL (0: out is not used further);  dy : as x, or NULL with norm = ROLA_NORM_NONE.  One of them at least
+ *   dx    : out, as x; may be dout or dy;  dh : out, as h; may be dout or dy (not dx); NULL without h
+ *   dgate, dscale, dshift : out, fp32 [groups][d] (dense);  dgamma_h, dgamma, dbeta : out, fp32 [d].  Each may be NULL
+ *           (not wanted); a gradient of gate, gamma_h, gamma, beta or scale asks for its vector
+ * The rows are summed in fp32 per CTA, the CTAs' sums in a fixed order.
+ */
+rola_status_t rola_residual_norm_backward(const rola_residual_norm_config_t* cfg, const void* x, const void* h,
+                                          const void* gate, const void* gamma_h, const void* gamma, const void* beta,
+                                          const void* scale, const float* stats, const void* dout, const void* dy,
+                                          void* dx, void* dh, float* dgate, float* dgamma_h, float* dgamma,
+                                          float* dbeta, float* dscale, float* dshift, void* ws, size_t ws_bytes,
+                                          void* stream);
 
 /*
  * Synchronises `stream`, then reads the device status word at the start of

@@ -1,10 +1,12 @@
 // C ABI entry points of the block operators in include/rola.h (layer norm,
-// gated feed-forward, dense attention): validation, workspace layout, launches.
+// gated feed-forward, dense attention, residual norm): validation, workspace
+// layout, launches.
 #include <limits.h>
 #include <math.h>
 #include <string.h>
 
 #include "block_ops.cuh"
+#include "residual_norm.cuh"
 
 using namespace rola;
 
@@ -198,6 +200,54 @@ AttnWorkspace attn_layout(const AttnShape& s, bool backward)
     return w;
 }
 
+// ---------------------------------------------------------------- residual norm
+
+bool norm_kind(int n) { return n == ROLA_NORM_NONE || n == ROLA_NORM_LAYER || n == ROLA_NORM_RMS; }
+
+rola_status_t validate(const rola_residual_norm_config_t* c)
+{
+    if (!c || c->groups < 1 || c->rows < 1 || c->d < 1 || !norm_kind(c->norm) || !norm_kind(c->branch_norm))
+        return ROLA_ERR_INVALID_ARG;
+    if (c->mod_stride != 0 && c->mod_stride < c->d) return ROLA_ERR_INVALID_ARG;
+    if (!(c->eps >= 0.0f) || !isfinite(c->eps) || (c->dtype != ROLA_BF16 && c->dtype != ROLA_FP32))
+        return ROLA_ERR_INVALID_ARG;
+    if (c->d > (1 << 20) || (int64_t)c->groups * c->rows > ((int64_t)1 << 40) / c->d) return ROLA_ERR_UNSUPPORTED;
+    return ROLA_OK;
+}
+
+RnShape make_shape(const rola_residual_norm_config_t& c)
+{
+    RnShape s;
+    s.groups = c.groups; s.rows = c.rows; s.d = c.d;
+    s.norm = c.norm; s.branch = c.branch_norm;
+    s.mod_stride = c.mod_stride ? c.mod_stride : c.d;
+    s.total = (int64_t)c.groups * c.rows;
+    s.eps = c.eps;
+    return s;
+}
+
+struct RnWorkspace {
+    size_t part, moments, total;
+};
+RnWorkspace rn_layout(const RnShape& s)
+{
+    RnWorkspace w;
+    size_t off = 0;
+    w.part = off; off = align_up(off + sizeof(float) * 3 * (size_t)s.d * ((size_t)rn_parts(s) + s.groups - 1));
+    w.moments = off; off = align_up(off + (rn_long(s) ? sizeof(float4) * (size_t)s.total : 0));
+    w.total = off;
+    return w;
+}
+
+// The vectors that a residual norm's sizes allow: those of the branch with h, those of the norm with a norm.
+bool rn_vectors(const rola_residual_norm_config_t& c, const void* h, const void* gate, const void* gamma_h,
+                const void* gamma, const void* beta, const void* scale, const void* shift)
+{
+    if (!h && (gate || gamma_h || c.branch_norm != ROLA_NORM_NONE || c.norm == ROLA_NORM_NONE)) return false;
+    if (gamma_h && c.branch_norm == ROLA_NORM_NONE) return false;
+    return c.norm != ROLA_NORM_NONE || (!gamma && !beta && !scale && !shift);
+}
+
 }  // namespace
 
 extern "C" {
@@ -228,6 +278,67 @@ rola_status_t rola_layer_norm_backward(int64_t rows, int32_t d, rola_dtype_t dty
     ROLA_CHECK(check_ws(ws, ws_bytes, layer_norm_backward_scratch(rows, d)));
     ROLA_TRY(launch_layer_norm_backward(dtype, rows, d, x, gamma, mean, rstd, dy, dx, dgamma, dbeta,
                                         static_cast<float*>(ws), static_cast<cudaStream_t>(stream)));
+    return ROLA_OK;
+}
+
+rola_status_t rola_residual_norm_config_init(rola_residual_norm_config_t* cfg)
+{
+    if (!cfg) return ROLA_ERR_INVALID_ARG;
+    memset(cfg, 0, sizeof(*cfg));
+    cfg->norm = ROLA_NORM_LAYER;
+    cfg->branch_norm = ROLA_NORM_NONE;
+    cfg->eps = 1e-6f;
+    cfg->dtype = ROLA_BF16;
+    return ROLA_OK;
+}
+
+rola_status_t rola_residual_norm(const rola_residual_norm_config_t* cfg, const void* x, const void* h, const void* gate,
+                                 const void* gamma_h, const void* gamma, const void* beta, const void* scale,
+                                 const void* shift, void* out, void* y, float* stats, void* stream)
+{
+    ROLA_CHECK(validate(cfg));
+    if (!x || !h != !out || (cfg->norm == ROLA_NORM_NONE) != !y || (out && out == y)) return ROLA_ERR_INVALID_ARG;
+    if (!rn_vectors(*cfg, h, gate, gamma_h, gamma, beta, scale, shift)) return ROLA_ERR_INVALID_ARG;
+    if (!aligned(elem(cfg->dtype), x, h, gate, gamma_h, gamma, beta, scale, shift, out, y) || !aligned(16, stats))
+        return ROLA_ERR_INVALID_ARG;
+    RnArgs a{};
+    a.x = x; a.h = h; a.gate = gate; a.gamma_h = gamma_h; a.gamma = gamma; a.beta = beta; a.scale = scale; a.shift = shift;
+    a.out = out; a.y = y; a.stats = stats;
+    ROLA_TRY(launch_residual_norm(cfg->dtype, make_shape(*cfg), a, static_cast<cudaStream_t>(stream)));
+    return ROLA_OK;
+}
+
+size_t rola_residual_norm_backward_workspace_bytes(const rola_residual_norm_config_t* cfg)
+{
+    return validate(cfg) == ROLA_OK ? rn_layout(make_shape(*cfg)).total : 0;
+}
+
+rola_status_t rola_residual_norm_backward(const rola_residual_norm_config_t* cfg, const void* x, const void* h,
+                                          const void* gate, const void* gamma_h, const void* gamma, const void* beta,
+                                          const void* scale, const float* stats, const void* dout, const void* dy,
+                                          void* dx, void* dh, float* dgate, float* dgamma_h, float* dgamma,
+                                          float* dbeta, float* dscale, float* dshift, void* ws, size_t ws_bytes,
+                                          void* stream)
+{
+    ROLA_CHECK(validate(cfg));
+    if (!x || !stats || !dx || !h != !dh || dx == dh || (!dout && !dy) || (cfg->norm == ROLA_NORM_NONE) != !dy)
+        return ROLA_ERR_INVALID_ARG;
+    if (!rn_vectors(*cfg, h, gate, gamma_h, gamma, beta, scale, dshift)) return ROLA_ERR_INVALID_ARG;
+    if ((dgate && !gate) || (dgamma_h && !gamma_h) || (dgamma && !gamma) || (dbeta && !beta) || (dscale && !scale))
+        return ROLA_ERR_INVALID_ARG;
+    if (!aligned(elem(cfg->dtype), x, h, gate, gamma_h, gamma, beta, scale, dout, dy, dx, dh) || !aligned(16, stats) ||
+        !aligned(4, dgate, dgamma_h, dgamma, dbeta, dscale, dshift))
+        return ROLA_ERR_INVALID_ARG;
+    const RnShape s = make_shape(*cfg);
+    const RnWorkspace w = rn_layout(s);
+    ROLA_CHECK(check_ws(ws, ws_bytes, w.total));
+    RnArgs a{};
+    a.x = x; a.h = h; a.gate = gate; a.gamma_h = gamma_h; a.gamma = gamma; a.beta = beta; a.scale = scale;
+    a.stats = const_cast<float*>(stats); a.dout = dout; a.dy = dy; a.dx = dx; a.dh = dh;
+    a.dgate = dgate; a.dgamma_h = dgamma_h; a.dgamma = dgamma; a.dbeta = dbeta; a.dscale = dscale; a.dshift = dshift;
+    a.part = at<float>(ws, w.part);
+    a.moments = at<float4>(ws, w.moments);
+    ROLA_TRY(launch_residual_norm_backward(cfg->dtype, s, a, static_cast<cudaStream_t>(stream)));
     return ROLA_OK;
 }
 

@@ -63,6 +63,12 @@ class RolaAttentionConfig(ctypes.Structure):
     ]
 
 
+class RolaResidualNormConfig(ctypes.Structure):
+    """Mirror of rola_residual_norm_config_t."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("groups", "rows", "d", "norm", "branch_norm", "mod_stride")] + [
+        ("eps", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
 ROLA_DEBUG_SKIP_FIRST_K_COPY = 1
 # rola_lowrank_rope_t: where the truncated RoPE sits in the low-rank features
 ROLA_LOWRANK_ROPE_OUTSIDE, ROLA_LOWRANK_ROPE_INSIDE, ROLA_LOWRANK_ROPE_NONE = 0, 1, 2
@@ -74,6 +80,9 @@ LOWRANK_ACTS = {"silu": ROLA_LOWRANK_ACT_SILU, "identity": ROLA_LOWRANK_ACT_IDEN
 # rola_block_geometry_t: contiguous 64-token chunks, or 4 x 4 x 4 cubes of the latent grid
 ROLA_BLOCK_FLAT, ROLA_BLOCK_CUBE = 0, 1
 BLOCK_GEOMETRIES = {"flat": ROLA_BLOCK_FLAT, "cube": ROLA_BLOCK_CUBE}
+# rola_norm_t: the norms of a residual norm, and the names that its binding takes
+ROLA_NORM_NONE, ROLA_NORM_LAYER, ROLA_NORM_RMS = 0, 1, 2
+NORMS = {"none": ROLA_NORM_NONE, "layer": ROLA_NORM_LAYER, "rms": ROLA_NORM_RMS}
 
 
 class RolaError(RuntimeError):
@@ -91,6 +100,7 @@ def _load():
     I32, I64 = ctypes.c_int32, ctypes.c_int64
     cfgp = ctypes.POINTER(RolaConfig)
     ffnp, attnp = ctypes.POINTER(RolaFfnConfig), ctypes.POINTER(RolaAttentionConfig)
+    rnp = ctypes.POINTER(RolaResidualNormConfig)
     st = ctypes.c_int
     sig = {
         "rola_config_init": (st, [cfgp]),
@@ -125,6 +135,10 @@ def _load():
         "rola_attention_backward_workspace_bytes": (S, [attnp]),
         "rola_attention": (st, [attnp] + [P] * 7 + [S, P]),
         "rola_attention_backward": (st, [attnp] + [P] * 11 + [S, P]),
+        "rola_residual_norm_config_init": (st, [rnp]),
+        "rola_residual_norm": (st, [rnp] + [P] * 12),
+        "rola_residual_norm_backward_workspace_bytes": (S, [rnp]),
+        "rola_residual_norm_backward": (st, [rnp] + [P] * 19 + [S, P]),
         "rola_get_device_status": (st, [P, P]),
         "rola_status_string": (ctypes.c_char_p, [st]),
     }
@@ -464,6 +478,64 @@ def attention_backward(c, q, k, v, kv_len, o, lse, dO, dq, dk, dv, ws, stream=No
          *_ws(ws, w, dev))
 
 
+def make_residual_norm_config(groups: int, rows: int, d: int, norm="layer", branch_norm="none", eps: float = 1e-6,
+                              mod_stride: int = 0, dtype: int = ROLA_BF16) -> RolaResidualNormConfig:
+    """rola_residual_norm_config_t; the norms are names in NORMS or their numbers, mod_stride 0 is d."""
+    c = RolaResidualNormConfig()
+    _lib.rola_residual_norm_config_init(ctypes.byref(c))
+    c.groups, c.rows, c.d, c.eps, c.mod_stride, c.dtype = groups, rows, d, eps, mod_stride, dtype
+    c.norm, c.branch_norm = (NORMS[n] if isinstance(n, str) else int(n) for n in (norm, branch_norm))
+    return c
+
+
+def residual_norm_backward_workspace(c: RolaResidualNormConfig, device="cuda") -> torch.Tensor:
+    return _bytes(_lib.rola_residual_norm_backward_workspace_bytes(c), "rola_residual_norm_backward_workspace_bytes", device)
+
+
+def _mod(t, c, dt, where: str, name: str, dev: int):
+    """The address of a vector of each sample [groups][d], whose samples are c.mod_stride (0: d) elements apart."""
+    if t is None:
+        return None
+    apart = c.mod_stride or c.d
+    if (t.dtype is not dt or t.shape != (c.groups, c.d) or (c.d > 1 and t.stride(1) != 1) or t.get_device() != dev
+            or (c.groups > 1 and t.stride(0) != apart)):
+        raise ValueError(f"{where}: {name} must be a tensor on GPU {dev}, {dt} of shape {(c.groups, c.d)} with strides "
+                         f"{(apart, 1)}, not {t.dtype} {tuple(t.shape)} with {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
+def residual_norm(c, x, h, out, y, *, gate=None, gamma_h=None, gamma=None, beta=None, scale=None, shift=None, stats=None,
+                  stream=None):
+    """out = x + gate a with a = h or norm_b(h) gamma_h, and y = (norm(out) gamma + beta) (1 + scale) + shift.
+    x, h, out, y [groups][rows][d]; gate, scale, shift [groups][d] with c.mod_stride between the samples; gamma_h, gamma,
+    beta [d]; every vector may be None.  h and out None: the norm of x; y None: no norm.  stats (fp32
+    [groups][rows][4]), if given, receives what residual_norm_backward reads."""
+    w, dt, shape, d = "rola_residual_norm", _TORCH_DTYPES.get(c.dtype), (c.groups, c.rows, c.d), (c.d,)
+    dev = _gpu(x, w, "x")
+    _run(_lib.rola_residual_norm, w, dev, stream, c, _a(x, dt, shape, w, "x", dev), _a(h, dt, shape, w, "h", dev),
+         _mod(gate, c, dt, w, "gate", dev), _a(gamma_h, dt, d, w, "gamma_h", dev), _a(gamma, dt, d, w, "gamma", dev),
+         _a(beta, dt, d, w, "beta", dev), _mod(scale, c, dt, w, "scale", dev), _mod(shift, c, dt, w, "shift", dev),
+         _a(out, dt, shape, w, "out", dev), _a(y, dt, shape, w, "y", dev),
+         _a(stats, _F32, shape[:2] + (4,), w, "stats", dev))
+
+
+def residual_norm_backward(c, x, h, stats, dout, dy, dx, dh, ws, *, gate=None, gamma_h=None, gamma=None, beta=None,
+                           scale=None, dgate=None, dgamma_h=None, dgamma=None, dbeta=None, dscale=None, dshift=None,
+                           stream=None):
+    """dx, dh of residual_norm from the gradients dout and dy of its results (None: 0 / no y), and those of its vectors
+    (fp32, dense, in the vectors' shapes; None: not wanted)."""
+    w, dt, shape, d = "rola_residual_norm_backward", _TORCH_DTYPES.get(c.dtype), (c.groups, c.rows, c.d), (c.d,)
+    dev, per = _gpu(x, w, "x"), (c.groups, c.d)
+    _run(_lib.rola_residual_norm_backward, w, dev, stream, c, _a(x, dt, shape, w, "x", dev), _a(h, dt, shape, w, "h", dev),
+         _mod(gate, c, dt, w, "gate", dev), _a(gamma_h, dt, d, w, "gamma_h", dev), _a(gamma, dt, d, w, "gamma", dev),
+         _a(beta, dt, d, w, "beta", dev), _mod(scale, c, dt, w, "scale", dev),
+         _a(stats, _F32, shape[:2] + (4,), w, "stats", dev), _a(dout, dt, shape, w, "dout", dev),
+         _a(dy, dt, shape, w, "dy", dev), _a(dx, dt, shape, w, "dx", dev), _a(dh, dt, shape, w, "dh", dev),
+         _a(dgate, _F32, per, w, "dgate", dev), _a(dgamma_h, _F32, d, w, "dgamma_h", dev),
+         _a(dgamma, _F32, d, w, "dgamma", dev), _a(dbeta, _F32, d, w, "dbeta", dev),
+         _a(dscale, _F32, per, w, "dscale", dev), _a(dshift, _F32, per, w, "dshift", dev), *_ws(ws, w, dev))
+
+
 def get_device_status(ws, stream=None) -> int:
     p = _p(ws)
     with torch.cuda.device(ws.device):
@@ -608,3 +680,59 @@ class AttentionFunction(torch.autograd.Function):
         attention_backward(ctx.c, q, k, v, kv_len, o, lse, dO.contiguous(), dq, dk, dv,
                            attention_backward_workspace(ctx.c, q.device))
         return dq, dk, dv, None, None
+
+
+class ResidualNormFunction(torch.autograd.Function):
+    """The gated residual sum and its norms as a differentiable torch op:
+    ``apply(x, h, gate, gamma_h, gamma, beta, scale, shift, norm, branch_norm, eps)`` returns (out, y).
+
+    x, h [groups, rows, d]; gate, scale, shift [groups, d]; gamma_h, gamma, beta [d]; h and every vector may be None.
+    With h None, out is None; with norm "none", y is None."""
+
+    @staticmethod
+    def forward(ctx, x, h, gate, gamma_h, gamma, beta, scale, shift, norm, branch_norm, eps):
+        B, n, d = x.shape
+        x, h = x.contiguous(), None if h is None else h.contiguous()
+        gamma_h, gamma, beta = (None if t is None else t.contiguous() for t in (gamma_h, gamma, beta))
+        gate, scale, shift, apart = _same_stride((gate, scale, shift), d)
+        c = make_residual_norm_config(B, n, d, norm, branch_norm, eps, apart, _dtype_of(x, "rola_residual_norm"))
+        out = None if h is None else torch.empty_like(x)
+        y = None if c.norm == ROLA_NORM_NONE else torch.empty_like(x)
+        stats = torch.empty((B, n, 4), dtype=torch.float32, device=x.device)
+        residual_norm(c, x, h, out, y, gate=gate, gamma_h=gamma_h, gamma=gamma, beta=beta, scale=scale, shift=shift,
+                      stats=stats)
+        ctx.c, ctx.shifted = c, None if shift is None else shift.dtype
+        ctx.save_for_backward(x, h, gate, gamma_h, gamma, beta, scale, stats)
+        ctx.set_materialize_grads(False)
+        return out, y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout, dy):
+        c = ctx.c
+        x, h, gate, gamma_h, gamma, beta, scale, stats = ctx.saved_tensors
+        if dout is None and dy is None:
+            return (None,) * 11
+        if c.norm != ROLA_NORM_NONE and dy is None:          # out alone was used
+            dy = torch.zeros_like(x)
+        dout, dy = (None if t is None else t.contiguous() for t in (dout, dy))
+        dx, dh = torch.empty_like(x), None if h is None else torch.empty_like(h)
+        want = ctx.needs_input_grad
+        named = dict(dgate=(gate, 2), dgamma_h=(gamma_h, 3), dgamma=(gamma, 4), dbeta=(beta, 5), dscale=(scale, 6))
+        grads = {k: torch.empty(t.shape, dtype=torch.float32, device=x.device) if t is not None and want[i] else None
+                 for k, (t, i) in named.items()}
+        grads["dshift"] = torch.empty((c.groups, c.d), dtype=torch.float32, device=x.device) if want[7] else None
+        residual_norm_backward(c, x, h, stats, dout, dy, dx, dh, residual_norm_backward_workspace(c, x.device), gate=gate,
+                               gamma_h=gamma_h, gamma=gamma, beta=beta, scale=scale, **grads)
+        return (dx, dh, *(None if grads[k] is None else grads[k].to(t.dtype) for k, (t, _) in named.items()),
+                None if grads["dshift"] is None else grads["dshift"].to(ctx.shifted), None, None, None)
+
+
+def _same_stride(vectors, d: int):
+    """Vectors of each sample, as they are where they are slices of one modulation (one distance between the samples of
+    all), else dense; and that distance."""
+    there = [t for t in vectors if t is not None]
+    apart = {t.stride(0) if t.shape[0] > 1 else d for t in there}
+    if len(apart) == 1 and d <= min(apart) < 2 ** 31 and all(t.stride(1) == 1 for t in there):
+        return (*vectors, apart.pop())
+    return (*(None if t is None else t.contiguous() for t in vectors), d)
