@@ -403,10 +403,11 @@ rola_status_t rola_lowrank_summary_static(const rola_config_t* cfg, const void* 
 /* ------------------------------------------------------------------------
  * The rest of a transformer block around the module: the norm before each
  * sub-layer, softmax attention over a dense key set (cross-attention, a causal
- * sequence, a single new token), the gated feed-forward, and the gated residual
- * sum between two parts of a conditioned block, each with its backward pass.  The conventions above hold: device pointers, 16-byte aligned
- * where not said otherwise, densely packed, nothing allocated, asynchronous
- * on `stream`.  Every reduction has a fixed order: the same call gives the same
+ * sequence, a single new token), the gated feed-forward, linear layers with
+ * their epilogue, and the gated residual sum between two parts of a conditioned
+ * block, each with its backward pass.  The conventions above hold: device
+ * pointers, 16-byte aligned where not said otherwise, densely packed, nothing
+ * allocated, asynchronous on `stream`.  Every reduction has a fixed order: the same call gives the same
  * bits.  Launches go to the current device, where the pointers have to be; calls
  * of several host threads, each with a workspace of its own, are independent.
  */
@@ -554,6 +555,55 @@ rola_status_t rola_attention(const rola_attention_config_t* cfg, const void* q, 
 rola_status_t rola_attention_backward(const rola_attention_config_t* cfg, const void* q, const void* k, const void* v,
                                       const int32_t* kv_len, const void* o, const float* lse, const void* dO, void* dq,
                                       void* dk, void* dv, void* ws, size_t ws_bytes, void* stream);
+
+/* Sizes of a linear layer.  Fill with rola_linear_config_init, then set the sizes. */
+typedef struct {
+    int32_t tokens;            /* rows of X, >= 1, at most 2^22 */
+    int32_t d_in, d_out;       /* widths, multiples of 8, at most 2^20 */
+    int32_t act;               /* phi, one of rola_lowrank_act_t; default ROLA_LOWRANK_ACT_IDENTITY */
+    rola_dtype_t dtype;        /* ROLA_BF16 (default) or ROLA_FP32 */
+    int32_t wait_limit_ms;     /* bound of every device-side wait (0 = 2000 ms); at most 60000 */
+    int32_t debug_flags;       /* as rola_ffn_config_t */
+} rola_linear_config_t;
+
+/* Fill *cfg with defaults (sizes zero).  Returns ROLA_ERR_INVALID_ARG on NULL. */
+rola_status_t rola_linear_config_init(rola_linear_config_t* cfg);
+
+/* Bytes of workspace rola_linear / rola_linear_train and rola_linear_backward need (256-byte aligned;
+ * its first bytes hold the status word); 0 if cfg is invalid. */
+size_t rola_linear_workspace_bytes(const rola_linear_config_t* cfg);
+size_t rola_linear_backward_workspace_bytes(const rola_linear_config_t* cfg);
+
+/*
+ * Linear layer with its epilogue, in one kernel:
+ *   Z = X W^T + b,  Y = residual + phi(Z)
+ * The sum over d_in, the bias, phi and the residual are fp32; Y is rounded once.
+ *   X : [tokens][d_in];  W : [d_out][d_in] (the nn.Linear layout);  b : [d_out], or NULL (0), all cfg->dtype
+ *   residual : [tokens][d_out], cfg->dtype, or NULL (0)
+ *   Y : out, [tokens][d_out], cfg->dtype; may be residual, and overlaps no other argument
+ */
+rola_status_t rola_linear(const rola_linear_config_t* cfg, const void* X, const void* W, const void* b,
+                          const void* residual, void* Y, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * rola_linear for training: also writes Z (fp32 [tokens][d_out]), which rola_linear_backward reads.  With the
+ * identity, whose gradient needs no argument, Z may be NULL and is then not written.
+ */
+rola_status_t rola_linear_train(const rola_linear_config_t* cfg, const void* X, const void* W, const void* b,
+                                const void* residual, void* Y, float* Z, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Gradients of rola_linear (that of the residual is dY itself):
+ *   dZ = dY * phi'(Z),  dX = dZ W,  dW = dZ^T X,  db = sum_tokens dZ
+ * phi' of ROLA_LOWRANK_ACT_RELU at 0 is 0.  dZ is rounded once to dtype, as the operand of the products; db is
+ * summed in fp32 before that rounding.
+ *   X, W, Z : as rola_linear_train read and wrote them (Z NULL with the identity);  dY : [tokens][d_out]
+ *   dX : out, [tokens][d_in];  dW : out, [d_out][d_in], both cfg->dtype;  db : out, fp32 [d_out].  Each may be
+ *        NULL (not wanted), not all three
+ */
+rola_status_t rola_linear_backward(const rola_linear_config_t* cfg, const void* X, const void* W, const float* Z,
+                                   const void* dY, void* dX, void* dW, float* db, void* ws, size_t ws_bytes,
+                                   void* stream);
 
 /* Which norm, of rola_residual_norm. */
 typedef enum {

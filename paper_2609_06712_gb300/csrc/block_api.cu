@@ -1,11 +1,12 @@
 // C ABI entry points of the block operators in include/rola.h (layer norm,
-// gated feed-forward, dense attention, residual norm): validation, workspace
-// layout, launches.
+// gated feed-forward, linear layer, dense attention, residual norm): validation,
+// workspace layout, launches.
 #include <limits.h>
 #include <math.h>
 #include <string.h>
 
 #include "block_ops.cuh"
+#include "linear.cuh"
 #include "residual_norm.cuh"
 
 using namespace rola;
@@ -110,6 +111,55 @@ rola_status_t ffn_forward(const rola_ffn_config_t* cfg, const void* X, const voi
         ROLA_TRY(launch_ffn_up_simt(s, X, Wg, Wu, H, G, U, st));
         ROLA_TRY(launch_ffn_down_simt(s, H, Wd, Y, st));
     }
+    return ROLA_OK;
+}
+
+// ---------------------------------------------------------------- linear
+
+rola_status_t validate(const rola_linear_config_t* c)
+{
+    if (!c || c->tokens < 1 || c->d_in < 8 || c->d_out < 8 || c->d_in % 8 || c->d_out % 8) return ROLA_ERR_INVALID_ARG;
+    if (c->dtype != ROLA_BF16 && c->dtype != ROLA_FP32) return ROLA_ERR_INVALID_ARG;
+    if (c->act < ROLA_LOWRANK_ACT_SILU || c->act > ROLA_LOWRANK_ACT_GELU) return ROLA_ERR_INVALID_ARG;
+    if (c->wait_limit_ms < 0 || c->wait_limit_ms > 60000) return ROLA_ERR_INVALID_ARG;
+    if (c->debug_flags & ~ROLA_DEBUG_SKIP_FIRST_K_COPY) return ROLA_ERR_INVALID_ARG;
+    if (c->tokens > (1 << 22) || c->d_in > (1 << 20) || c->d_out > (1 << 20)) return ROLA_ERR_UNSUPPORTED;
+    return ROLA_OK;
+}
+
+LinShape make_shape(const rola_linear_config_t& c)
+{
+    return {c.tokens, c.d_in, c.d_out, c.act, wait_limit_ns(c.wait_limit_ms), c.debug_flags};
+}
+
+struct LinWorkspace {
+    size_t status, dZ, part, total;
+};
+LinWorkspace linear_layout(const rola_linear_config_t& c, bool backward)
+{
+    const LinShape s = make_shape(c);
+    const bool dz = backward && c.act != ROLA_LOWRANK_ACT_IDENTITY;      // else dZ is dY
+    LinWorkspace w;
+    size_t off = 0;
+    w.status = off; off = align_up(off + sizeof(DeviceStatus));
+    w.dZ = off; off = align_up(off + (dz ? elem(c.dtype) * (size_t)s.M * s.N : 0));
+    w.part = off; off = align_up(off + (backward ? 4 * (size_t)linear_grad_parts(s) * s.N : 0));
+    w.total = off;
+    return w;
+}
+
+rola_status_t linear_forward(const rola_linear_config_t* cfg, const void* X, const void* W, const void* b, const void* R,
+                             void* Y, float* Z, void* ws, size_t ws_bytes, void* stream)
+{
+    if (!X || !W || !Y || !aligned(16, X, W, b, R, Y, Z)) return ROLA_ERR_INVALID_ARG;
+    const LinWorkspace w = linear_layout(*cfg, false);
+    ROLA_CHECK(check_ws(ws, ws_bytes, w.total));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    DeviceStatus* status = at<DeviceStatus>(ws, w.status);
+    ROLA_TRY(cudaMemsetAsync(status, 0, sizeof(DeviceStatus), st));
+    const LinShape s = make_shape(*cfg);
+    if (cfg->dtype == ROLA_BF16) ROLA_TRY(launch_linear_tc(s, X, W, b, R, Y, Z, status, st));
+    else ROLA_TRY(launch_linear_simt(s, X, W, b, R, Y, Z, st));
     return ROLA_OK;
 }
 
@@ -396,6 +446,64 @@ rola_status_t rola_ffn_backward(const rola_ffn_config_t* cfg, const void* X, con
     else
         ROLA_TRY(launch_ffn_backward_simt(s, X, W_gate, W_up, W_down, G, U, dY, H, dG, dU, dX, dW_gate, dW_up, dW_down,
                                           st));
+    return ROLA_OK;
+}
+
+rola_status_t rola_linear_config_init(rola_linear_config_t* cfg)
+{
+    if (!cfg) return ROLA_ERR_INVALID_ARG;
+    memset(cfg, 0, sizeof(*cfg));
+    cfg->act = ROLA_LOWRANK_ACT_IDENTITY;
+    cfg->dtype = ROLA_BF16;
+    return ROLA_OK;
+}
+
+size_t rola_linear_workspace_bytes(const rola_linear_config_t* cfg)
+{
+    return validate(cfg) == ROLA_OK ? linear_layout(*cfg, false).total : 0;
+}
+
+size_t rola_linear_backward_workspace_bytes(const rola_linear_config_t* cfg)
+{
+    return validate(cfg) == ROLA_OK ? linear_layout(*cfg, true).total : 0;
+}
+
+rola_status_t rola_linear(const rola_linear_config_t* cfg, const void* X, const void* W, const void* b,
+                          const void* residual, void* Y, void* ws, size_t ws_bytes, void* stream)
+{
+    ROLA_CHECK(validate(cfg));
+    return linear_forward(cfg, X, W, b, residual, Y, nullptr, ws, ws_bytes, stream);
+}
+
+rola_status_t rola_linear_train(const rola_linear_config_t* cfg, const void* X, const void* W, const void* b,
+                                const void* residual, void* Y, float* Z, void* ws, size_t ws_bytes, void* stream)
+{
+    ROLA_CHECK(validate(cfg));
+    if (!Z && cfg->act != ROLA_LOWRANK_ACT_IDENTITY) return ROLA_ERR_INVALID_ARG;
+    return linear_forward(cfg, X, W, b, residual, Y, Z, ws, ws_bytes, stream);
+}
+
+rola_status_t rola_linear_backward(const rola_linear_config_t* cfg, const void* X, const void* W, const float* Z,
+                                   const void* dY, void* dX, void* dW, float* db, void* ws, size_t ws_bytes,
+                                   void* stream)
+{
+    ROLA_CHECK(validate(cfg));
+    const bool identity = cfg->act == ROLA_LOWRANK_ACT_IDENTITY;
+    if (!X || !W || !dY || (!Z && !identity) || (!dX && !dW && !db)) return ROLA_ERR_INVALID_ARG;
+    if (!aligned(16, X, W, Z, dY, dX, dW, db)) return ROLA_ERR_INVALID_ARG;
+    const LinWorkspace w = linear_layout(*cfg, true);
+    ROLA_CHECK(check_ws(ws, ws_bytes, w.total));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const LinShape s = make_shape(*cfg);
+    DeviceStatus* status = at<DeviceStatus>(ws, w.status);
+    ROLA_TRY(cudaMemsetAsync(status, 0, sizeof(DeviceStatus), st));
+    const void* dZ = dY;
+    if (!identity) dZ = at<void>(ws, w.dZ);
+    if (!identity || db)
+        ROLA_TRY(launch_linear_grad(cfg->dtype, s, dY, identity ? nullptr : Z, at<void>(ws, w.dZ), db,
+                                    at<float>(ws, w.part), st));
+    if (cfg->dtype == ROLA_BF16) ROLA_TRY(launch_linear_backward_tc(s, X, W, dZ, dX, dW, status, st));
+    else ROLA_TRY(launch_linear_backward_simt(s, X, W, dZ, dX, dW, st));
     return ROLA_OK;
 }
 

@@ -1,6 +1,7 @@
-// The gated feed-forward's products in plain fp32 arithmetic (no tensor
+// The gated feed-forward's and the linear layer's products in plain fp32 arithmetic (no tensor
 // cores): the fp32 mode.
 //
+//   Y = R + phi(X W^T + b);  dX = dZ W,  dW = dZ^T X
 //   H = phi(X Wg^T) * (X Wu^T),  Y = H Wd^T
 //   dG, dU, H from dH = dY Wd;  dX = dG Wg + dU Wu;  dWg = dG^T X,  dWu = dU^T X,  dWd = dY^T H
 //
@@ -25,13 +26,14 @@
 // meet in a fixed order.
 #include "block_ops.cuh"
 #include "cluster.cuh"
+#include "linear.cuh"
 
 namespace rola {
 namespace {
 
 constexpr int kTile = 128, kStep = 16, kPad = 132;
 
-enum Epilogue { kStore, kGateUp, kGateGrad };
+enum Epilogue { kStore, kGateUp, kGateGrad, kLinear };
 
 // An operand: element (i, k) at p[i * ld + k] (k contiguous) or p[k * ld + i].
 // ld and the contiguous extent are multiples of 8 elements, p is 16-byte aligned.
@@ -44,10 +46,19 @@ struct Operand {
 struct Args {
     int M, N, K, sources, act;
     int ldc;
-    const float *G_in, *U_in;
-    float *G, *U;
+    const float *G_in, *U_in;        // kLinear: the bias and the residual, or NULL
+    float *G, *U;                    // kLinear: Z in G, or NULL
     void *C, *C2, *C3;
 };
+
+// One output of a linear layer from its sum over k.
+__device__ __forceinline__ float finish_linear(const Args& p, size_t at, int n, float z)
+{
+    if (p.G_in) z += p.G_in[n];
+    if (p.G) p.G[at] = z;
+    const float y = gate_act(p.act, z);
+    return p.U_in ? y + p.U_in[at] : y;
+}
 
 // This thread's 8 elements of a 128 x 16 tile: along k, row t / 2 and k = 8 (t % 2); along i, k = t / 16 and
 // rows 8 (t % 16).  Elements outside the operand are 0.
@@ -108,6 +119,10 @@ __device__ __forceinline__ void finish(const Args& p, int m, int n, float4 c, fl
         }
     } else if constexpr (E == kStore) {
         store4(static_cast<float*>(p.C) + at, c);
+    } else if constexpr (E == kLinear) {
+        store4(static_cast<float*>(p.C) + at,
+               make_float4(finish_linear(p, at, n, c.x), finish_linear(p, at + 1, n + 1, c.y),
+                           finish_linear(p, at + 2, n + 2, c.z), finish_linear(p, at + 3, n + 3, c.w)));
     } else {
         const float4 g4 = load4(p.G_in + at), u4 = load4(p.U_in + at);
         const float cc[4] = {c.x, c.y, c.z, c.w}, g[4] = {g4.x, g4.y, g4.z, g4.w}, uu[4] = {u4.x, u4.y, u4.z, u4.w};
@@ -286,6 +301,8 @@ __global__ void __launch_bounds__(256) few_rows_kernel(Operand a, Operand b0, Op
                     p.G[at] = g;
                     p.U[at] = u;
                 }
+            } else if constexpr (E == kLinear) {
+                static_cast<float*>(p.C)[at] = finish_linear(p, at, n0 + f, acc[f][m]);
             } else {
                 static_cast<float*>(p.C)[at] = acc[f][m];
             }
@@ -470,6 +487,34 @@ cudaError_t launch_ffn_backward_simt(const FfnShape& s, const void* X, const voi
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
+}
+
+cudaError_t launch_linear_simt(const LinShape& s, const void* X, const void* W, const void* b, const void* R, void* Y,
+                               float* Z, cudaStream_t st)
+{
+    Args p{};
+    p.M = s.M; p.N = s.N; p.K = s.K; p.sources = 1; p.act = s.act; p.ldc = s.N;
+    p.C = Y; p.G = Z; p.G_in = static_cast<const float*>(b); p.U_in = static_cast<const float*>(R);
+    const Operand x{static_cast<const float*>(X), s.M, s.K}, w{static_cast<const float*>(W), s.N, s.K};
+    return gemm<true, true, kLinear>(x, w, x, w, p, st);
+}
+
+cudaError_t launch_linear_backward_simt(const LinShape& s, const void* X, const void* W, const void* dZ, void* dX,
+                                        void* dW, cudaStream_t st)
+{
+    auto op = [](const void* p, int rows, int ld) { return Operand{static_cast<const float*>(p), rows, ld}; };
+    if (dX) {
+        Args p{};
+        p.M = s.M; p.N = s.K; p.K = s.N; p.sources = 1; p.ldc = s.K; p.C = dX;
+        const Operand dz = op(dZ, s.M, s.N), w = op(W, s.K, s.K);
+        cudaError_t e = gemm<true, false, kStore>(dz, w, dz, w, p, st);
+        if (e != cudaSuccess) return e;
+    }
+    if (!dW) return cudaSuccess;
+    Args p{};                                    // k = token
+    p.M = s.N; p.N = s.K; p.K = s.M; p.sources = 1; p.ldc = s.K; p.C = dW;
+    const Operand dz = op(dZ, s.N, s.N), x = op(X, s.K, s.K);
+    return gemm<false, false, kStore>(dz, x, dz, x, p, st);
 }
 
 }  // namespace rola

@@ -63,6 +63,12 @@ class RolaAttentionConfig(ctypes.Structure):
     ]
 
 
+class RolaLinearConfig(ctypes.Structure):
+    """Mirror of rola_linear_config_t."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "d_in", "d_out", "act", "dtype", "wait_limit_ms",
+                                              "debug_flags")]
+
+
 class RolaResidualNormConfig(ctypes.Structure):
     """Mirror of rola_residual_norm_config_t."""
     _fields_ = [(n, ctypes.c_int32) for n in ("groups", "rows", "d", "norm", "branch_norm", "mod_stride")] + [
@@ -100,7 +106,7 @@ def _load():
     I32, I64 = ctypes.c_int32, ctypes.c_int64
     cfgp = ctypes.POINTER(RolaConfig)
     ffnp, attnp = ctypes.POINTER(RolaFfnConfig), ctypes.POINTER(RolaAttentionConfig)
-    rnp = ctypes.POINTER(RolaResidualNormConfig)
+    rnp, linp = ctypes.POINTER(RolaResidualNormConfig), ctypes.POINTER(RolaLinearConfig)
     st = ctypes.c_int
     sig = {
         "rola_config_init": (st, [cfgp]),
@@ -135,6 +141,12 @@ def _load():
         "rola_attention_backward_workspace_bytes": (S, [attnp]),
         "rola_attention": (st, [attnp] + [P] * 7 + [S, P]),
         "rola_attention_backward": (st, [attnp] + [P] * 11 + [S, P]),
+        "rola_linear_config_init": (st, [linp]),
+        "rola_linear_workspace_bytes": (S, [linp]),
+        "rola_linear_backward_workspace_bytes": (S, [linp]),
+        "rola_linear": (st, [linp] + [P] * 6 + [S, P]),
+        "rola_linear_train": (st, [linp] + [P] * 7 + [S, P]),
+        "rola_linear_backward": (st, [linp] + [P] * 8 + [S, P]),
         "rola_residual_norm_config_init": (st, [rnp]),
         "rola_residual_norm": (st, [rnp] + [P] * 12),
         "rola_residual_norm_backward_workspace_bytes": (S, [rnp]),
@@ -478,6 +490,52 @@ def attention_backward(c, q, k, v, kv_len, o, lse, dO, dq, dk, dv, ws, stream=No
          *_ws(ws, w, dev))
 
 
+def make_linear_config(tokens: int, d_in: int, d_out: int, act="identity", dtype: int = ROLA_BF16) -> RolaLinearConfig:
+    """rola_linear_config_t; act is a name in LOWRANK_ACTS or its number."""
+    c = RolaLinearConfig()
+    _lib.rola_linear_config_init(ctypes.byref(c))
+    c.tokens, c.d_in, c.d_out, c.dtype = tokens, d_in, d_out, dtype
+    c.act = LOWRANK_ACTS[act] if isinstance(act, str) else int(act)
+    return c
+
+
+def linear_workspace(c: RolaLinearConfig, device="cuda") -> torch.Tensor:
+    return _bytes(_lib.rola_linear_workspace_bytes(c), "rola_linear_workspace_bytes", device)
+
+
+def linear_backward_workspace(c: RolaLinearConfig, device="cuda") -> torch.Tensor:
+    return _bytes(_lib.rola_linear_backward_workspace_bytes(c), "rola_linear_backward_workspace_bytes", device)
+
+
+def linear(c, X, W, b, residual, Y, ws, stream=None):
+    """Y = residual + phi(X W^T + b); X [tokens][d_in], W [d_out][d_in], b [d_out] or None, residual (or None) and
+    Y [tokens][d_out]; Y may be residual."""
+    w, dt, m, k, n = "rola_linear", _TORCH_DTYPES.get(c.dtype), c.tokens, c.d_in, c.d_out
+    dev = _gpu(X, w, "X")
+    _run(_lib.rola_linear, w, dev, stream, c, _a(X, dt, (m, k), w, "X", dev), _a(W, dt, (n, k), w, "W", dev),
+         _a(b, dt, (n,), w, "b", dev), _a(residual, dt, (m, n), w, "residual", dev), _a(Y, dt, (m, n), w, "Y", dev),
+         *_ws(ws, w, dev))
+
+
+def linear_train(c, X, W, b, residual, Y, Z, ws, stream=None):
+    """linear keeping Z = X W^T + b (fp32 [tokens][d_out]; None with the identity) for linear_backward."""
+    w, dt, m, k, n = "rola_linear_train", _TORCH_DTYPES.get(c.dtype), c.tokens, c.d_in, c.d_out
+    dev = _gpu(X, w, "X")
+    _run(_lib.rola_linear_train, w, dev, stream, c, _a(X, dt, (m, k), w, "X", dev), _a(W, dt, (n, k), w, "W", dev),
+         _a(b, dt, (n,), w, "b", dev), _a(residual, dt, (m, n), w, "residual", dev), _a(Y, dt, (m, n), w, "Y", dev),
+         _a(Z, _F32, (m, n), w, "Z", dev), *_ws(ws, w, dev))
+
+
+def linear_backward(c, X, W, Z, dY, dX, dW, db, ws, stream=None):
+    """Gradients of linear_train: dX and dW in the tensors' dtype, db (fp32 [d_out]); each may be None (not wanted).  The
+    residual's is dY."""
+    w, dt, m, k, n = "rola_linear_backward", _TORCH_DTYPES.get(c.dtype), c.tokens, c.d_in, c.d_out
+    dev = _gpu(X, w, "X")
+    _run(_lib.rola_linear_backward, w, dev, stream, c, _a(X, dt, (m, k), w, "X", dev), _a(W, dt, (n, k), w, "W", dev),
+         _a(Z, _F32, (m, n), w, "Z", dev), _a(dY, dt, (m, n), w, "dY", dev), _a(dX, dt, (m, k), w, "dX", dev),
+         _a(dW, dt, (n, k), w, "dW", dev), _a(db, _F32, (n,), w, "db", dev), *_ws(ws, w, dev))
+
+
 def make_residual_norm_config(groups: int, rows: int, d: int, norm="layer", branch_norm="none", eps: float = 1e-6,
                               mod_stride: int = 0, dtype: int = ROLA_BF16) -> RolaResidualNormConfig:
     """rola_residual_norm_config_t; the norms are names in NORMS or their numbers, mod_stride 0 is d."""
@@ -680,6 +738,39 @@ class AttentionFunction(torch.autograd.Function):
         attention_backward(ctx.c, q, k, v, kv_len, o, lse, dO.contiguous(), dq, dk, dv,
                            attention_backward_workspace(ctx.c, q.device))
         return dq, dk, dv, None, None
+
+
+class LinearFunction(torch.autograd.Function):
+    """A linear layer with its epilogue as a differentiable torch op: ``apply(X, W, b, residual, act)``;
+    X [..., d_in], residual [..., d_out]; b and residual may be None."""
+
+    @staticmethod
+    def forward(ctx, X, W, b, residual, act):
+        x, W = X.contiguous().view(-1, X.shape[-1]), W.contiguous()
+        c = make_linear_config(x.shape[0], x.shape[1], W.shape[0], act, _dtype_of(x, "rola_linear"))
+        Y = torch.empty((c.tokens, c.d_out), dtype=x.dtype, device=x.device)
+        Z = None
+        if c.act != ROLA_LOWRANK_ACT_IDENTITY:
+            Z = torch.empty((c.tokens, c.d_out), dtype=torch.float32, device=x.device)
+        r = None if residual is None else residual.contiguous().view(-1, residual.shape[-1])
+        linear_train(c, x, W, None if b is None else b.contiguous(), r, Y, Z, linear_workspace(c, x.device))
+        ctx.c, ctx.bias_dtype = c, None if b is None else b.dtype
+        ctx.save_for_backward(x, W, Z)
+        return Y.view(*X.shape[:-1], c.d_out)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dY):
+        c = ctx.c
+        x, W, Z = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dX, dW = (torch.empty_like(t) if need[i] else None for i, t in enumerate((x, W)))
+        db = torch.empty((c.d_out,), dtype=torch.float32, device=x.device) if need[2] else None
+        if any(need[:3]):
+            linear_backward(c, x, W, Z, dY.contiguous().view(c.tokens, c.d_out), dX, dW, db,
+                            linear_backward_workspace(c, x.device))
+        return (None if dX is None else dX.view(*dY.shape[:-1], c.d_in), dW, None if db is None else db.to(ctx.bias_dtype),
+                dY if need[3] else None, None)
 
 
 class ResidualNormFunction(torch.autograd.Function):
