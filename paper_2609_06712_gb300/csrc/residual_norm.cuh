@@ -21,6 +21,7 @@ struct RnArgs {
     float* part;                     // [parts + groups - 1][3][d]: sums of dy v, dy and dx hh over the rows that a part and a sample share
     float4* moments;                 // [total], rows too long for registers: the four means of the backward
     int parts;                       // of the rows
+    const void* in[4];               // the matrices that a kernel streams, or NULL
 };
 
 // Rows [rn_row(i), rn_row(i + 1)) are part i's; part i leaves the sums of sample s in slot i + s.  Parts and samples both
@@ -35,7 +36,7 @@ __host__ __device__ __forceinline__ int rn_part(long long total, int parts, long
 int rn_parts(const RnShape& s);                      // most parts of the backward, for the workspace
 bool rn_long(const RnShape& s);                      // whether the backward takes the rows from memory in several passes
 
-cudaError_t launch_residual_norm(rola_dtype_t dt, const RnShape& s, const RnArgs& a, cudaStream_t st);
+cudaError_t launch_residual_norm(rola_dtype_t dt, const RnShape& s, RnArgs& a, cudaStream_t st);
 cudaError_t launch_residual_norm_backward(rola_dtype_t dt, const RnShape& s, RnArgs& a, cudaStream_t st);
 
 }  // namespace rola
