@@ -277,13 +277,15 @@ RnShape make_shape(const rola_residual_norm_config_t& c)
 }
 
 struct RnWorkspace {
-    size_t part, moments, total;
+    size_t part, shared, moments, total;
 };
 RnWorkspace rn_layout(const RnShape& s)
 {
     RnWorkspace w;
     size_t off = 0;
-    w.part = off; off = align_up(off + sizeof(float) * 3 * (size_t)s.d * ((size_t)rn_parts(s) + s.groups - 1));
+    const size_t slot = sizeof(float) * 3 * (size_t)rn_padded(s.d);
+    w.part = off; off = align_up(off + slot * ((size_t)rn_parts(s) + s.groups - 1));
+    w.shared = off; off = align_up(off + slot * rn_shares(s));
     w.moments = off; off = align_up(off + (rn_long(s) ? sizeof(float4) * (size_t)s.total : 0));
     w.total = off;
     return w;
@@ -387,6 +389,7 @@ rola_status_t rola_residual_norm_backward(const rola_residual_norm_config_t* cfg
     a.stats = const_cast<float*>(stats); a.dout = dout; a.dy = dy; a.dx = dx; a.dh = dh;
     a.dgate = dgate; a.dgamma_h = dgamma_h; a.dgamma = dgamma; a.dbeta = dbeta; a.dscale = dscale; a.dshift = dshift;
     a.part = at<float>(ws, w.part);
+    a.shared = at<float>(ws, w.shared);
     a.moments = at<float4>(ws, w.moments);
     ROLA_TRY(launch_residual_norm_backward(cfg->dtype, s, a, static_cast<cudaStream_t>(stream)));
     return ROLA_OK;

@@ -167,10 +167,11 @@ __global__ void __launch_bounds__(128) rn_columns_kernel(const RnShape sh, const
         B += e.dy;
         E = fmaf(e.t, e.hh, E);
         if (r + 1 == r1 || (r + 1) % sh.rows == 0) {
-            float* out = a.part + (size_t)(part + s) * 3 * sh.d + c;
+            const int dp = rn_padded(sh.d);
+            float* out = a.part + (size_t)(part + s) * 3 * dp + c;
             out[0] = A;
-            out[sh.d] = B;
-            out[2 * (size_t)sh.d] = E;
+            out[dp] = B;
+            out[2 * (size_t)dp] = E;
             A = B = E = 0.0f;
         }
     }
@@ -211,11 +212,11 @@ __host__ __device__ __forceinline__ uint32_t place_bytes(int d, int esz, bool wi
 // memory by bulk copies, one per matrix, with an mbarrier a slot.  A slot is refilled after its row has been read into
 // registers by the whole group.  V = 1: rows that start at any element; they are copied with the whole 16-byte words that
 // they begin and end in, and where such a word is not all inside the matrix (its first and last row) element by element.
-template <typename T, int V, int NV, int N>
+template <typename T, int V, int NV, int N, bool FULL>
 struct Feed {
     long long next, end;
     int tpr, gt, depth, slot, phase;
-    uint32_t ring, bars;
+    uint32_t ring, bars, here, step;     // here: the present slot; step: bytes of a slot
 
     static __device__ __forceinline__ uint32_t place(const RnShape& sh) { return place_bytes(sh.d, sizeof(T), V > 1); }
     static __device__ __forceinline__ int count(const RnArgs& a)
@@ -243,7 +244,7 @@ struct Feed {
     __device__ __forceinline__ void copy(const RnShape& sh, const RnArgs& a, int to)         // one thread
     {
         const uint32_t bar = bars + to * 8, step = place(sh);
-        uint32_t at = ring + to * count(a) * step, bytes = count(a) * step;
+        uint32_t at = ring + to * this->step, bytes = this->step;
         if constexpr (V == 1) {
             bytes = 0;
             uint32_t p = at;
@@ -294,6 +295,8 @@ struct Feed {
     {
         bars = smem_u32(smem) + group * kMaxDepth * 8;
         ring = smem_u32(smem) + (uint32_t)kBarBytes + (uint32_t)(group * depth * count(a)) * place(sh);
+        step = count(a) * place(sh);
+        here = ring;
         next = r0;
         slot = phase = 0;
         if (gt == 0) {
@@ -308,17 +311,16 @@ struct Feed {
         int never = 0;
         return tc::mbar_wait(bars + slot * 8, phase, &never, kWaitLimitNs);
     }
-    // Row r of matrix n (k-th of those there) as fp32, zeros where there is none; NaN where its copy never arrived (the
-    // call has no status word).
-    __device__ __forceinline__ void read(const RnShape& sh, const RnArgs& a, int n, int k, long long r, bool ok,
+    // Row r of matrix n (`skip` bytes into a slot) as fp32, zeros where there is none.
+    __device__ __forceinline__ void read(const RnShape& sh, const RnArgs& a, int n, uint32_t skip, long long r,
                                          float (&v)[NV][V]) const
     {
         const int pieces = sh.d / V;
-        const uint32_t at = ring + (uint32_t)(slot * count(a) + k) * place(sh) + offset(sh, a, n, r);
+        const uint32_t at = here + skip + offset(sh, a, n, r);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = gt + i * tpr;
-            if (a.in[n] && c < pieces) {
+            if (a.in[n] && (FULL || c < pieces)) {
                 if constexpr (V > 1) {
                     Piece<T, V> x;
                     asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n"
@@ -333,7 +335,6 @@ struct Feed {
                     asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(b) : "r"(at + c * 2) : "memory");
                     v[i][0] = __uint_as_float((uint32_t)b << 16);
                 }
-                if (!ok) v[i][0] = __int_as_float(0x7fc00000);
             } else {
 #pragma unroll
                 for (int e = 0; e < V; ++e) v[i][e] = 0.0f;
@@ -343,8 +344,10 @@ struct Feed {
     __device__ __forceinline__ void refill(const RnShape& sh, const RnArgs& a)       // after every thread of the group has read
     {
         if (gt == 0 && next < end) copy(sh, a, slot);
+        here += step;
         if (++slot == depth) {
             slot = 0;
+            here = ring;
             phase ^= 1;
         }
     }
@@ -369,15 +372,79 @@ __device__ __forceinline__ void vec_piece(const void* p, size_t at, float none, 
     }
 }
 
+// Of a row whose copy never arrived (the call has no status word): NaN, in an element of each thread.
+#define kLost __int_as_float(0x7fc00000)
+
+// Sums of N = 1, 2, 4 or 8 values over the threads of a group, the same bits in every thread.  While a lane holds more
+// than one value a step hands half of them to the lane across and takes the others' (8 values take 9 shuffles, not
+// 40).  The warps' sums meet in shared memory, [two buffers][value][warp], zero where there is no warp; `turn`
+// alternates between the buffers, so that a sum's barrier separates its reads from the writes of the sum after the next.
+struct Sums {
+    float buf[2][8][32];
+};
+template <bool WARP, int N>
+__device__ __forceinline__ void sum_group(float (&v)[N], Sums& red, int& turn)
+{
+    constexpr unsigned kAll = 0xffffffffu;
+    const int lane = threadIdx.x & 31;
+    int off = 16;
+#pragma unroll
+    for (int n = N / 2; n >= 1; n >>= 1, off >>= 1) {
+        const bool upper = lane & off;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float mine = upper ? v[i + n] : v[i], other = upper ? v[i] : v[i + n];
+            v[i] = mine + __shfl_xor_sync(kAll, other, off);
+        }
+    }
+    float x = v[0];                                  // of value lane / (32 / N)
+#pragma unroll
+    for (; off >= 1; off >>= 1) x += __shfl_xor_sync(kAll, x, off);
+    constexpr int kLanes = 32 / N;
+    if constexpr (!WARP) {
+        float(&buf)[8][32] = red.buf[turn];
+        turn ^= 1;
+        if (lane % kLanes == 0) buf[lane / kLanes][threadIdx.x >> 5] = x;
+        __syncthreads();
+        const int warps = blockDim.x >> 5;
+        if constexpr (N <= 2) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                v[n] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < 20; w += 4)
+                    if (w < warps) {
+                        const float4 t = *reinterpret_cast<const float4*>(&buf[n][w]);
+                        v[n] += (t.x + t.y) + (t.z + t.w);
+                    }
+            }
+            return;
+        }
+        x = 0.0f;
+        for (int w = lane % kLanes; w < warps; w += kLanes) x += buf[lane / kLanes][w];
+#pragma unroll
+        for (off = kLanes / 2; off >= 1; off >>= 1) x += __shfl_xor_sync(kAll, x, off);
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = __shfl_sync(kAll, x, n * kLanes);
+}
+template <bool WARP>
+__device__ __forceinline__ float sum_group(float a, Sums& red, int& turn)
+{
+    float v[1] = {a};
+    sum_group<WARP, 1>(v, red, turn);
+    return v[0];
+}
+
 // g, c and gate gamma_h of sample s for this thread's pieces.
-template <typename T, int V, int NV, bool SHIFT>
+template <typename T, int V, int NV, bool SHIFT, bool FULL>
 __device__ __forceinline__ void load_vectors(const RnShape& sh, const RnArgs& a, int s, int gt, int tpr, int pieces,
                                              float (&g)[NV][V], float (&c)[NV][V], float (&b)[NV][V])
 {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int p = gt + i * tpr;
-        if (p >= pieces) {
+        if (!FULL && p >= pieces) {
 #pragma unroll
             for (int e = 0; e < V; ++e) g[i][e] = c[i][e] = b[i][e] = 0.0f;
             continue;
@@ -404,63 +471,77 @@ __device__ __forceinline__ void load_vectors(const RnShape& sh, const RnArgs& a,
     }
 }
 
+// x / d for 1 / d rounded: the quotient's remainder once more (of a row of one value the mean is that value, as with the
+// division, which takes some twenty instructions in each thread).
+__device__ __forceinline__ float quotient(float x, int d, float inv_d)
+{
+    const float q = x * inv_d;
+    return fmaf(fmaf(-q, (float)d, x), inv_d, q);
+}
+
 // v = normalised v; returns (mean, 1 / size).  `first` runs after the first barrier: every thread of the group has
 // read its pieces.
-template <bool WARP, int V, int NV, typename F>
-__device__ __forceinline__ float2 normalise(int kind, int d, float eps, int gt, int tpr, int pieces, float (&v)[NV][V],
-                                            float2 (*red)[32], int& turn, F first)
+template <bool WARP, int V, int NV, bool FULL, typename F>
+__device__ __forceinline__ float2 normalise(int kind, int d, float inv_d, float eps, int gt, int tpr, int pieces, float (&v)[NV][V],
+                                            Sums& red, int& turn, F first)
 {
     float mu = 0.0f;
     if (kind == ROLA_NORM_LAYER) {
         float s[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < NV; ++i) sum_piece<V>(s, v[i]);
-        mu = group_sum<WARP>(s[0] + s[1], 0.0f, red, turn).x / (float)d;
+        mu = quotient(sum_group<WARP>(s[0] + s[1], red, turn), d, inv_d);
         first();
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (gt + i * tpr < pieces) fma_piece<V>(v[i], v[i], 1.0f, -mu);
+            if (FULL || gt + i * tpr < pieces) fma_piece<V>(v[i], v[i], 1.0f, -mu);
     }
     float q[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < NV; ++i) dot_piece<V>(q, v[i], v[i]);
-    const float r = 1.0f / sqrtf(group_sum<WARP>(q[0] + q[1], 0.0f, red, turn).x / (float)d + eps);
+    const float r = rsqrtf(fmaf(sum_group<WARP>(q[0] + q[1], red, turn), inv_d, eps));
     if (kind != ROLA_NORM_LAYER) first();
 #pragma unroll
     for (int i = 0; i < NV; ++i) fma_piece<V>(v[i], v[i], r, 0.0f);
     return make_float2(mu, r);
 }
 
-template <typename T, int V, int EL, bool WARP, int TH, int MIN>
+template <typename T, int V, int EL, bool WARP, bool FULL, int TH, int MIN>
 __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
     rn_fwd_kernel(const __grid_constant__ RnShape sh, const __grid_constant__ RnArgs a, int depth)
 {
     constexpr int NV = EL / V;
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ float2 red[2][32];
+    __shared__ __align__(16) Sums red;
     int turn = 0;
+    if constexpr (!WARP)                                 // (the barrier in front of the rows follows)
+        for (int i = threadIdx.x; i < 512; i += blockDim.x) (&red.buf[0][0][0])[i] = 0.0f;
     const int group = WARP ? threadIdx.x >> 5 : 0, part = WARP ? blockIdx.x * kWarpGroups + group : blockIdx.x;
     if (part >= a.parts) return;                         // a whole warp: no barrier of the CTA follows
-    Feed<T, V, NV, 2> q;
+    Feed<T, V, NV, 2, FULL> q;
     q.tpr = WARP ? 32 : blockDim.x;
     q.gt = WARP ? threadIdx.x & 31 : threadIdx.x;
     q.depth = depth;
     q.end = rn_row(sh.total, a.parts, part + 1);
     long long r = rn_row(sh.total, a.parts, part);
     const int pieces = sh.d / V;
+    const uint32_t place = q.place(sh);
     q.start(sh, a, smem, group, r);
+    const float inv_d = 1.0f / (float)sh.d;
+    size_t at = (size_t)r * sh.d;                        // the row's first element
     group_sync<WARP>();                                  // the mbarriers are there
 #pragma unroll 1
     for (int s = (int)(r / sh.rows); r < q.end; ++s) {   // the part's samples, and their rows
         const long long stop = min(q.end, (long long)(s + 1) * sh.rows);
         float g[NV][V], c[NV][V], b[NV][V];
-        load_vectors<T, V, NV, true>(sh, a, s, q.gt, q.tpr, pieces, g, c, b);
+        load_vectors<T, V, NV, true, FULL>(sh, a, s, q.gt, q.tpr, pieces, g, c, b);
 #pragma unroll 1
-        for (; r < stop; ++r) {
+        for (; r < stop; ++r, at += sh.d) {
             const bool ok = q.wait();
             float u[NV][V], hh[NV][V];
-            q.read(sh, a, 0, 0, r, ok, u);
-            q.read(sh, a, 1, 1, r, ok, hh);
+            q.read(sh, a, 0, 0, r, u);
+            q.read(sh, a, 1, place, r, hh);
+            if (!ok) u[0][0] = kLost;
             bool held = true;
             auto refill = [&]() {
                 if (!held) return;
@@ -471,29 +552,29 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
             float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (a.h) {
                 if (sh.branch != ROLA_NORM_NONE) {
-                    const float2 m = normalise<WARP, V, NV>(sh.branch, sh.d, sh.eps, q.gt, q.tpr, pieces, hh, red, turn, refill);
+                    const float2 m = normalise<WARP, V, NV, FULL>(sh.branch, sh.d, inv_d, sh.eps, q.gt, q.tpr, pieces, hh, red, turn, refill);
                     st.z = m.x;
                     st.w = m.y;
                 }
-                T* out = static_cast<T*>(a.out) + r * sh.d;
+                T* out = static_cast<T*>(a.out) + at;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     const int p = q.gt + i * q.tpr;
-                    if (p < pieces) {
+                    if (FULL || p < pieces) {
                         fma_piece<V>(u[i], b[i], hh[i], u[i]);
                         store_piece<T, V>(out + (size_t)p * V, u[i]);
                     }
                 }
             }
             if (sh.norm != ROLA_NORM_NONE) {
-                const float2 m = normalise<WARP, V, NV>(sh.norm, sh.d, sh.eps, q.gt, q.tpr, pieces, u, red, turn, refill);
+                const float2 m = normalise<WARP, V, NV, FULL>(sh.norm, sh.d, inv_d, sh.eps, q.gt, q.tpr, pieces, u, red, turn, refill);
                 st.x = m.x;
                 st.y = m.y;
-                T* y = static_cast<T*>(a.y) + r * sh.d;
+                T* y = static_cast<T*>(a.y) + at;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     const int p = q.gt + i * q.tpr;
-                    if (p < pieces) {
+                    if (FULL || p < pieces) {
                         fma_piece<V>(u[i], u[i], g[i], c[i]);
                         store_piece<T, V>(y + (size_t)p * V, u[i]);
                     }
@@ -508,18 +589,20 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
     }
 }
 
-template <typename T, int V, int EL, bool WARP, int TH, int MIN>
+template <typename T, int V, int EL, bool WARP, bool FULL, int TH, int MIN>
 __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
     rn_bwd_kernel(const __grid_constant__ RnShape sh, const __grid_constant__ RnArgs a, int depth)
 {
     constexpr int NV = EL / V;
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ float2 red[2][32];
+    __shared__ __align__(16) Sums red;
     int turn = 0;
+    if constexpr (!WARP)                                 // (the barrier in front of the rows follows)
+        for (int i = threadIdx.x; i < 512; i += blockDim.x) (&red.buf[0][0][0])[i] = 0.0f;
     const int group = WARP ? threadIdx.x >> 5 : 0, part = WARP ? blockIdx.x * kWarpGroups + group : blockIdx.x;
     if (part >= a.parts) return;
     const bool normed = sh.norm != ROLA_NORM_NONE;
-    Feed<T, V, NV, 4> q;
+    Feed<T, V, NV, 4, FULL> q;
     q.tpr = WARP ? 32 : blockDim.x;
     q.gt = WARP ? threadIdx.x & 31 : threadIdx.x;
     q.depth = depth;
@@ -527,29 +610,32 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
     long long r = rn_row(sh.total, a.parts, part);
     q.start(sh, a, smem, group, r);
     const int pieces = sh.d / V;
-    const int k1 = a.in[0] != nullptr, k2 = k1 + (a.in[1] != nullptr), k3 = k2 + (a.in[2] != nullptr);
+    const uint32_t place = q.place(sh), k1 = a.in[0] ? place : 0, k2 = k1 + (a.in[1] ? place : 0), k3 = k2 + (a.in[2] ? place : 0);
     const float inv_d = 1.0f / (float)sh.d;
+    size_t at = (size_t)r * sh.d;                        // the row's first element
     group_sync<WARP>();                                  // the mbarriers are there
     float4 st = reinterpret_cast<const float4*>(a.stats)[r];
+    if (a.part) asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");       // the sums' kernel, which waits
 #pragma unroll 1
     for (int s = (int)(r / sh.rows); r < q.end; ++s) {   // the part's samples, and their rows
         const long long stop = min(q.end, (long long)(s + 1) * sh.rows);
         float g[NV][V], b[NV][V], A[NV][V], B[NV][V], E[NV][V];
-        load_vectors<T, V, NV, false>(sh, a, s, q.gt, q.tpr, pieces, g, A, b);
+        load_vectors<T, V, NV, false, FULL>(sh, a, s, q.gt, q.tpr, pieces, g, A, b);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int e = 0; e < V; ++e) A[i][e] = B[i][e] = E[i][e] = 0.0f;
 #pragma unroll 1
-        for (; r < stop; ++r) {
+        for (; r < stop; ++r, at += sh.d) {
             const float4 now = st;
             if (r + 1 < q.end) st = reinterpret_cast<const float4*>(a.stats)[r + 1];
             const bool ok = q.wait();
             float v[NV][V], hh[NV][V], dy[NV][V], t[NV][V];
-            q.read(sh, a, 0, 0, r, ok, v);
-            q.read(sh, a, 1, k1, r, ok, hh);
-            q.read(sh, a, 2, k2, r, ok, dy);
-            q.read(sh, a, 3, k3, r, ok, t);
+            q.read(sh, a, 0, 0, r, v);
+            q.read(sh, a, 1, k1, r, hh);
+            q.read(sh, a, 2, k2, r, dy);
+            q.read(sh, a, 3, k3, r, t);
+            if (!ok) t[0][0] = hh[0][0] = kLost;
             bool held = true;
             auto refill = [&]() {
                 if (!held) return;
@@ -560,97 +646,143 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
             if (sh.branch != ROLA_NORM_NONE)
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
-                    if (q.gt + i * q.tpr < pieces) {
+                    if (FULL || q.gt + i * q.tpr < pieces) {
                         fma_piece<V>(hh[i], hh[i], 1.0f, -now.z);
                         fma_piece<V>(hh[i], hh[i], now.w, 0.0f);
                     }
+            // With a norm behind the branch its two sums are of e = b t, t = t0 + k1 + k2 v with t0 = dout + rstd a and
+            // k1, k2 known only after the sums of a and a v.  They are taken apart instead, and all sums are one step:
+            //   sum e = sum b t0 + k1 sum b + k2 sum b v,  sum e hh = sum b hh t0 + k1 sum b hh + k2 sum b hh v
+            float n1 = 0.0f, n2 = 0.0f;                      // mean e (layer norm), mean e hh
             if (normed) {
-                float s1[2] = {0.0f, 0.0f}, s2[2] = {0.0f, 0.0f}, zero[V] = {};
+                float zero[V] = {};
+                const float size[2] = {now.y, now.y};
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
-                    if (q.gt + i * q.tpr < pieces) {
-                        fma_piece<V>(v[i], b[i], hh[i], v[i]);           // the forward's sum, to the bit
+                    if (FULL || q.gt + i * q.tpr < pieces) {
+                        fma_piece<V>(v[i], b[i], hh[i], v[i]);       // the forward's sum, to the bit
                         fma_piece<V>(v[i], v[i], 1.0f, -now.x);
                         fma_piece<V>(v[i], v[i], now.y, 0.0f);
                         fma_piece<V>(A[i], dy[i], v[i], A[i]);
                         add_piece<V>(B[i], dy[i]);
                         fma_piece<V>(dy[i], dy[i], g[i], zero);
-                        sum_piece<V>(s1, dy[i]);
-                        dot_piece<V>(s2, dy[i], v[i]);
+                        if constexpr (V == 1) t[i][0] = fmaf(dy[i][0], now.y, t[i][0]);
+                        else
+#pragma unroll
+                            for (int e = 0; e < V; e += 2) fma2(&t[i][e], &dy[i][e], size, &t[i][e]);
                     }
-                const float2 m = group_sum<WARP>(s1[0] + s1[1], s2[0] + s2[1], red, turn);
-                refill();
-                const float m1 = sh.norm == ROLA_NORM_LAYER ? m.x * inv_d : 0.0f, m2 = m.y * inv_d;
-                const float size[2] = {now.y, now.y};
+                float sa[2] = {0.0f, 0.0f}, sav[2] = {0.0f, 0.0f};
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
-                    fma_piece<V>(v[i], v[i], -m2, -m1);
-                    add_piece<V>(v[i], dy[i]);
-                    if constexpr (V == 1) t[i][0] = fmaf(v[i][0], now.y, t[i][0]);
-                    else
-#pragma unroll
-                        for (int e = 0; e < V; e += 2) fma2(&t[i][e], &v[i][e], size, &t[i][e]);
+                    sum_piece<V>(sa, dy[i]);
+                    dot_piece<V>(sav, dy[i], v[i]);
                 }
+                const bool centred = sh.norm == ROLA_NORM_LAYER, branch_centred = sh.branch == ROLA_NORM_LAYER;
+                float k1, k2;
+                if (sh.branch == ROLA_NORM_NONE) {
+                    float sum[2] = {sa[0] + sa[1], sav[0] + sav[1]};
+                    sum_group<WARP, 2>(sum, red, turn);
+                    k1 = centred ? -now.y * (sum[0] * inv_d) : 0.0f;
+                    k2 = -now.y * (sum[1] * inv_d);
+                } else {
+                    float c[2] = {0.0f, 0.0f}, cv[2] = {0.0f, 0.0f}, w[V];       // sum b hh t0, sum b hh v
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) {
+                        fma_piece<V>(w, b[i], hh[i], zero);
+                        dot_piece<V>(c, w, t[i]);
+                        dot_piece<V>(cv, w, v[i]);
+                    }
+                    if (!centred && !branch_centred) {
+                        float sum[4] = {sav[0] + sav[1], c[0] + c[1], cv[0] + cv[1], 0.0f};
+                        sum_group<WARP, 4>(sum, red, turn);
+                        k1 = 0.0f;
+                        k2 = -now.y * (sum[0] * inv_d);
+                        n2 = fmaf(k2, sum[2], sum[1]) * inv_d;
+                    } else {
+                        float sb[2] = {0.0f, 0.0f}, sbv[2] = {0.0f, 0.0f}, sbt[2] = {0.0f, 0.0f}, sw[2] = {0.0f, 0.0f};
+#pragma unroll
+                        for (int i = 0; i < NV; ++i) {
+                            sum_piece<V>(sb, b[i]);
+                            dot_piece<V>(sbv, b[i], v[i]);
+                            dot_piece<V>(sbt, b[i], t[i]);
+                            dot_piece<V>(sw, b[i], hh[i]);
+                        }
+                        float sum[8] = {sa[0] + sa[1],   sav[0] + sav[1], sbt[0] + sbt[1], sb[0] + sb[1],
+                                        sbv[0] + sbv[1], c[0] + c[1],     sw[0] + sw[1],   cv[0] + cv[1]};
+                        sum_group<WARP, 8>(sum, red, turn);
+                        k1 = centred ? -now.y * (sum[0] * inv_d) : 0.0f;
+                        k2 = -now.y * (sum[1] * inv_d);
+                        n1 = branch_centred ? fmaf(k2, sum[4], fmaf(k1, sum[3], sum[2])) * inv_d : 0.0f;
+                        n2 = fmaf(k2, sum[7], fmaf(k1, sum[6], sum[5])) * inv_d;
+                    }
+                }
+                refill();
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    fma_piece<V>(v[i], v[i], k2, k1);
+                    add_piece<V>(t[i], v[i]);
+                }
+            } else if (sh.branch != ROLA_NORM_NONE) {
+                float zero[V] = {}, w[V], se[2] = {0.0f, 0.0f}, seh[2] = {0.0f, 0.0f};
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    fma_piece<V>(w, b[i], t[i], zero);
+                    sum_piece<V>(se, w);
+                    dot_piece<V>(seh, w, hh[i]);
+                }
+                float sum[2] = {se[0] + se[1], seh[0] + seh[1]};
+                sum_group<WARP, 2>(sum, red, turn);
+                refill();
+                n1 = sh.branch == ROLA_NORM_LAYER ? sum[0] * inv_d : 0.0f;
+                n2 = sum[1] * inv_d;
             }
-            T* dx = static_cast<T*>(a.dx) + r * sh.d;
+            if (held) {                                      // dx may be dout, of which the group has not read all yet
+                group_sync<WARP>();
+                refill();
+            }
+            T* dx = static_cast<T*>(a.dx) + at;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int p = q.gt + i * q.tpr;
-                if (p < pieces) {
+                if (FULL || p < pieces) {
                     fma_piece<V>(E[i], t[i], hh[i], E[i]);
-                    if (held) continue;                      // dx may be dout, of which the group has not read all yet
                     store_piece<T, V>(dx + (size_t)p * V, t[i]);
-                }
-            }
-            if (held) {
-                group_sync<WARP>();
-                refill();
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int p = q.gt + i * q.tpr;
-                    if (p < pieces) store_piece<T, V>(dx + (size_t)p * V, t[i]);
                 }
             }
             if (a.dh) {
                 float zero[V] = {};
-                T* dh = static_cast<T*>(a.dh) + r * sh.d;
-                float s1[2] = {0.0f, 0.0f}, s2[2] = {0.0f, 0.0f};
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (q.gt + i * q.tpr < pieces) {
-                        fma_piece<V>(t[i], t[i], b[i], zero);
-                        sum_piece<V>(s1, t[i]);
-                        dot_piece<V>(s2, t[i], hh[i]);
-                    }
-                if (sh.branch != ROLA_NORM_NONE) {
-                    const float2 m = group_sum<WARP>(s1[0] + s1[1], s2[0] + s2[1], red, turn);
-                    const float m1 = sh.branch == ROLA_NORM_LAYER ? m.x * inv_d : 0.0f, m2 = m.y * inv_d;
-#pragma unroll
-                    for (int i = 0; i < NV; ++i) {
-                        fma_piece<V>(hh[i], hh[i], -m2, -m1);
-                        add_piece<V>(t[i], hh[i]);
-                        fma_piece<V>(t[i], t[i], now.w, 0.0f);
-                    }
-                }
+                T* dh = static_cast<T*>(a.dh) + at;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     const int p = q.gt + i * q.tpr;
-                    if (p < pieces) store_piece<T, V>(dh + (size_t)p * V, t[i]);
+                    if (FULL || p < pieces) {
+                        fma_piece<V>(t[i], t[i], b[i], zero);
+                        if (sh.branch != ROLA_NORM_NONE) {
+                            fma_piece<V>(hh[i], hh[i], -n2, -n1);
+                            add_piece<V>(t[i], hh[i]);
+                            fma_piece<V>(t[i], t[i], now.w, 0.0f);
+                        }
+                        store_piece<T, V>(dh + (size_t)p * V, t[i]);
+                    }
                 }
             }
         }
         if (a.part) {
-            float* out = a.part + (size_t)(part + s) * 3 * sh.d;
+            const int dp = rn_padded(sh.d);
+            float* out = a.part + (size_t)(part + s) * 3 * dp;
+            auto store = [&](float* to, const float(&x)[V]) {
+                if constexpr (V == 1) to[0] = x[0];
+                else
+#pragma unroll
+                    for (int e = 0; e < V; e += 4) store4(to + e, make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]));
+            };
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int p = q.gt + i * q.tpr;
-                if (p < pieces)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        out[(size_t)p * V + e] = A[i][e];
-                        out[sh.d + (size_t)p * V + e] = B[i][e];
-                        out[2 * (size_t)sh.d + (size_t)p * V + e] = E[i][e];
-                    }
+                const int p = (q.gt + i * q.tpr) * V;
+                if (!FULL && p >= sh.d) continue;
+                store(out + p, A[i]);
+                store(out + dp + p, B[i]);
+                store(out + 2 * dp + p, E[i]);
             }
         }
     }
@@ -658,69 +790,109 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
 
 // ---------------------------------------------------------------- column sums to gradients
 
-// The vectors' gradients from the parts' sums.  A CTA takes 32 columns; its 32 warps share the samples, 32 / ways of
-// them at a time, `ways` warps to a sample, which add every ways-th of its slots.  The warps' sums meet in warp order,
-// the samples' in sample order within a warp, then in warp order: the same bits every time.
-template <typename T>
-__global__ void __launch_bounds__(1024) rn_reduce_kernel(const RnShape sh, const RnArgs a, int ways)
+constexpr int kReduceWarps = 16;
+
+__device__ __forceinline__ float4 operator+(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
+__device__ __forceinline__ float4 shuffled(float4 a, int off)
 {
-    __shared__ float sum[3][32][33];
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-    const int at_once = 32 / ways, way = w % ways;
-    const bool in = c < sh.d;
-    float dgamma = 0.0f, dbeta = 0.0f, dgamma_h = 0.0f;
-    const float gamma = in ? vec<T>(a.gamma, c, 1.0f) : 0.0f, beta = in ? vec<T>(a.beta, c, 0.0f) : 0.0f;
-    const float gamma_h = in ? vec<T>(a.gamma_h, c, 1.0f) : 0.0f;
-    for (int s0 = 0; s0 < sh.groups; s0 += at_once) {
+    constexpr unsigned kAll = 0xffffffffu;
+    return make_float4(__shfl_xor_sync(kAll, a.x, off), __shfl_xor_sync(kAll, a.y, off), __shfl_xor_sync(kAll, a.z, off),
+                       __shfl_xor_sync(kAll, a.w, off));
+}
+
+// The vectors' gradients from the parts' sums.  A CTA takes 32 columns, four a lane, and of grid y = 0 the sums A and B, of
+// 1 the sums E; grid z shares the samples out.  A warp's four groups of eight lanes and `ways` warps share the slots of a
+// sample, 16 / ways samples at a time.  They meet in a fixed order, as do the samples: the same bits every time.  What
+// is summed over the samples goes to `shared` [z][3][dp] where there is more than one z.
+// It is launched while the rows' kernel runs and waits for it (programmatic dependent launch).
+template <typename T>
+__global__ void __launch_bounds__(32 * kReduceWarps) rn_reduce_kernel(const __grid_constant__ RnShape sh,
+                                                                      const __grid_constant__ RnArgs a, int ways)
+{
+    __shared__ float4 sum[2][kReduceWarps][8];
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, quad = lane & 7;
+    const int c = blockIdx.x * 32 + quad * 4, dp = rn_padded(sh.d), at_once = kReduceWarps / ways, way = w % ways;
+    const bool branch = blockIdx.y + (a.norm_sums ? 0 : 1) == 1;
+    const int s_begin = (int)((long long)sh.groups * blockIdx.z / gridDim.z);
+    const int s_end = (int)((long long)sh.groups * (blockIdx.z + 1) / gridDim.z);
+    float4 total[2] = {};                                // over the samples: of (1 + scale) A and (1 + scale) B, or of gate E
+    for (int s0 = s_begin; s0 < s_end; s0 += at_once) {
         const int s = s0 + w / ways;
-        float A = 0.0f, B = 0.0f, E = 0.0f;
-        if (s < sh.groups && in) {
+        float4 x[2] = {};
+        if (s < s_end && c < sh.d) {
             const int lo = rn_part(sh.total, a.parts, (long long)s * sh.rows);
             const int hi = rn_part(sh.total, a.parts, (long long)(s + 1) * sh.rows - 1);
 #pragma unroll 4
-            for (int i = lo + way; i <= hi; i += ways) {
-                const float* p = a.part + (size_t)(i + s) * 3 * sh.d + c;
-                A += p[0];
-                B += p[sh.d];
-                E += p[2 * (size_t)sh.d];
+            for (int i = lo + way * 4 + (lane >> 3); i <= hi; i += ways * 4) {
+                const float* p = a.part + (size_t)(i + s) * 3 * dp + c;
+                x[0] = x[0] + *reinterpret_cast<const float4*>(p + (branch ? 2 * dp : 0));
+                if (!branch) x[1] = x[1] + *reinterpret_cast<const float4*>(p + dp);
             }
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            x[n] = x[n] + shuffled(x[n], 8);
+            x[n] = x[n] + shuffled(x[n], 16);
         }
         if (ways > 1) {
             __syncthreads();                             // the last samples' sums have been read
-            sum[0][w][lane] = A;
-            sum[1][w][lane] = B;
-            sum[2][w][lane] = E;
+            if (lane < 8)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) sum[n][w][quad] = x[n];
             __syncthreads();
             if (way == 0)
-                for (int i = 1; i < ways; ++i) {
-                    A += sum[0][w + i][lane];
-                    B += sum[1][w + i][lane];
-                    E += sum[2][w + i][lane];
-                }
+                for (int i = 1; i < ways; ++i)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) x[n] = x[n] + sum[n][w + i][quad];
         }
-        if (way == 0 && s < sh.groups && in) {
-            const size_t at = (size_t)s * sh.d + c, mod = (size_t)(s * sh.mod_stride + c);
-            if (a.dscale) a.dscale[at] = fmaf(gamma, A, beta * B);
-            if (a.dshift) a.dshift[at] = B;
-            if (a.dgate) a.dgate[at] = gamma_h * E;
-            const float s1 = 1.0f + vec<T>(a.scale, mod, 0.0f);
-            dgamma = fmaf(s1, A, dgamma);
-            dbeta = fmaf(s1, B, dbeta);
-            dgamma_h = fmaf(vec<T>(a.gate, mod, 1.0f), E, dgamma_h);
+        if (way == 0 && s < s_end && lane < 8) {
+            const float A[4] = {x[0].x, x[0].y, x[0].z, x[0].w}, B[4] = {x[1].x, x[1].y, x[1].z, x[1].w};
+            float tA[4] = {total[0].x, total[0].y, total[0].z, total[0].w}, tB[4] = {total[1].x, total[1].y, total[1].z, total[1].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (c + e >= sh.d) break;
+                const size_t at = (size_t)s * sh.d + c + e, mod = (size_t)(s * sh.mod_stride + c + e);
+                if (branch) {
+                    if (a.dgate) a.dgate[at] = vec<T>(a.gamma_h, c + e, 1.0f) * A[e];
+                    tA[e] = fmaf(vec<T>(a.gate, mod, 1.0f), A[e], tA[e]);
+                } else {
+                    if (a.dscale) a.dscale[at] = fmaf(vec<T>(a.gamma, c + e, 1.0f), A[e], vec<T>(a.beta, c + e, 0.0f) * B[e]);
+                    if (a.dshift) a.dshift[at] = B[e];
+                    const float s1 = 1.0f + vec<T>(a.scale, mod, 0.0f);
+                    tA[e] = fmaf(s1, A[e], tA[e]);
+                    tB[e] = fmaf(s1, B[e], tB[e]);
+                }
+            }
+            total[0] = make_float4(tA[0], tA[1], tA[2], tA[3]);
+            total[1] = make_float4(tB[0], tB[1], tB[2], tB[3]);
         }
     }
     if (!a.dgamma && !a.dbeta && !a.dgamma_h) return;
     __syncthreads();
-    sum[0][w][lane] = dgamma;
-    sum[1][w][lane] = dbeta;
-    sum[2][w][lane] = dgamma_h;
+    if (lane < 8)
+#pragma unroll
+        for (int n = 0; n < 2; ++n) sum[n][w][quad] = total[n];      // warps whose way is not 0 hold zeros
     __syncthreads();
-    if (w < 3 && in) {                                   // warps whose way is not 0 hold zeros
-        float total = 0.0f;
-        for (int i = 0; i < 32; i += ways) total += sum[w][i][lane];
-        float* out = w == 0 ? a.dgamma : w == 1 ? a.dbeta : a.dgamma_h;
-        if (out) out[c] = total;
-    }
+    const int n = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+    if (n >= (branch ? 1 : 2) || col >= sh.d) return;
+    float t = 0.0f;
+    for (int i = 0; i < kReduceWarps; i += ways) t += reinterpret_cast<const float*>(&sum[n][i][0])[lane];
+    float* out = branch ? a.dgamma_h : n ? a.dbeta : a.dgamma;
+    if (gridDim.z > 1) a.shared[((size_t)blockIdx.z * 3 + (branch ? 2 : n)) * dp + col] = t;
+    else if (out) out[col] = t;
+}
+
+// dgamma, dbeta, dgamma_h from the sums over each z's samples.
+__global__ void __launch_bounds__(128) rn_shared_kernel(const __grid_constant__ RnShape sh, const __grid_constant__ RnArgs a, int z)
+{
+    const int c = blockIdx.x * 128 + threadIdx.x, n = blockIdx.y, dp = rn_padded(sh.d);
+    float* out = n == 0 ? a.dgamma : n == 1 ? a.dbeta : a.dgamma_h;
+    if (c >= sh.d || !out) return;
+    float t = 0.0f;
+#pragma unroll 4
+    for (int i = 0; i < z; ++i) t += a.shared[((size_t)i * 3 + n) * dp + c];
+    out[c] = t;
 }
 
 // ---------------------------------------------------------------- dispatch
@@ -730,7 +902,7 @@ int long_grid(long long rows) { return (int)(rows < 608 ? rows : 608); }     // 
 bool wants_sums(const RnArgs& a) { return a.dgate || a.dgamma_h || a.dgamma || a.dbeta || a.dscale || a.dshift; }
 
 constexpr int kMostParts = 4864, kMostCtas = 1216;       // of warps, of CTAs: 32 and 8 on each of 152 SMs
-constexpr int kFwdRegisters = 16384, kBwdRegisters = 8192;       // longest rows that are held in registers
+constexpr int kFwdRegisters = 16384, kBwdRegisters = 8192;       // longest rows held in registers (forward, single elements: 8192)
 
 // Whether every row, and every vector, can be taken in 16-byte pieces.
 bool wide(const RnShape& s, const RnArgs& a, int esz)
@@ -750,7 +922,10 @@ cudaError_t sm_count(int* n)
     return cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
 }
 
-// Threads, parts, ring depth and shared memory of a launch: `ctas` of them fit an SM's registers.
+// Registers of a thread that let `ctas` CTAs of `threads` onto an SM: its four sub-partitions hold 512 of a warp's each.
+constexpr int registers_of(int threads, int ctas) { return 512 / ((threads / 32 * ctas + 3) / 4) / 8 * 8; }
+
+// Threads, parts, ring depth and shared memory of a launch.
 struct Launch {
     int threads, grid, parts, depth;
     size_t smem;
@@ -763,7 +938,7 @@ cudaError_t shape_of(K kernel, const RnShape& s, bool warp, int el, int register
     if (e != cudaSuccess) return e;
     const int groups = warp ? kWarpGroups : 1;
     l->threads = warp ? 32 * kWarpGroups : ((s.d + el - 1) / el + 31) / 32 * 32;
-    int ctas = 65536 / (registers * l->threads);
+    int ctas = 512 / registers * 4 / (l->threads / 32);
     ctas = ctas < 1 ? 1 : ctas > 8 ? 8 : ctas;
     while (ctas > 1 && groups * row_bytes * 2 * ctas > kRingBytes) --ctas;       // two rows a group at least, if they fit
     long long parts = (long long)nsm * ctas * groups;
@@ -781,13 +956,15 @@ cudaError_t shape_of(K kernel, const RnShape& s, bool warp, int el, int register
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kRingBytes + kBarBytes));
 }
 
-template <typename T, int V, int EL, bool WARP, int TH, int MIN>
+template <typename T, int V, int EL, bool WARP, int TH, int MIN, bool FULL = false>
 cudaError_t fwd_one(const RnShape& s, RnArgs& a, cudaStream_t st)
 {
+    if constexpr (V > 1 && !WARP && !FULL)
+        if (s.d % (32 * EL) == 0) return fwd_one<T, V, EL, WARP, TH, MIN, true>(s, a, st);
     Launch l;
-    auto kernel = rn_fwd_kernel<T, V, EL, WARP, TH, MIN>;
+    auto kernel = rn_fwd_kernel<T, V, EL, WARP, FULL, TH, MIN>;
     const size_t row = (size_t)place_bytes(s.d, sizeof(T), V > 1) * (a.h ? 2 : 1);
-    cudaError_t e = shape_of(kernel, s, WARP, EL, 65536 / (TH * MIN) / 8 * 8, row, 1ll << 30, &l);
+    cudaError_t e = shape_of(kernel, s, WARP, EL, registers_of(TH, MIN), row, 1ll << 30, &l);
     if (e != cudaSuccess) return e;
     a.in[0] = a.x;
     a.in[1] = a.h;
@@ -795,14 +972,16 @@ cudaError_t fwd_one(const RnShape& s, RnArgs& a, cudaStream_t st)
     kernel<<<l.grid, l.threads, l.smem, st>>>(s, a, l.depth);
     return cudaGetLastError();
 }
-template <typename T, int V, int EL, bool WARP, int TH, int MIN>
+template <typename T, int V, int EL, bool WARP, int TH, int MIN, bool FULL = false>
 cudaError_t bwd_one(const RnShape& s, RnArgs& a, cudaStream_t st)
 {
+    if constexpr (V > 1 && !WARP && !FULL)
+        if (s.d % (32 * EL) == 0) return bwd_one<T, V, EL, WARP, TH, MIN, true>(s, a, st);
     Launch l;
-    auto kernel = rn_bwd_kernel<T, V, EL, WARP, TH, MIN>;
+    auto kernel = rn_bwd_kernel<T, V, EL, WARP, FULL, TH, MIN>;
     const int matrices = (s.norm != ROLA_NORM_NONE ? 1 : 0) + (a.h ? 1 : 0) + (a.dy ? 1 : 0) + (a.dout ? 1 : 0);
     const size_t row = (size_t)place_bytes(s.d, sizeof(T), V > 1) * matrices;
-    cudaError_t e = shape_of(kernel, s, WARP, EL, 65536 / (TH * MIN) / 8 * 8, row, rn_parts(s), &l);
+    cudaError_t e = shape_of(kernel, s, WARP, EL, registers_of(TH, MIN), row, rn_parts(s), &l);
     if (e != cudaSuccess) return e;
     a.in[0] = s.norm != ROLA_NORM_NONE ? a.x : nullptr;
     a.in[1] = a.h;
@@ -813,16 +992,20 @@ cudaError_t bwd_one(const RnShape& s, RnArgs& a, cudaStream_t st)
     return cudaGetLastError();
 }
 
-// A warp a row up to 16 elements a lane, then a CTA a row of the least whole number of warps.
+// A warp a row up to 16 elements a lane, then a CTA a row of the least whole number of warps, 16 elements a thread: with
+// 8 the work that a warp does once a row counts twice (2 x 16380 x 1536: backward 133 us with 8, 118 with 16; forward
+// 76 either way, 1024 wide 68 and 54).  The register limit is that of 16 warps an SM forward (12 or 10 backward).
 template <typename T, int V>
 cudaError_t fwd(const RnShape& s, RnArgs& a, cudaStream_t st)
 {
     if (s.d <= 256) return fwd_one<T, V, 8, true, 128, 6>(s, a, st);
     if (s.d <= 512) return fwd_one<T, V, 16, true, 128, 4>(s, a, st);
-    if (s.d <= 8 * 256) return fwd_one<T, V, 8, false, 256, 3>(s, a, st);
-    if (s.d <= 16 * 320) return fwd_one<T, V, 16, false, 320, 2>(s, a, st);
+    constexpr int kFewer = V == 1;                   // CTAs: addresses of single elements take more registers
+    if (s.d <= 16 * 160) return fwd_one<T, V, 16, false, 160, 3 - kFewer>(s, a, st);
+    if (s.d <= 16 * 320) return fwd_one<T, V, 16, false, 320, 2 - kFewer>(s, a, st);
     if (s.d <= 16 * 512) return fwd_one<T, V, 16, false, 512, 1>(s, a, st);
-    if (s.d <= kFwdRegisters) return fwd_one<T, V, 32, false, 512, 1>(s, a, st);
+    if constexpr (V > 1)
+        if (s.d <= kFwdRegisters) return fwd_one<T, V, 32, false, 512, 1>(s, a, st);
     rn_fwd_long_kernel<T><<<long_grid(s.total), kLongThreads, 0, st>>>(s, a);
     return cudaGetLastError();
 }
@@ -832,8 +1015,7 @@ cudaError_t bwd(const RnShape& s, RnArgs& a, cudaStream_t st)
 {
     if (s.d <= 256) return bwd_one<T, V, 8, true, 128, 4>(s, a, st);
     if (s.d <= 512) return bwd_one<T, V, 16, true, 128, 2>(s, a, st);
-    if (s.d <= 8 * 320) return bwd_one<T, V, 8, false, 320, 2>(s, a, st);
-    if (s.d <= 8 * 640) return bwd_one<T, V, 8, false, 640, 1>(s, a, st);
+    if (s.d <= 16 * 320) return bwd_one<T, V, 16, false, 320, 1>(s, a, st);
     if (s.d <= kBwdRegisters) return bwd_one<T, V, 16, false, 512, 1>(s, a, st);
     a.parts = rn_parts(s);
     rn_moments_kernel<T><<<long_grid(s.total), kLongThreads, 0, st>>>(s, a);
@@ -849,9 +1031,23 @@ cudaError_t backward(const RnShape& s, RnArgs& a, cudaStream_t st)
     if (!sums) a.part = nullptr;
     cudaError_t e = wide(s, a, sizeof(T)) ? bwd<T, 16 / sizeof(T)>(s, a, st) : bwd<T, 1>(s, a, st);
     if (e != cudaSuccess || !sums) return e;
-    int ways = 32;
-    while (ways > 1 && ways * s.groups > 32) ways /= 2;
-    rn_reduce_kernel<T><<<(s.d + 31) / 32, 1024, 0, st>>>(s, a, ways);
+    a.norm_sums = a.dgamma || a.dbeta || a.dscale || a.dshift;
+    const bool branch_sums = a.dgate || a.dgamma_h, shared = a.dgamma || a.dbeta || a.dgamma_h;
+    int ways = kReduceWarps;
+    while (ways > 1 && ways * s.groups > kReduceWarps) ways /= 2;
+    const int z = rn_shares(s), columns = (s.d + 31) / 32;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(columns, a.norm_sums && branch_sums ? 2 : 1, z);
+    cfg.blockDim = dim3(32 * kReduceWarps);
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, rn_reduce_kernel<T>, s, static_cast<const RnArgs&>(a), ways);
+    if (e != cudaSuccess || z == 1 || !shared) return e;
+    rn_shared_kernel<<<dim3((s.d + 127) / 128, 3), 128, 0, st>>>(s, a, z);
     return cudaGetLastError();
 }
 
@@ -861,6 +1057,13 @@ int rn_parts(const RnShape& s)
 {
     const long long want = (s.total + 1) / 2, most = s.d <= 512 ? kMostParts : kMostCtas;
     return (int)(want < most ? want : most);
+}
+
+int rn_shares(const RnShape& s)
+{
+    // 64 samples a share at least, and no more CTAs than 4 on each of 152 SMs
+    const int columns = (s.d + 31) / 32, most = (608 + columns - 1) / columns, want = (s.groups + 63) / 64;
+    return want < most ? want : most;
 }
 
 bool rn_long(const RnShape& s) { return s.d > kBwdRegisters; }

@@ -18,10 +18,12 @@ struct RnArgs {
     void *out, *y, *dx, *dh;
     float* stats;                    // [total][4]: mean, rstd of the sum; mean, rstd of the branch
     float *dgate, *dgamma_h, *dgamma, *dbeta, *dscale, *dshift;
-    float* part;                     // [parts + groups - 1][3][d]: sums of dy v, dy and dx hh over the rows that a part and a sample share
+    float* part;                     // [parts + groups - 1][3][rn_padded(d)]: sums of dy v, dy and dx hh over the rows that a part and a sample share
+    float* shared;                   // [rn_shares][3][rn_padded(d)]: of the vectors that all samples share
     float4* moments;                 // [total], rows too long for registers: the four means of the backward
     int parts;                       // of the rows
     const void* in[4];               // the matrices that a kernel streams, or NULL
+    int norm_sums;                   // whether the norm's vectors have a gradient that is wanted
 };
 
 // Rows [rn_row(i), rn_row(i + 1)) are part i's; part i leaves the sums of sample s in slot i + s.  Parts and samples both
@@ -33,6 +35,9 @@ __host__ __device__ __forceinline__ int rn_part(long long total, int parts, long
     return (int)(((r + 1) * parts - 1) / total);
 }
 
+__host__ __device__ __forceinline__ int rn_padded(int d) { return (d + 3) / 4 * 4; }
+
+int rn_shares(const RnShape& s);                     // shares of the samples in the sums over them
 int rn_parts(const RnShape& s);                      // most parts of the backward, for the workspace
 bool rn_long(const RnShape& s);                      // whether the backward takes the rows from memory in several passes
 
