@@ -5,6 +5,8 @@
 //   a = dy g,  t = dout + rstd (a [- mean a] - v mean(a v)),  dx = t
 //   e = t gate gamma_h,  dh = rstd_h (e [- mean e] - hh mean(e hh)) or e
 //   column sums of each sample: A = sum dy v, B = sum dy, E = sum t hh; every vector's gradient is made of them.
+#include <type_traits>
+
 #include "norm_rows.cuh"
 #include "residual_norm.cuh"
 #include "tcgen05.cuh"
@@ -201,6 +203,15 @@ constexpr size_t kRingBytes = 208 << 10;             // of the rings of an SM's 
 constexpr size_t kBarBytes = kWarpGroups * kMaxDepth * 8;
 constexpr uint64_t kWaitLimitNs = 2000000000ull;     // bound of the wait for a row
 
+// The elements of piece i of a thread's EL.
+template <int V, int EL>
+__device__ __forceinline__ float (&slice(float (&v)[EL], int i))[V] { return reinterpret_cast<float(&)[V]>(v[i * V]); }
+
+// Pieces are 16 bytes where every row starts at a multiple of them, else one element, or two of bf16 where the width
+// and the pointers allow 4 bytes.
+template <typename T, int V>
+constexpr bool kWide = V * sizeof(T) == 16;
+
 // Bytes of a row's place in the ring: a row that starts anywhere is copied with the 16-byte words that it begins and
 // ends in.
 __host__ __device__ __forceinline__ uint32_t place_bytes(int d, int esz, bool wide)
@@ -210,15 +221,15 @@ __host__ __device__ __forceinline__ uint32_t place_bytes(int d, int esz, bool wi
 
 // A group's rows [next, end) of the matrices a.in (those that are not NULL), brought ahead into `depth` slots of shared
 // memory by bulk copies, one per matrix, with an mbarrier a slot.  A slot is refilled after its row has been read into
-// registers by the whole group.  V = 1: rows that start at any element; they are copied with the whole 16-byte words that
+// registers by the whole group.  Pieces of less than 16 bytes: rows that start at any element; they are copied with the whole 16-byte words that
 // they begin and end in, and where such a word is not all inside the matrix (its first and last row) element by element.
-template <typename T, int V, int NV, int N, bool FULL>
+template <typename T, int V, int EL, int N, bool FULL>
 struct Feed {
     long long next, end;
     int tpr, gt, depth, slot, phase;
     uint32_t ring, bars, here, step;     // here: the present slot; step: bytes of a slot
 
-    static __device__ __forceinline__ uint32_t place(const RnShape& sh) { return place_bytes(sh.d, sizeof(T), V > 1); }
+    static __device__ __forceinline__ uint32_t place(const RnShape& sh) { return place_bytes(sh.d, sizeof(T), kWide<T, V>); }
     static __device__ __forceinline__ int count(const RnArgs& a)
     {
         int k = 0;
@@ -229,7 +240,7 @@ struct Feed {
     // Bytes from a 16-byte word's begin to row r of matrix n.
     static __device__ __forceinline__ uint32_t offset(const RnShape& sh, const RnArgs& a, int n, long long r)
     {
-        if constexpr (V > 1) return 0;
+        if constexpr (kWide<T, V>) return 0;
         else return (uint32_t)(reinterpret_cast<uintptr_t>(a.in[n]) + (unsigned long long)r * (sh.d * sizeof(T))) & 15u;
     }
     // Of the words that row r lies in, from its first, bytes [lo, hi) are copied: those of words inside the matrix.
@@ -245,7 +256,7 @@ struct Feed {
     {
         const uint32_t bar = bars + to * 8, step = place(sh);
         uint32_t at = ring + to * this->step, bytes = this->step;
-        if constexpr (V == 1) {
+        if constexpr (!kWide<T, V>) {
             bytes = 0;
             uint32_t p = at;
 #pragma unroll 1
@@ -276,7 +287,7 @@ struct Feed {
         for (int n = 0; n < N; ++n)
             if (a.in[n]) {
                 uint32_t from = 0, lo = 0, hi = step;
-                if constexpr (V == 1) {
+                if constexpr (!kWide<T, V>) {
                     from = offset(sh, a, n, next);
                     span(sh, next, from, lo, hi);
                 }
@@ -313,31 +324,37 @@ struct Feed {
     }
     // Row r of matrix n (`skip` bytes into a slot) as fp32, zeros where there is none.
     __device__ __forceinline__ void read(const RnShape& sh, const RnArgs& a, int n, uint32_t skip, long long r,
-                                         float (&v)[NV][V]) const
+                                         float (&v)[EL]) const
     {
+        constexpr int NV = EL / V;
         const int pieces = sh.d / V;
         const uint32_t at = here + skip + offset(sh, a, n, r);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = gt + i * tpr;
             if (a.in[n] && (FULL || c < pieces)) {
-                if constexpr (V > 1) {
+                if constexpr (V * sizeof(T) == 16) {
                     Piece<T, V> x;
                     asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n"
                                  : "=r"(x.w.x), "=r"(x.w.y), "=r"(x.w.z), "=r"(x.w.w)
                                  : "r"(at + c * 16)
                                  : "memory");
-                    unpack<T, V>(x, v[i]);
+                    unpack<T, V>(x, slice<V>(v, i));
                 } else if constexpr (sizeof(T) == 4) {
-                    asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v[i][0]) : "r"(at + c * 4) : "memory");
+                    asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v[i]) : "r"(at + c * 4) : "memory");
+                } else if constexpr (V == 2) {
+                    uint32_t x;
+                    asm volatile("ld.shared.u32 %0, [%1];\n" : "=r"(x) : "r"(at + c * 4) : "memory");
+                    v[2 * i] = __uint_as_float(x << 16);
+                    v[2 * i + 1] = __uint_as_float(x & 0xffff0000u);
                 } else {
-                    uint16_t b;
-                    asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(b) : "r"(at + c * 2) : "memory");
-                    v[i][0] = __uint_as_float((uint32_t)b << 16);
+                    uint16_t x;
+                    asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(x) : "r"(at + c * 2) : "memory");
+                    v[i] = __uint_as_float((uint32_t)x << 16);
                 }
             } else {
 #pragma unroll
-                for (int e = 0; e < V; ++e) v[i][e] = 0.0f;
+                for (int e = 0; e < V; ++e) v[i * V + e] = 0.0f;
             }
         }
     }
@@ -360,16 +377,26 @@ __device__ __forceinline__ void group_sync()
     else __syncthreads();
 }
 
-// A piece of a vector, or `none` everywhere.
+// Piece `at` / V of a vector, or `none` everywhere.
 template <typename T, int V>
 __device__ __forceinline__ void vec_piece(const void* p, size_t at, float none, float (&v)[V])
 {
-    if (p) {
-        unpack<T, V>(load_piece<T, V>(static_cast<const T*>(p) + at), v);
-    } else {
+    if (!p) {
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] = none;
+    } else if constexpr (sizeof(T) == 2 && V == 2) {
+        const float2 x = unpack_bf16(*reinterpret_cast<const uint32_t*>(static_cast<const T*>(p) + at));
+        v[0] = x.x;
+        v[1] = x.y;
+    } else {
+        unpack<T, V>(load_piece<T, V>(static_cast<const T*>(p) + at), v);
     }
+}
+template <typename T, int V>
+__device__ __forceinline__ void put_piece(T* p, const float (&v)[V])
+{
+    if constexpr (sizeof(T) == 2 && V == 2) *reinterpret_cast<uint32_t*>(p) = pack_bf16(v[0], v[1]);
+    else store_piece<T, V>(p, v);
 }
 
 // Of a row whose copy never arrived (the call has no status word): NaN, in an element of each thread.
@@ -437,37 +464,69 @@ __device__ __forceinline__ float sum_group(float a, Sums& red, int& turn)
 }
 
 // g, c and gate gamma_h of sample s for this thread's pieces.
-template <typename T, int V, int NV, bool SHIFT, bool FULL>
+template <typename T, int V, int EL, bool SHIFT, bool FULL>
 __device__ __forceinline__ void load_vectors(const RnShape& sh, const RnArgs& a, int s, int gt, int tpr, int pieces,
-                                             float (&g)[NV][V], float (&c)[NV][V], float (&b)[NV][V])
+                                             float (&g)[EL], float (&c)[EL], float (&b)[EL])
 {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
+    for (int i = 0; i < EL / V; ++i) {
         const int p = gt + i * tpr;
+        float(&gp)[V] = slice<V>(g, i), (&cp)[V] = slice<V>(c, i), (&bp)[V] = slice<V>(b, i);
         if (!FULL && p >= pieces) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) g[i][e] = c[i][e] = b[i][e] = 0.0f;
+            for (int e = 0; e < V; ++e) gp[e] = cp[e] = bp[e] = 0.0f;
             continue;
         }
         const size_t at = (size_t)p * V, mod = (size_t)(s * sh.mod_stride) + at;
         float s1[V], w[V];
         vec_piece<T, V>(a.scale, mod, 0.0f, s1);
-        vec_piece<T, V>(a.gamma, at, 1.0f, g[i]);
+        vec_piece<T, V>(a.gamma, at, 1.0f, gp);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             s1[e] += 1.0f;
-            g[i][e] *= s1[e];
+            gp[e] *= s1[e];
         }
         if constexpr (SHIFT) {
             vec_piece<T, V>(a.beta, at, 0.0f, w);
-            vec_piece<T, V>(a.shift, mod, 0.0f, c[i]);
+            vec_piece<T, V>(a.shift, mod, 0.0f, cp);
 #pragma unroll
-            for (int e = 0; e < V; ++e) c[i][e] = fmaf(w[e], s1[e], c[i][e]);
+            for (int e = 0; e < V; ++e) cp[e] = fmaf(w[e], s1[e], cp[e]);
         }
-        vec_piece<T, V>(a.gate, mod, 1.0f, b[i]);
+        vec_piece<T, V>(a.gate, mod, 1.0f, bp);
         vec_piece<T, V>(a.gamma_h, at, 1.0f, w);
 #pragma unroll
-        for (int e = 0; e < V; ++e) b[i][e] *= w[e];
+        for (int e = 0; e < V; ++e) bp[e] *= w[e];
+    }
+}
+
+// t += k v
+template <int EL>
+__device__ __forceinline__ void scaled_add(float (&t)[EL], const float (&v)[EL], float k)
+{
+    const float kk[2] = {k, k};
+#pragma unroll
+    for (int e = 0; e < EL; e += 2) fma2(&t[e], &v[e], kk, &t[e]);
+}
+
+// v = 0 past the row's end.
+template <int V, bool FULL, int EL>
+__device__ __forceinline__ void clear_rest(int gt, int tpr, int pieces, float (&v)[EL])
+{
+    if constexpr (!FULL)
+#pragma unroll
+        for (int i = 0; i < EL / V; ++i)
+            if (gt + i * tpr >= pieces)
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[i * V + e] = 0.0f;
+}
+// This thread's pieces of a row into `row`.
+template <typename T, int V, bool FULL, int EL>
+__device__ __forceinline__ void put_row(T* row, int gt, int tpr, int pieces, float (&v)[EL])
+{
+#pragma unroll
+    for (int i = 0; i < EL / V; ++i) {
+        const int p = gt + i * tpr;
+        if (FULL || p < pieces) put_piece<T, V>(row + (size_t)p * V, slice<V>(v, i));
     }
 }
 
@@ -481,28 +540,24 @@ __device__ __forceinline__ float quotient(float x, int d, float inv_d)
 
 // v = normalised v; returns (mean, 1 / size).  `first` runs after the first barrier: every thread of the group has
 // read its pieces.
-template <bool WARP, int V, int NV, bool FULL, typename F>
-__device__ __forceinline__ float2 normalise(int kind, int d, float inv_d, float eps, int gt, int tpr, int pieces, float (&v)[NV][V],
-                                            Sums& red, int& turn, F first)
+template <bool WARP, int V, bool FULL, int EL, typename F>
+__device__ __forceinline__ float2 normalise(int kind, int d, float inv_d, float eps, int gt, int tpr, int pieces,
+                                            float (&v)[EL], Sums& red, int& turn, F first)
 {
     float mu = 0.0f;
     if (kind == ROLA_NORM_LAYER) {
         float s[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int i = 0; i < NV; ++i) sum_piece<V>(s, v[i]);
+        sum_piece<EL>(s, v);
         mu = quotient(sum_group<WARP>(s[0] + s[1], red, turn), d, inv_d);
         first();
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (FULL || gt + i * tpr < pieces) fma_piece<V>(v[i], v[i], 1.0f, -mu);
+        fma_piece<EL>(v, v, 1.0f, -mu);
+        clear_rest<V, FULL>(gt, tpr, pieces, v);
     }
     float q[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < NV; ++i) dot_piece<V>(q, v[i], v[i]);
+    dot_piece<EL>(q, v, v);
     const float r = rsqrtf(fmaf(sum_group<WARP>(q[0] + q[1], red, turn), inv_d, eps));
     if (kind != ROLA_NORM_LAYER) first();
-#pragma unroll
-    for (int i = 0; i < NV; ++i) fma_piece<V>(v[i], v[i], r, 0.0f);
+    fma_piece<EL>(v, v, r, 0.0f);
     return make_float2(mu, r);
 }
 
@@ -510,7 +565,6 @@ template <typename T, int V, int EL, bool WARP, bool FULL, int TH, int MIN>
 __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
     rn_fwd_kernel(const __grid_constant__ RnShape sh, const __grid_constant__ RnArgs a, int depth)
 {
-    constexpr int NV = EL / V;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ __align__(16) Sums red;
     int turn = 0;
@@ -518,7 +572,7 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
         for (int i = threadIdx.x; i < 512; i += blockDim.x) (&red.buf[0][0][0])[i] = 0.0f;
     const int group = WARP ? threadIdx.x >> 5 : 0, part = WARP ? blockIdx.x * kWarpGroups + group : blockIdx.x;
     if (part >= a.parts) return;                         // a whole warp: no barrier of the CTA follows
-    Feed<T, V, NV, 2, FULL> q;
+    Feed<T, V, EL, 2, FULL> q;
     q.tpr = WARP ? 32 : blockDim.x;
     q.gt = WARP ? threadIdx.x & 31 : threadIdx.x;
     q.depth = depth;
@@ -533,15 +587,15 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
 #pragma unroll 1
     for (int s = (int)(r / sh.rows); r < q.end; ++s) {   // the part's samples, and their rows
         const long long stop = min(q.end, (long long)(s + 1) * sh.rows);
-        float g[NV][V], c[NV][V], b[NV][V];
-        load_vectors<T, V, NV, true, FULL>(sh, a, s, q.gt, q.tpr, pieces, g, c, b);
+        float g[EL], c[EL], b[EL];
+        load_vectors<T, V, EL, true, FULL>(sh, a, s, q.gt, q.tpr, pieces, g, c, b);
 #pragma unroll 1
         for (; r < stop; ++r, at += sh.d) {
             const bool ok = q.wait();
-            float u[NV][V], hh[NV][V];
+            float u[EL], hh[EL];
             q.read(sh, a, 0, 0, r, u);
             q.read(sh, a, 1, place, r, hh);
-            if (!ok) u[0][0] = kLost;
+            if (!ok) u[0] = kLost;
             bool held = true;
             auto refill = [&]() {
                 if (!held) return;
@@ -552,33 +606,19 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
             float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (a.h) {
                 if (sh.branch != ROLA_NORM_NONE) {
-                    const float2 m = normalise<WARP, V, NV, FULL>(sh.branch, sh.d, inv_d, sh.eps, q.gt, q.tpr, pieces, hh, red, turn, refill);
+                    const float2 m = normalise<WARP, V, FULL>(sh.branch, sh.d, inv_d, sh.eps, q.gt, q.tpr, pieces, hh, red, turn, refill);
                     st.z = m.x;
                     st.w = m.y;
                 }
-                T* out = static_cast<T*>(a.out) + at;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int p = q.gt + i * q.tpr;
-                    if (FULL || p < pieces) {
-                        fma_piece<V>(u[i], b[i], hh[i], u[i]);
-                        store_piece<T, V>(out + (size_t)p * V, u[i]);
-                    }
-                }
+                fma_piece<EL>(u, b, hh, u);
+                put_row<T, V, FULL>(static_cast<T*>(a.out) + at, q.gt, q.tpr, pieces, u);
             }
             if (sh.norm != ROLA_NORM_NONE) {
-                const float2 m = normalise<WARP, V, NV, FULL>(sh.norm, sh.d, inv_d, sh.eps, q.gt, q.tpr, pieces, u, red, turn, refill);
+                const float2 m = normalise<WARP, V, FULL>(sh.norm, sh.d, inv_d, sh.eps, q.gt, q.tpr, pieces, u, red, turn, refill);
                 st.x = m.x;
                 st.y = m.y;
-                T* y = static_cast<T*>(a.y) + at;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int p = q.gt + i * q.tpr;
-                    if (FULL || p < pieces) {
-                        fma_piece<V>(u[i], u[i], g[i], c[i]);
-                        store_piece<T, V>(y + (size_t)p * V, u[i]);
-                    }
-                }
+                fma_piece<EL>(u, u, g, c);
+                put_row<T, V, FULL>(static_cast<T*>(a.y) + at, q.gt, q.tpr, pieces, u);
             }
             if (held) {
                 group_sync<WARP>();
@@ -593,7 +633,6 @@ template <typename T, int V, int EL, bool WARP, bool FULL, int TH, int MIN>
 __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
     rn_bwd_kernel(const __grid_constant__ RnShape sh, const __grid_constant__ RnArgs a, int depth)
 {
-    constexpr int NV = EL / V;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ __align__(16) Sums red;
     int turn = 0;
@@ -602,7 +641,7 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
     const int group = WARP ? threadIdx.x >> 5 : 0, part = WARP ? blockIdx.x * kWarpGroups + group : blockIdx.x;
     if (part >= a.parts) return;
     const bool normed = sh.norm != ROLA_NORM_NONE;
-    Feed<T, V, NV, 4, FULL> q;
+    Feed<T, V, EL, 4, FULL> q;
     q.tpr = WARP ? 32 : blockDim.x;
     q.gt = WARP ? threadIdx.x & 31 : threadIdx.x;
     q.depth = depth;
@@ -619,23 +658,21 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
 #pragma unroll 1
     for (int s = (int)(r / sh.rows); r < q.end; ++s) {   // the part's samples, and their rows
         const long long stop = min(q.end, (long long)(s + 1) * sh.rows);
-        float g[NV][V], b[NV][V], A[NV][V], B[NV][V], E[NV][V];
-        load_vectors<T, V, NV, false, FULL>(sh, a, s, q.gt, q.tpr, pieces, g, A, b);
+        float g[EL], b[EL], A[EL], B[EL], E[EL];
+        load_vectors<T, V, EL, false, FULL>(sh, a, s, q.gt, q.tpr, pieces, g, A, b);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < V; ++e) A[i][e] = B[i][e] = E[i][e] = 0.0f;
+        for (int e = 0; e < EL; ++e) A[e] = B[e] = E[e] = 0.0f;
 #pragma unroll 1
         for (; r < stop; ++r, at += sh.d) {
             const float4 now = st;
             if (r + 1 < q.end) st = reinterpret_cast<const float4*>(a.stats)[r + 1];
             const bool ok = q.wait();
-            float v[NV][V], hh[NV][V], dy[NV][V], t[NV][V];
+            float v[EL], hh[EL], dy[EL], t[EL];
             q.read(sh, a, 0, 0, r, v);
             q.read(sh, a, 1, k1, r, hh);
             q.read(sh, a, 2, k2, r, dy);
             q.read(sh, a, 3, k3, r, t);
-            if (!ok) t[0][0] = hh[0][0] = kLost;
+            if (!ok) t[0] = hh[0] = kLost;
             bool held = true;
             auto refill = [&]() {
                 if (!held) return;
@@ -643,40 +680,28 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
                 if constexpr (WARP) __syncwarp();
                 q.refill(sh, a);
             };
-            if (sh.branch != ROLA_NORM_NONE)
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (FULL || q.gt + i * q.tpr < pieces) {
-                        fma_piece<V>(hh[i], hh[i], 1.0f, -now.z);
-                        fma_piece<V>(hh[i], hh[i], now.w, 0.0f);
-                    }
+            if (sh.branch != ROLA_NORM_NONE) {
+                fma_piece<EL>(hh, hh, 1.0f, -now.z);
+                fma_piece<EL>(hh, hh, now.w, 0.0f);
+                clear_rest<V, FULL>(q.gt, q.tpr, pieces, hh);
+            }
             // With a norm behind the branch its two sums are of e = b t, t = t0 + k1 + k2 v with t0 = dout + rstd a and
             // k1, k2 known only after the sums of a and a v.  They are taken apart instead, and all sums are one step:
             //   sum e = sum b t0 + k1 sum b + k2 sum b v,  sum e hh = sum b hh t0 + k1 sum b hh + k2 sum b hh v
             float n1 = 0.0f, n2 = 0.0f;                      // mean e (layer norm), mean e hh
             if (normed) {
-                float zero[V] = {};
-                const float size[2] = {now.y, now.y};
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (FULL || q.gt + i * q.tpr < pieces) {
-                        fma_piece<V>(v[i], b[i], hh[i], v[i]);       // the forward's sum, to the bit
-                        fma_piece<V>(v[i], v[i], 1.0f, -now.x);
-                        fma_piece<V>(v[i], v[i], now.y, 0.0f);
-                        fma_piece<V>(A[i], dy[i], v[i], A[i]);
-                        add_piece<V>(B[i], dy[i]);
-                        fma_piece<V>(dy[i], dy[i], g[i], zero);
-                        if constexpr (V == 1) t[i][0] = fmaf(dy[i][0], now.y, t[i][0]);
-                        else
-#pragma unroll
-                            for (int e = 0; e < V; e += 2) fma2(&t[i][e], &dy[i][e], size, &t[i][e]);
-                    }
+                float zero[EL] = {};
+                fma_piece<EL>(v, b, hh, v);                  // the forward's sum, to the bit
+                fma_piece<EL>(v, v, 1.0f, -now.x);
+                fma_piece<EL>(v, v, now.y, 0.0f);
+                clear_rest<V, FULL>(q.gt, q.tpr, pieces, v);
+                fma_piece<EL>(A, dy, v, A);
+                add_piece<EL>(B, dy);
+                fma_piece<EL>(dy, dy, g, zero);
+                scaled_add(t, dy, now.y);
                 float sa[2] = {0.0f, 0.0f}, sav[2] = {0.0f, 0.0f};
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    sum_piece<V>(sa, dy[i]);
-                    dot_piece<V>(sav, dy[i], v[i]);
-                }
+                sum_piece<EL>(sa, dy);
+                dot_piece<EL>(sav, dy, v);
                 const bool centred = sh.norm == ROLA_NORM_LAYER, branch_centred = sh.branch == ROLA_NORM_LAYER;
                 float k1, k2;
                 if (sh.branch == ROLA_NORM_NONE) {
@@ -685,13 +710,10 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
                     k1 = centred ? -now.y * (sum[0] * inv_d) : 0.0f;
                     k2 = -now.y * (sum[1] * inv_d);
                 } else {
-                    float c[2] = {0.0f, 0.0f}, cv[2] = {0.0f, 0.0f}, w[V];       // sum b hh t0, sum b hh v
-#pragma unroll
-                    for (int i = 0; i < NV; ++i) {
-                        fma_piece<V>(w, b[i], hh[i], zero);
-                        dot_piece<V>(c, w, t[i]);
-                        dot_piece<V>(cv, w, v[i]);
-                    }
+                    float c[2] = {0.0f, 0.0f}, cv[2] = {0.0f, 0.0f}, w[EL];      // sum b hh t0, sum b hh v
+                    fma_piece<EL>(w, b, hh, zero);
+                    dot_piece<EL>(c, w, t);
+                    dot_piece<EL>(cv, w, v);
                     if (!centred && !branch_centred) {
                         float sum[4] = {sav[0] + sav[1], c[0] + c[1], cv[0] + cv[1], 0.0f};
                         sum_group<WARP, 4>(sum, red, turn);
@@ -700,13 +722,10 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
                         n2 = fmaf(k2, sum[2], sum[1]) * inv_d;
                     } else {
                         float sb[2] = {0.0f, 0.0f}, sbv[2] = {0.0f, 0.0f}, sbt[2] = {0.0f, 0.0f}, sw[2] = {0.0f, 0.0f};
-#pragma unroll
-                        for (int i = 0; i < NV; ++i) {
-                            sum_piece<V>(sb, b[i]);
-                            dot_piece<V>(sbv, b[i], v[i]);
-                            dot_piece<V>(sbt, b[i], t[i]);
-                            dot_piece<V>(sw, b[i], hh[i]);
-                        }
+                        sum_piece<EL>(sb, b);
+                        dot_piece<EL>(sbv, b, v);
+                        dot_piece<EL>(sbt, b, t);
+                        sum_piece<EL>(sw, w);
                         float sum[8] = {sa[0] + sa[1],   sav[0] + sav[1], sbt[0] + sbt[1], sb[0] + sb[1],
                                         sbv[0] + sbv[1], c[0] + c[1],     sw[0] + sw[1],   cv[0] + cv[1]};
                         sum_group<WARP, 8>(sum, red, turn);
@@ -717,19 +736,13 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
                     }
                 }
                 refill();
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    fma_piece<V>(v[i], v[i], k2, k1);
-                    add_piece<V>(t[i], v[i]);
-                }
+                fma_piece<EL>(v, v, k2, k1);
+                add_piece<EL>(t, v);                         // k1 past the row's end, where b is 0
             } else if (sh.branch != ROLA_NORM_NONE) {
-                float zero[V] = {}, w[V], se[2] = {0.0f, 0.0f}, seh[2] = {0.0f, 0.0f};
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    fma_piece<V>(w, b[i], t[i], zero);
-                    sum_piece<V>(se, w);
-                    dot_piece<V>(seh, w, hh[i]);
-                }
+                float zero[EL] = {}, w[EL], se[2] = {0.0f, 0.0f}, seh[2] = {0.0f, 0.0f};
+                fma_piece<EL>(w, b, t, zero);
+                sum_piece<EL>(se, w);
+                dot_piece<EL>(seh, w, hh);
                 float sum[2] = {se[0] + se[1], seh[0] + seh[1]};
                 sum_group<WARP, 2>(sum, red, turn);
                 refill();
@@ -740,49 +753,38 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
                 group_sync<WARP>();
                 refill();
             }
-            T* dx = static_cast<T*>(a.dx) + at;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int p = q.gt + i * q.tpr;
-                if (FULL || p < pieces) {
-                    fma_piece<V>(E[i], t[i], hh[i], E[i]);
-                    store_piece<T, V>(dx + (size_t)p * V, t[i]);
-                }
-            }
+            fma_piece<EL>(E, t, hh, E);
+            put_row<T, V, FULL>(static_cast<T*>(a.dx) + at, q.gt, q.tpr, pieces, t);
             if (a.dh) {
-                float zero[V] = {};
-                T* dh = static_cast<T*>(a.dh) + at;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int p = q.gt + i * q.tpr;
-                    if (FULL || p < pieces) {
-                        fma_piece<V>(t[i], t[i], b[i], zero);
-                        if (sh.branch != ROLA_NORM_NONE) {
-                            fma_piece<V>(hh[i], hh[i], -n2, -n1);
-                            add_piece<V>(t[i], hh[i]);
-                            fma_piece<V>(t[i], t[i], now.w, 0.0f);
-                        }
-                        store_piece<T, V>(dh + (size_t)p * V, t[i]);
-                    }
+                float zero[EL] = {};
+                fma_piece<EL>(t, t, b, zero);
+                if (sh.branch != ROLA_NORM_NONE) {
+                    fma_piece<EL>(hh, hh, -n2, -n1);
+                    add_piece<EL>(t, hh);
+                    fma_piece<EL>(t, t, now.w, 0.0f);
                 }
+                put_row<T, V, FULL>(static_cast<T*>(a.dh) + at, q.gt, q.tpr, pieces, t);
             }
         }
         if (a.part) {
             const int dp = rn_padded(sh.d);
             float* out = a.part + (size_t)(part + s) * 3 * dp;
-            auto store = [&](float* to, const float(&x)[V]) {
-                if constexpr (V == 1) to[0] = x[0];
-                else
 #pragma unroll
-                    for (int e = 0; e < V; e += 4) store4(to + e, make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]));
-            };
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
+            for (int i = 0; i < EL / V; ++i) {
                 const int p = (q.gt + i * q.tpr) * V;
                 if (!FULL && p >= sh.d) continue;
-                store(out + p, A[i]);
-                store(out + dp + p, B[i]);
-                store(out + 2 * dp + p, E[i]);
+#pragma unroll
+                for (int n = 0; n < 3; ++n) {
+                    const float(&x)[V] = slice<V>(n == 0 ? A : n == 1 ? B : E, i);
+                    float* to = out + n * dp + p;
+                    if constexpr (V >= 4) {
+#pragma unroll
+                        for (int e = 0; e < V; e += 4) store4(to + e, make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < V; ++e) to[e] = x[e];
+                    }
+                }
             }
         }
     }
@@ -904,14 +906,14 @@ bool wants_sums(const RnArgs& a) { return a.dgate || a.dgamma_h || a.dgamma || a
 constexpr int kMostParts = 4864, kMostCtas = 1216;       // of warps, of CTAs: 32 and 8 on each of 152 SMs
 constexpr int kFwdRegisters = 16384, kBwdRegisters = 8192;       // longest rows held in registers (forward, single elements: 8192)
 
-// Whether every row, and every vector, can be taken in 16-byte pieces.
-bool wide(const RnShape& s, const RnArgs& a, int esz)
+// Whether every row and every vector starts at a multiple of `to` bytes.
+bool starts_at(int to, const RnShape& s, const RnArgs& a, int esz)
 {
     uintptr_t bits = 0;
     for (const void* p : {a.x, a.h, a.gate, a.gamma_h, a.gamma, a.beta, a.scale, a.shift, a.dout, a.dy,
                           (const void*)a.out, (const void*)a.y, (const void*)a.dx, (const void*)a.dh})
         bits |= reinterpret_cast<uintptr_t>(p);
-    return (int64_t)s.d * esz % 16 == 0 && s.mod_stride * esz % 16 == 0 && (bits & 15u) == 0;
+    return (int64_t)s.d * esz % to == 0 && s.mod_stride * esz % to == 0 && (bits & (to - 1)) == 0;
 }
 
 cudaError_t sm_count(int* n)
@@ -959,11 +961,11 @@ cudaError_t shape_of(K kernel, const RnShape& s, bool warp, int el, int register
 template <typename T, int V, int EL, bool WARP, int TH, int MIN, bool FULL = false>
 cudaError_t fwd_one(const RnShape& s, RnArgs& a, cudaStream_t st)
 {
-    if constexpr (V > 1 && !WARP && !FULL)
+    if constexpr (kWide<T, V> && !WARP && !FULL)
         if (s.d % (32 * EL) == 0) return fwd_one<T, V, EL, WARP, TH, MIN, true>(s, a, st);
     Launch l;
     auto kernel = rn_fwd_kernel<T, V, EL, WARP, FULL, TH, MIN>;
-    const size_t row = (size_t)place_bytes(s.d, sizeof(T), V > 1) * (a.h ? 2 : 1);
+    const size_t row = (size_t)place_bytes(s.d, sizeof(T), kWide<T, V>) * (a.h ? 2 : 1);
     cudaError_t e = shape_of(kernel, s, WARP, EL, registers_of(TH, MIN), row, 1ll << 30, &l);
     if (e != cudaSuccess) return e;
     a.in[0] = a.x;
@@ -975,12 +977,12 @@ cudaError_t fwd_one(const RnShape& s, RnArgs& a, cudaStream_t st)
 template <typename T, int V, int EL, bool WARP, int TH, int MIN, bool FULL = false>
 cudaError_t bwd_one(const RnShape& s, RnArgs& a, cudaStream_t st)
 {
-    if constexpr (V > 1 && !WARP && !FULL)
+    if constexpr (kWide<T, V> && !WARP && !FULL)
         if (s.d % (32 * EL) == 0) return bwd_one<T, V, EL, WARP, TH, MIN, true>(s, a, st);
     Launch l;
     auto kernel = rn_bwd_kernel<T, V, EL, WARP, FULL, TH, MIN>;
     const int matrices = (s.norm != ROLA_NORM_NONE ? 1 : 0) + (a.h ? 1 : 0) + (a.dy ? 1 : 0) + (a.dout ? 1 : 0);
-    const size_t row = (size_t)place_bytes(s.d, sizeof(T), V > 1) * matrices;
+    const size_t row = (size_t)place_bytes(s.d, sizeof(T), kWide<T, V>) * matrices;
     cudaError_t e = shape_of(kernel, s, WARP, EL, registers_of(TH, MIN), row, rn_parts(s), &l);
     if (e != cudaSuccess) return e;
     a.in[0] = s.norm != ROLA_NORM_NONE ? a.x : nullptr;
@@ -1000,11 +1002,11 @@ cudaError_t fwd(const RnShape& s, RnArgs& a, cudaStream_t st)
 {
     if (s.d <= 256) return fwd_one<T, V, 8, true, 128, 6>(s, a, st);
     if (s.d <= 512) return fwd_one<T, V, 16, true, 128, 4>(s, a, st);
-    constexpr int kFewer = V == 1;                   // CTAs: addresses of single elements take more registers
+    constexpr int kFewer = !kWide<T, V>;                   // CTAs: addresses of single elements take more registers
     if (s.d <= 16 * 160) return fwd_one<T, V, 16, false, 160, 3 - kFewer>(s, a, st);
     if (s.d <= 16 * 320) return fwd_one<T, V, 16, false, 320, 2 - kFewer>(s, a, st);
     if (s.d <= 16 * 512) return fwd_one<T, V, 16, false, 512, 1>(s, a, st);
-    if constexpr (V > 1)
+    if constexpr (kWide<T, V>)
         if (s.d <= kFwdRegisters) return fwd_one<T, V, 32, false, 512, 1>(s, a, st);
     rn_fwd_long_kernel<T><<<long_grid(s.total), kLongThreads, 0, st>>>(s, a);
     return cudaGetLastError();
@@ -1024,12 +1026,22 @@ cudaError_t bwd(const RnShape& s, RnArgs& a, cudaStream_t st)
     return cudaGetLastError();
 }
 
+// f of the largest piece that every row and every vector can be taken in.
+template <typename T, typename F>
+cudaError_t by_piece(const RnShape& s, const RnArgs& a, F f)
+{
+    if (starts_at(16, s, a, sizeof(T))) return f(std::integral_constant<int, 16 / sizeof(T)>());
+    if constexpr (sizeof(T) == 2)
+        if (starts_at(4, s, a, 2)) return f(std::integral_constant<int, 2>());
+    return f(std::integral_constant<int, 1>());
+}
+
 template <typename T>
 cudaError_t backward(const RnShape& s, RnArgs& a, cudaStream_t st)
 {
     const bool sums = wants_sums(a);
     if (!sums) a.part = nullptr;
-    cudaError_t e = wide(s, a, sizeof(T)) ? bwd<T, 16 / sizeof(T)>(s, a, st) : bwd<T, 1>(s, a, st);
+    cudaError_t e = by_piece<T>(s, a, [&](auto v) { return bwd<T, decltype(v)::value>(s, a, st); });
     if (e != cudaSuccess || !sums) return e;
     a.norm_sums = a.dgamma || a.dbeta || a.dscale || a.dshift;
     const bool branch_sums = a.dgate || a.dgamma_h, shared = a.dgamma || a.dbeta || a.dgamma_h;
@@ -1061,8 +1073,8 @@ int rn_parts(const RnShape& s)
 
 int rn_shares(const RnShape& s)
 {
-    // 64 samples a share at least, and no more CTAs than 4 on each of 152 SMs
-    const int columns = (s.d + 31) / 32, most = (608 + columns - 1) / columns, want = (s.groups + 63) / 64;
+    // 32 samples a share at least, and some 4000 CTAs at most
+    const int columns = (s.d + 31) / 32, most = (4096 + columns - 1) / columns, want = (s.groups + 31) / 32;
     return want < most ? want : most;
 }
 
@@ -1070,8 +1082,9 @@ bool rn_long(const RnShape& s) { return s.d > kBwdRegisters; }
 
 cudaError_t launch_residual_norm(rola_dtype_t dt, const RnShape& s, RnArgs& a, cudaStream_t st)
 {
-    if (dt == ROLA_BF16) return wide(s, a, 2) ? fwd<__nv_bfloat16, 8>(s, a, st) : fwd<__nv_bfloat16, 1>(s, a, st);
-    return wide(s, a, 4) ? fwd<float, 4>(s, a, st) : fwd<float, 1>(s, a, st);
+    if (dt == ROLA_BF16)
+        return by_piece<__nv_bfloat16>(s, a, [&](auto v) { return fwd<__nv_bfloat16, decltype(v)::value>(s, a, st); });
+    return by_piece<float>(s, a, [&](auto v) { return fwd<float, decltype(v)::value>(s, a, st); });
 }
 
 cudaError_t launch_residual_norm_backward(rola_dtype_t dt, const RnShape& s, RnArgs& a, cudaStream_t st)

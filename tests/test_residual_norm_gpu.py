@@ -370,3 +370,31 @@ def test_refusals(rl):
     for bad in ((0, 5, 64), (2, 0, 64), (2, 5, 0)):
         with pytest.raises(rl.RolaError):
             rl.residual_norm_backward_workspace(rl.make_residual_norm_config(*bad))
+
+
+@pytest.mark.parametrize("skip", [1, 2, 4])
+@pytest.mark.parametrize("dname", sorted(DTYPES))
+@pytest.mark.parametrize("d", [2, 30, 778, 1536, 2050])
+def test_tensors_that_start_anywhere(rl, d, dname, skip):
+    """Every tensor `skip` elements past a 16-byte boundary, with a guard on both sides."""
+    case = Case(rl, 2, 9, d, "layer", "rms", ALL, DTYPES[dname], seed=d)
+    want = case.run()
+    made = []
+
+    def moved(t, fill=None):
+        buf = torch.full((t.numel() + 64,), 7.0, dtype=t.dtype, device="cuda")
+        view = buf[16 + skip:16 + skip + t.numel()].view(t.shape)
+        view.copy_(t if fill is None else torch.full_like(t, fill))
+        made.append((buf, t.numel()))
+        return view
+    case.x, case.h, case.dout, case.dy = (moved(t) for t in (case.x, case.h, case.dout, case.dy))
+    case.v = {n: moved(t) for n, t in case.v.items()}
+    blank = {n: moved(t, float("nan")) for n, t in want.items() if n in ("out", "y", "dx", "dh")}
+    stats, ws = torch.empty_like(want["stats"]), rl.residual_norm_backward_workspace(case.c)
+    grads = {"d" + n: moved(want["d" + n], float("nan")) for n in VECTORS}
+    rl.residual_norm(case.c, case.x, case.h, blank["out"], blank["y"], **case.v, stats=stats)
+    rl.residual_norm_backward(case.c, case.x, case.h, stats, case.dout, case.dy, blank["dx"], blank["dh"], ws,
+                              **{n: t for n, t in case.v.items() if n != "shift"}, **grads)
+    case.check(dict(blank, stats=stats, **grads))
+    for buf, n in made:
+        assert (buf[:16 + skip] == 7.0).all() and (buf[16 + skip + n:] == 7.0).all()
