@@ -132,18 +132,34 @@ LinShape make_shape(const rola_linear_config_t& c)
     return {c.tokens, c.d_in, c.d_out, c.act, wait_limit_ns(c.wait_limit_ms), c.debug_flags};
 }
 
+// The form of a bf16 layer's forward pass, and of its dX.
+enum LinearForm { kLinearByRows, kLinearFew, kLinearTiles };
+LinearForm linear_form(const LinShape& s)
+{
+    return s.M <= kLinearRows ? kLinearByRows : linear_few(s) ? kLinearFew : kLinearTiles;
+}
+LinearForm linear_dx_form(const LinShape& s) { return s.M <= kFfnFewTokens ? kLinearFew : kLinearTiles; }
+
 struct LinWorkspace {
-    size_t status, dZ, part, total;
+    size_t status, dZ, sums, part, total;
 };
 LinWorkspace linear_layout(const rola_linear_config_t& c, bool backward)
 {
     const LinShape s = make_shape(c);
     const bool dz = backward && c.act != ROLA_LOWRANK_ACT_IDENTITY;      // else dZ is dY
+    size_t part = 0;                             // of a split K axis, of one product at a time
+    if (c.dtype == ROLA_BF16 && !backward && linear_form(s) == kLinearTiles) part = linear_part_bytes(s.M, s.N, s.K);
+    if (c.dtype == ROLA_BF16 && backward) {
+        const size_t dx = linear_dx_form(s) == kLinearTiles ? linear_part_bytes(s.M, s.K, s.N) : 0;
+        const size_t dw = linear_part_bytes(s.N, s.K, s.M);
+        part = dx > dw ? dx : dw;
+    }
     LinWorkspace w;
     size_t off = 0;
     w.status = off; off = align_up(off + sizeof(DeviceStatus));
     w.dZ = off; off = align_up(off + (dz ? elem(c.dtype) * (size_t)s.M * s.N : 0));
-    w.part = off; off = align_up(off + (backward ? 4 * (size_t)linear_grad_parts(s) * s.N : 0));
+    w.sums = off; off = align_up(off + (backward ? 4 * (size_t)linear_grad_parts(s) * s.N : 0));
+    w.part = off; off = align_up(off + part);
     w.total = off;
     return w;
 }
@@ -156,10 +172,17 @@ rola_status_t linear_forward(const rola_linear_config_t* cfg, const void* X, con
     ROLA_CHECK(check_ws(ws, ws_bytes, w.total));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     DeviceStatus* status = at<DeviceStatus>(ws, w.status);
-    ROLA_TRY(cudaMemsetAsync(status, 0, sizeof(DeviceStatus), st));
     const LinShape s = make_shape(*cfg);
-    if (cfg->dtype == ROLA_BF16) ROLA_TRY(launch_linear_tc(s, X, W, b, R, Y, Z, status, st));
-    else ROLA_TRY(launch_linear_simt(s, X, W, b, R, Y, Z, st));
+    if (cfg->dtype == ROLA_FP32) {
+        ROLA_TRY(cudaMemsetAsync(status, 0, sizeof(DeviceStatus), st));
+        ROLA_TRY(launch_linear_simt(s, X, W, b, R, Y, Z, st));
+        return ROLA_OK;
+    }
+    switch (linear_form(s)) {
+        case kLinearByRows: ROLA_TRY(launch_linear_rows(s, X, W, b, R, Y, Z, status, st)); break;
+        case kLinearFew: ROLA_TRY(launch_linear_few(s, X, W, b, R, Y, Z, status, st)); break;
+        default: ROLA_TRY(launch_linear_tc(s, X, W, b, R, Y, Z, at<float>(ws, w.part), status, st));
+    }
     return ROLA_OK;
 }
 
@@ -499,14 +522,23 @@ rola_status_t rola_linear_backward(const rola_linear_config_t* cfg, const void* 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const LinShape s = make_shape(*cfg);
     DeviceStatus* status = at<DeviceStatus>(ws, w.status);
-    ROLA_TRY(cudaMemsetAsync(status, 0, sizeof(DeviceStatus), st));
-    const void* dZ = dY;
-    if (!identity) dZ = at<void>(ws, w.dZ);
-    if (!identity || db)
-        ROLA_TRY(launch_linear_grad(cfg->dtype, s, dY, identity ? nullptr : Z, at<void>(ws, w.dZ), db,
-                                    at<float>(ws, w.part), st));
-    if (cfg->dtype == ROLA_BF16) ROLA_TRY(launch_linear_backward_tc(s, X, W, dZ, dX, dW, status, st));
-    else ROLA_TRY(launch_linear_backward_simt(s, X, W, dZ, dX, dW, st));
+    const void* dZ = identity ? dY : at<void>(ws, w.dZ);
+    bool clear = true;                           // whether the next kernel clears the status word
+    if (!identity || db) {
+        ROLA_TRY(launch_linear_grad(cfg->dtype, s, dY, identity ? nullptr : Z, at<void>(ws, w.dZ), db, at<float>(ws, w.sums),
+                                    status, st));
+        clear = false;
+    }
+    if (cfg->dtype == ROLA_FP32) {
+        if (clear) ROLA_TRY(cudaMemsetAsync(status, 0, sizeof(DeviceStatus), st));
+        ROLA_TRY(launch_linear_backward_simt(s, X, W, dZ, dX, dW, st));
+        return ROLA_OK;
+    }
+    if (dX) {
+        if (linear_dx_form(s) == kLinearFew) ROLA_TRY(launch_linear_few_dx(s, W, dZ, dX, clear, status, st));
+        else ROLA_TRY(launch_linear_dx_tc(s, W, dZ, dX, at<float>(ws, w.part), clear, status, st));
+    }
+    if (dW) ROLA_TRY(launch_linear_dw_tc(s, X, dZ, dW, at<float>(ws, w.part), clear && !dX, status, st));
     return ROLA_OK;
 }
 

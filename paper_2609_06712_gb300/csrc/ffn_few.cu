@@ -1,4 +1,4 @@
-// The gated feed-forward's products for few tokens (bf16 operands, tcgen05):
+// The gated feed-forward's and the linear layer's products for few tokens (bf16 operands, tcgen05):
 // every weight is read once for all of them, and that is what bounds the work
 // (one token at widths 5120 x 13824: 425 MB of weights, 63 us at the measured
 // 6.8 TB/s, and 72 measured; its 0.4 GFLOP are nothing).  More than 96 tokens go in tiles of at most
@@ -9,7 +9,8 @@
 //   kUp     g, u (128 features x tokens) = Wg X^T, Wu X^T;  H = phi(g) * u
 //   kDown   Y^T  = Wd H^T
 //   kGrad   dH^T = Wd^T dY^T  (Wd read MN-major);  H, dG, dU from it and G, U
-//   kDX     dX^T = Wg^T dG^T + Wu^T dU^T  (MN-major; one sum over 2 d_ff)
+//   kDX     dX^T = Wg^T dG^T + Wu^T dU^T  (MN-major; one sum over 2 d_ff); a linear layer's dX is one of them
+//   kLinear Z^T  = W X^T + b;  Y = R + phi(Z)
 // There are too few row tiles to occupy the GPU (12 of 128 rows at d_model
 // 1536), so the K axis of a tile is split over a cluster of up to 8 CTAs.  Each
 // streams its share through a TMA ring into its own TMEM accumulator, then the
@@ -29,6 +30,7 @@
 
 #include "block_ops.cuh"
 #include "cluster.cuh"
+#include "linear.cuh"
 #include "tcgen05.cuh"
 #include "tma_2d.cuh"
 
@@ -37,7 +39,7 @@ namespace {
 
 using namespace tc;
 
-enum Mode { kUp, kDown, kGrad, kDX };
+enum Mode { kUp, kDown, kGrad, kDX, kLinear };
 
 constexpr int kTileM = 128, kStepK = 64, kThreads = 192, kMaxStages = 8;
 constexpr uint32_t kABytes = kTileM * kStepK * 2;
@@ -62,7 +64,9 @@ struct Params {
     int stages, act, skip_first;
     uint32_t stage_bytes, tiles_bytes;   // of a stage; of the tiles in front of the control block
     __nv_bfloat16 *c0, *c1, *c2;     // H / Y / dX; dG, dU
-    float *G, *U;                    // kUp: out or NULL; kGrad: in
+    float *G, *U;                    // kUp: out or NULL; kGrad: in; kLinear: Z in G, out or NULL
+    const __nv_bfloat16 *bias, *residual;    // kLinear, or NULL
+    int clear;                       // the status word is this kernel's to clear
     DeviceStatus* status;
     uint64_t wait_limit_ns;
 };
@@ -81,6 +85,8 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_few_kernel(const __grid_const
         if (atomicCAS(&p.status->code, 0, (int)ROLA_ERR_TIMEOUT) == 0) p.status->where = 128 + where;
     };
     if (tid == 0) {
+        // before any CTA can record a timeout, which takes 1 ms at least
+        if (p.clear && blockIdx.x == 0 && blockIdx.y == 0) p.status->code = p.status->where = 0;
         cb.abort = 0;
         for (int i = 0; i < p.stages; ++i) {
             mbar_init(bar(FULL + i), 1);
@@ -266,6 +272,21 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_few_kernel(const __grid_const
             store4(p.c0 + at, make_float4(h[0], h[1], h[2], h[3]));
             store4(p.c1 + at, make_float4(dg[0], dg[1], dg[2], dg[3]));
             store4(p.c2 + at, make_float4(du[0], du[1], du[2], du[3]));
+        } else if constexpr (MODE == kLinear) {
+            if (p.bias) {
+                const float4 b = load4(p.bias + f);
+                x[0] += b.x; x[1] += b.y; x[2] += b.z; x[3] += b.w;
+            }
+            if (p.G) *reinterpret_cast<float4*>(p.G + at) = make_float4(x[0], x[1], x[2], x[3]);
+            with_act(p.act, [&](auto act) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = act.phi(x[e]);
+            });
+            if (p.residual) {
+                const float4 r = load4(p.residual + at);
+                x[0] += r.x; x[1] += r.y; x[2] += r.z; x[3] += r.w;
+            }
+            store4(p.c0 + at, make_float4(x[0], x[1], x[2], x[3]));
         } else {
             store4(p.c0 + at, make_float4(x[0], x[1], x[2], x[3]));
         }
@@ -406,6 +427,41 @@ cudaError_t launch_ffn_few_grad(const FfnShape& s, const void* Wg, const void* W
         !map_of(&p.b[0], dG, s.M, s.F, p.nt) || !map_of(&p.b[1], dU, s.M, s.F, p.nt))
         return cudaErrorInvalidValue;
     return launch<kDX>(s, p, true, status, st);
+}
+
+// As ffn_few, of one product.
+bool linear_few(const LinShape& s)
+{
+    const int64_t tiles = (s.M + kMaxTokens - 1) / kMaxTokens;
+    return tiles == 1 || (tiles <= 7 && tiles * s.K * s.N <= 150000000 &&
+                          (int64_t)((s.M + 127) / 128) * ((s.N + 255) / 256) < 76);
+}
+
+cudaError_t launch_linear_few(const LinShape& s, const void* X, const void* W, const void* b, const void* R, void* Y,
+                              float* Z, DeviceStatus* status, cudaStream_t st)
+{
+    const FfnShape fs{s.M, s.K, s.N, s.act, s.wait_limit_ns, s.debug_flags};
+    Params p = params(fs);
+    p.rows = s.N; p.k_steps = steps(s.K); p.sources = 1;
+    p.c0 = static_cast<__nv_bfloat16*>(Y);
+    p.G = Z;
+    p.bias = static_cast<const __nv_bfloat16*>(b);
+    p.residual = static_cast<const __nv_bfloat16*>(R);
+    p.clear = 1;
+    if (!map_of(&p.a[0], W, s.N, s.K, kTileM) || !map_of(&p.b[0], X, s.M, s.K, p.nt)) return cudaErrorInvalidValue;
+    return launch<kLinear>(fs, p, false, status, st);
+}
+
+cudaError_t launch_linear_few_dx(const LinShape& s, const void* W, const void* dZ, void* dX, bool clear,
+                                 DeviceStatus* status, cudaStream_t st)
+{
+    const FfnShape fs{s.M, s.K, s.N, s.act, s.wait_limit_ns, s.debug_flags};
+    Params p = params(fs);
+    p.rows = s.K; p.k_steps = steps(s.N); p.sources = 1;
+    p.c0 = static_cast<__nv_bfloat16*>(dX);
+    p.clear = clear;
+    if (!map_of(&p.a[0], W, s.N, s.K, kStepK) || !map_of(&p.b[0], dZ, s.M, s.N, p.nt)) return cudaErrorInvalidValue;
+    return launch<kDX>(fs, p, false, status, st);
 }
 
 }  // namespace rola

@@ -5,6 +5,7 @@
 // lane sums its columns in registers, the warps meet in shared memory in warp order, the parts in a second kernel in
 // part order: the same bits every time.  The sums are of dZ in fp32, before it is rounded.
 #include "linear.cuh"
+#include "linear_finish.cuh"
 
 namespace rola {
 namespace {
@@ -29,8 +30,10 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) { 
 template <typename T, int ACT>
 __global__ void __launch_bounds__(32 * kWarps) linear_grad_kernel(int M, int N, const T* __restrict__ dY,
                                                                   const float* __restrict__ Z, T* __restrict__ dZ,
-                                                                  float* __restrict__ part)
+                                                                  float* __restrict__ part,
+                                                                  DeviceStatus* __restrict__ status)
 {
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) status->code = status->where = 0;
     __shared__ float sum[kWarps][kColumns + 8];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * kColumns + lane * 8;
     const int r0 = (int)((long long)M * blockIdx.y / gridDim.y), r1 = (int)((long long)M * (blockIdx.y + 1) / gridDim.y);
@@ -87,12 +90,33 @@ __global__ void __launch_bounds__(256) linear_bias_kernel(int n, int N, const fl
     db[c] = t;
 }
 
+// Eight outputs a thread from the parts of a split K axis.
+__global__ void __launch_bounds__(256) linear_join_kernel(const LinearEnd end, const float* __restrict__ part, int splits, int M,
+                                                          int N)
+{
+    const size_t all = (size_t)M * N, at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (at >= all) return;
+    float v[8];
+    load8(part + at, v);
+#pragma unroll 4
+    for (int i = 1; i < splits; ++i) {
+        float x[8];
+        load8(part + i * all + at, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += x[e];
+    }
+    const int f0 = (int)(at % N);
+    linear_end<true>(end, at - f0, f0, N, v);
+}
+
 template <typename T>
-cudaError_t grad(const LinShape& s, const void* dY, const float* Z, void* dZ, float* db, float* part, cudaStream_t st)
+cudaError_t grad(const LinShape& s, const void* dY, const float* Z, void* dZ, float* db, float* part, DeviceStatus* status,
+                 cudaStream_t st)
 {
     const dim3 grid((s.N + kColumns - 1) / kColumns, linear_grad_parts(s));
     auto go = [&](auto kernel) {
-        kernel<<<grid, 32 * kWarps, 0, st>>>(s.M, s.N, static_cast<const T*>(dY), Z, static_cast<T*>(dZ), db ? part : nullptr);
+        kernel<<<grid, 32 * kWarps, 0, st>>>(s.M, s.N, static_cast<const T*>(dY), Z, static_cast<T*>(dZ), db ? part : nullptr,
+                                           status);
         return cudaGetLastError();
     };
     cudaError_t e;
@@ -117,9 +141,17 @@ int linear_grad_parts(const LinShape& s)
 }
 
 cudaError_t launch_linear_grad(rola_dtype_t dt, const LinShape& s, const void* dY, const float* Z, void* dZ, float* db,
-                               float* part, cudaStream_t st)
+                               float* part, DeviceStatus* status, cudaStream_t st)
 {
-    return dt == ROLA_BF16 ? grad<__nv_bfloat16>(s, dY, Z, dZ, db, part, st) : grad<float>(s, dY, Z, dZ, db, part, st);
+    return dt == ROLA_BF16 ? grad<__nv_bfloat16>(s, dY, Z, dZ, db, part, status, st)
+                           : grad<float>(s, dY, Z, dZ, db, part, status, st);
+}
+
+cudaError_t launch_linear_join(const LinearEnd& end, const float* part, int splits, int M, int N, cudaStream_t st)
+{
+    const size_t pieces = (size_t)M * N / 8;
+    linear_join_kernel<<<(unsigned)((pieces + 255) / 256), 256, 0, st>>>(end, part, splits, M, N);
+    return cudaGetLastError();
 }
 
 }  // namespace rola

@@ -2,18 +2,30 @@
 //
 //   Y = R + phi(X W^T + b);  dX = dZ W,  dW = dZ^T X
 //
-// One persistent warp-specialised kernel computes C(m, n) = sum_k A(m, k) B(n, k) in tiles of 128 x 256, one CTA per
-// SM: TMA brings A and B in steps of 64 k into a ring of four stages in 128-byte-swizzled shared memory, one thread
-// issues the products, eight warps take the tile from TMEM (two buffers of 256 columns) under the next tile's products.
-// An operand is contiguous along k (K-major) or along m / n (MN-major), so that none is transposed in memory; what lies
-// past an edge is TMA's zero fill.
+// One persistent warp-specialised kernel computes C(m, n) = sum_k A(m, k) B(n, k) with pairs of CTAs (clusters of two,
+// one CTA an SM).  A pair has a tile of 256 x NT: CTA r holds rows 128 r .. of A and rows NT / 2 r .. of B in its shared
+// memory, and the products of cta_group::2, which the pair's first CTA issues, read both CTAs' halves of B; its rows
+// of the tile end up in each CTA's TMEM.  Against a CTA by itself the pair reads B from shared memory and L2 once instead
+// of twice.  TMA brings both operands in steps of 64 k into 128-byte-swizzled rings; the copies of both CTAs arrive at
+// the first one's mbarrier, the commits of its products at both.  The accumulator is double-buffered (2 x NT of 512
+// columns), so that eight warps of each CTA take a tile from TMEM under the next tile's products.
+//
+// An operand is contiguous along k (K-major, boxes of 64 k) or along m / n (MN-major, boxes of 64 x 64 k); the tensor
+// core reads either, so no operand is transposed in memory.  What lies past an edge is TMA's zero fill.
+//
+// Few tiles with a long K axis (the weights' gradients: K is the token) are split along K; the parts go to the
+// workspace in fp32, and a second kernel adds them in order and finishes the outputs (launch_linear_join).
 //
 // Every mbarrier wait is bounded; a wait that gives up records ROLA_ERR_TIMEOUT in the status word, and the CTA stops
-// issuing, lets what it issued complete and frees its TMEM.
+// issuing, lets what it issued complete, meets its pair and frees its TMEM.
 #include <cudaTypedefs.h>
 
+#include <type_traits>
+
 #include "attention_tc.cuh"
+#include "cluster.cuh"
 #include "linear.cuh"
+#include "linear_finish.cuh"
 #include "tma_2d.cuh"
 
 namespace rola {
@@ -21,26 +33,32 @@ namespace {
 
 using namespace tc;
 
-constexpr int kTileM = 128, kTileN = 256, kStepK = 64, kGroupM = 16;
-constexpr int kThreads = 320, kEpiWarps = 8, kStages = 4;
-constexpr uint32_t kABytes = kTileM * kStepK * 2, kBBytes = kTileN * kStepK * 2, kStageBytes = kABytes + kBBytes;
-constexpr uint32_t kSmemTiles = kStages * kStageBytes;
+constexpr int kHalfM = 128, kTileM = 2 * kHalfM, kStepK = 64, kGroupM = 8;
+constexpr int kThreads = 320, kEpiWarps = 8;
+constexpr uint32_t kABytes = kHalfM * kStepK * 2;
+constexpr uint32_t kRingBytes = 192 * 1024;
 
-enum Bar { FULL = 0, EMPTY = FULL + kStages, ACC_FULL = EMPTY + kStages, ACC_EMPTY = ACC_FULL + 2, DRAIN = ACC_EMPTY + 2, NUM_BARS };
+template <int NT>
+struct Cfg {
+    static constexpr uint32_t kBBytes = NT / 2 * kStepK * 2, kStageBytes = kABytes + kBBytes;
+    static constexpr int kStages = kRingBytes / kStageBytes;
+    static constexpr int FULL = 0, EMPTY = FULL + kStages, ACC_FULL = EMPTY + kStages, ACC_EMPTY = ACC_FULL + 2,
+                         DRAIN = ACC_EMPTY + 2, NUM_BARS = DRAIN + 1;
+};
 struct Ctrl {
-    uint64_t bar[NUM_BARS];
+    uint64_t bar[32];
     uint32_t tmem_base;
     int abort;
 };
+static_assert(Cfg<256>::NUM_BARS <= 32 && Cfg<128>::NUM_BARS <= 32, "mbarriers fit the control block");
 
 struct Params {
     CUtensorMap a, b;
-    __nv_bfloat16* c;
-    const __nv_bfloat16 *bias, *residual;        // or NULL
-    float* Z;                                    // or NULL
-    int M, N, m_tiles, n_tiles, k_steps, act;
-    int wide;                                    // the outputs' rows are 32-byte aligned
+    LinearEnd end;                               // what becomes of the sums
+    float* part;                                 // or, with splits, where they go: [splits][M][N]
+    int M, N, m_tiles, n_tiles, k_steps, splits;
     int skip_first;                              // test hook: a CTA's first load is never issued
+    int clear;                                   // the status word is this kernel's to clear
     DeviceStatus* status;
     uint64_t wait_limit_ns;
 };
@@ -50,13 +68,26 @@ __device__ __forceinline__ void record_timeout(const Params& p, int where)
     if (atomicCAS(&p.status->code, 0, (int)ROLA_ERR_TIMEOUT) == 0) p.status->where = 192 + where;
 }
 
-__device__ __forceinline__ void tile_of(const Params& p, int t, int& mt, int& nt)
+// Item i of the launch: (row tile, column tile) and K steps [k0, k1).  Splits outside, so that the pairs in flight share
+// the same K range; row tiles in groups of kGroupM, column tiles outside, row tiles inside, so that they share a few
+// column tiles of B and the group's rows of A in L2.
+struct Item {
+    int mt, nt, split, k0, k1;
+};
+__device__ __forceinline__ Item item_of(const Params& p, int i)
 {
-    const int per_group = kGroupM * p.n_tiles, g = t / per_group;
+    Item t;
+    const int tiles = p.m_tiles * p.n_tiles;
+    t.split = i / tiles;
+    i -= t.split * tiles;
+    const int per_group = kGroupM * p.n_tiles, g = i / per_group;
     const int rows = min(kGroupM, p.m_tiles - g * kGroupM);
-    t -= g * per_group;
-    nt = t / rows;
-    mt = g * kGroupM + t - nt * rows;
+    i -= g * per_group;
+    t.nt = i / rows;
+    t.mt = g * kGroupM + i - t.nt * rows;
+    t.k0 = (int)((long long)p.k_steps * t.split / p.splits);
+    t.k1 = (int)((long long)p.k_steps * (t.split + 1) / p.splits);
+    return t;
 }
 
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32])
@@ -67,196 +98,201 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32])
     reg_fence(*reinterpret_cast<float(*)[16]>(&v[16]));
 }
 
+// -- of a pair of CTAs
 
-// Y of 32 columns: v += bias, Z kept, phi, + residual, one rounding.
-template <bool EPI>
-__device__ __forceinline__ void finish(const Params& p, size_t at, int f0, float (&v)[32])
+// A box into this CTA's shared memory, its bytes counted at an mbarrier of either CTA of the pair.
+__device__ __forceinline__ void pair_load_2d(uint32_t dst, const void* map, uint32_t bar, int x, int y)
 {
-    if constexpr (EPI) {
-        if (p.bias)
-#pragma unroll
-            for (int e = 0; e < 32; e += 8)
-                if (f0 + e < p.N) {
-                    float b[8];
-                    load16(p.bias + f0 + e, b);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[e + j] += b[j];
-                }
-        if (p.Z)
-#pragma unroll
-            for (int e = 0; e < 32; e += 8)
-                if (f0 + e < p.N) {
-                    float* z = p.Z + at + f0 + e;
-                    uint32_t w[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[e + j]);
-                    if (p.wide) {
-                        st_global32(z, w);
-                    } else {
-                        *reinterpret_cast<uint4*>(z) = make_uint4(w[0], w[1], w[2], w[3]);
-                        *reinterpret_cast<uint4*>(z + 4) = make_uint4(w[4], w[5], w[6], w[7]);
-                    }
-                }
-        if (p.act != ROLA_LOWRANK_ACT_IDENTITY)
-            with_act(p.act, [&](auto act) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = act.phi(v[j]);
-            });
-        if (p.residual)
-#pragma unroll
-            for (int e = 0; e < 32; e += 8)
-                if (f0 + e < p.N) {
-                    float r[8];
-                    load16(p.residual + at + f0 + e, r);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[e + j] += r[j];
-                }
-    }
-#pragma unroll
-    for (int e = 0; e < 32; e += 16) {
-        uint32_t y[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = pack_bf16(v[e + 2 * j], v[e + 2 * j + 1]);
-        __nv_bfloat16* row = p.c + at + f0 + e;
-        if (f0 + e + 16 <= p.N) store_row32(row, y, p.wide);
-        else if (f0 + e < p.N) *reinterpret_cast<uint4*>(row) = make_uint4(y[0], y[1], y[2], y[3]);
-    }
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n" ::"r"(
+            dst),
+        "l"(map), "r"(bar), "r"(x), "r"(y)
+        : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi,
+                                         uint32_t idesc, uint32_t accum)
+{
+    asm volatile(
+        "{\n.reg .pred p;\n.reg .b64 da, db;\n"
+        "setp.ne.b32 p, %6, 0;\n"
+        "mov.b64 da, {%1, %2};\n"
+        "mov.b64 db, {%3, %4};\n"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %5, p;\n}\n" ::"r"(d_tmem),
+        "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accum)
+        : "memory");
+}
+// Arrives on the mbarrier at this offset in both CTAs when every product issued so far is done.
+__device__ __forceinline__ void pair_commit(uint32_t bar)
+{
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n" ::"r"(bar),
+        "h"((uint16_t)3)
+        : "memory");
+}
+__device__ __forceinline__ void remote_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_tmem_alloc(uint32_t dst_smem, uint32_t ncols)
+{
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(dst_smem), "r"(ncols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
+}
+__device__ __forceinline__ void pair_tmem_dealloc(uint32_t taddr, uint32_t ncols)
+{
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(taddr), "r"(ncols) : "memory");
 }
 
-template <bool AMn, bool BMn, bool EPI>
-__global__ void __launch_bounds__(kThreads, 1) linear_gemm_kernel(const __grid_constant__ Params p)
+// END: the sums become outputs here (bias, phi, residual), PLAIN: rounded only, PART: kept in fp32 for a join.
+enum Out { END, PLAIN, PART };
+
+template <bool AMn, bool BMn, int OUT, int NT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear_gemm_kernel(const __grid_constant__ Params p)
 {
+    using C = Cfg<NT>;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    if (smem_u32(smem_raw) & 1023u) {     // the 128-byte swizzle atoms need a 1024-byte aligned base
-        if (threadIdx.x == 0) atomicCAS(&p.status->code, 0, (int)ROLA_ERR_UNSUPPORTED);
-        return;
-    }
-    Ctrl& cb = *reinterpret_cast<Ctrl*>(smem_raw + kSmemTiles);
-    const uint32_t sbase = smem_u32(smem_raw);
+    const uint32_t sbase = smem_u32(smem_raw);           // 1024-byte aligned: there is no static shared memory
+    Ctrl& cb = *reinterpret_cast<Ctrl*>(smem_raw + kRingBytes);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = cluster_rank();
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     auto bar = [&](int i) { return smem_u32(&cb.bar[i]); };
     if (tid == 0) {
         cb.abort = 0;
-        for (int i = 0; i < kStages; ++i) {
-            mbar_init(bar(FULL + i), 1);
-            mbar_init(bar(EMPTY + i), 1);
+        for (int i = 0; i < C::kStages; ++i) {
+            mbar_init(bar(C::FULL + i), 1);
+            mbar_init(bar(C::EMPTY + i), 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(ACC_FULL + i), 1);
-            mbar_init(bar(ACC_EMPTY + i), kEpiWarps);
+            mbar_init(bar(C::ACC_FULL + i), 1);
+            mbar_init(bar(C::ACC_EMPTY + i), 2 * kEpiWarps);
         }
-        mbar_init(bar(DRAIN), 1);
+        mbar_init(bar(C::DRAIN), 1);
         fence_mbar_init();
+        // before any CTA can record a timeout, which takes 1 ms at least
+        if (p.clear && blockIdx.x == 0) p.status->code = p.status->where = 0;
     }
-    if (warp == 1) {
-        tmem_alloc(smem_u32(&cb.tmem_base), 2 * kTileN);
-        tmem_relinquish();
-    }
+    if (warp == 1) pair_tmem_alloc(smem_u32(&cb.tmem_base), 2 * NT);
     fence_before_sync();
-    __syncthreads();
+    cluster_sync();
     fence_after_sync();
     const uint32_t tmem = cb.tmem_base;
     volatile int* abort = &cb.abort;
     const uint64_t limit = p.wait_limit_ns;
-    const int tiles = p.m_tiles * p.n_tiles;
+    const int items = p.m_tiles * p.n_tiles * p.splits;
 
     if (warp == 0) {
         // ------------------------------------------------------------ TMA producer: a box per lane
-        constexpr int kABoxes = AMn ? 2 : 1, kBBoxes = BMn ? kTileN / 64 : 1;
+        constexpr int kABoxes = AMn ? 2 : 1, kBBoxes = BMn ? NT / 128 : 1;
+        constexpr uint32_t kBBox = BMn ? 8192 : C::kBBytes;
         bool ok = true;
-        int g = 0;
-        for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
-            int mt, nt;
-            tile_of(p, t, mt, nt);
-            for (int ks = 0; ks < p.k_steps; ++ks, ++g) {
-                const int s = g % kStages, k0 = ks * kStepK;
-                if (g >= kStages) ok = mbar_wait(bar(EMPTY + s), ((g / kStages) - 1) & 1, abort, limit);
+        int g = 0;                                       // K steps issued by this CTA
+        for (int i = pair; i < items && ok; i += pairs) {
+            const Item t = item_of(p, i);
+            const int m0 = t.mt * kTileM + rank * kHalfM, n0 = t.nt * NT + rank * (NT / 2);
+            for (int ks = t.k0; ks < t.k1; ++ks, ++g) {
+                const int s = g % C::kStages, k0 = ks * kStepK;
+                if (g >= C::kStages) ok = mbar_wait(bar(C::EMPTY + s), ((g / C::kStages) - 1) & 1, abort, limit);
                 ok = __shfl_sync(0xffffffffu, ok, 0);
                 if (!ok) break;
-                const bool skip = p.skip_first && g == 0;
-                if (lane == 0 && !skip) mbar_expect_tx(bar(FULL + s), kStageBytes);
+                if (p.skip_first && g == 0) continue;
+                if (lane == 0 && rank == 0) mbar_expect_tx(bar(C::FULL + s), 2 * C::kStageBytes);
                 __syncwarp();
-                const uint32_t dst = sbase + s * kStageBytes;
-                if (lane < kABoxes && !skip)
-                    tma_load_2d(dst + lane * 8192, &p.a, bar(FULL + s), AMn ? mt * kTileM + lane * 64 : k0, AMn ? k0 : mt * kTileM);
+                const uint32_t dst = sbase + s * C::kStageBytes, full = peer(bar(C::FULL + s), 0);
+                if (lane < kABoxes)
+                    pair_load_2d(dst + lane * 8192, &p.a, full, AMn ? m0 + lane * 64 : k0, AMn ? k0 : m0);
                 const int bl = lane - 2;
-                if (bl >= 0 && bl < kBBoxes && !skip)
-                    tma_load_2d(dst + kABytes + bl * 8192, &p.b, bar(FULL + s), BMn ? nt * kTileN + bl * 64 : k0,
-                                BMn ? k0 : nt * kTileN);
+                if (bl >= 0 && bl < kBBoxes)
+                    pair_load_2d(dst + kABytes + bl * kBBox, &p.b, full, BMn ? n0 + bl * 64 : k0, BMn ? k0 : n0);
             }
         }
         if (!ok && lane == 0) record_timeout(p, 1);
-        // the copies still in flight land before the CTA exits
+        // the pair's copies still in flight land, and the commits of its last products arrive, before either CTA goes on
+        // to the last barrier and may leave
         if (lane == 0) {
             int never = 0;
-            for (int u = g > kStages ? g - kStages : 0; u < g; ++u)
-                mbar_wait(bar(FULL + u % kStages), (u / kStages) & 1, &never, limit);
+            for (int u = g > C::kStages ? g - C::kStages : 0; u < g; ++u) {
+                if (rank == 0) mbar_wait(bar(C::FULL + u % C::kStages), (u / C::kStages) & 1, &never, limit);
+                if (!*abort && ok) ok = mbar_wait(bar(C::EMPTY + u % C::kStages), (u / C::kStages) & 1, abort, limit);
+            }
         }
+        __syncwarp();
     } else if (warp == 1) {
-        // ------------------------------------------------------------ products
-        if (lane == 0) {
-            const uint32_t idesc = idesc_bf16(kTileM, kTileN, AMn, BMn);
+        // ------------------------------------------------------------ products, issued by the first CTA
+        if (lane == 0 && rank == 0) {
+            const uint32_t idesc = idesc_bf16(kTileM, NT, AMn, BMn);
             const uint64_t da = smem_desc(sbase, AMn ? 8192 : 16, 1024), db = smem_desc(sbase + kABytes, BMn ? 8192 : 16, 1024);
             const uint32_t a_lo = (uint32_t)da, a_hi = (uint32_t)(da >> 32), b_lo = (uint32_t)db, b_hi = (uint32_t)(db >> 32);
             constexpr uint32_t a_k = AMn ? 128 : 2, b_k = BMn ? 128 : 2;    // 16 k: 16 rows of 128 B, or 32 B of a row
             bool ok = true;
             int g = 0, it = 0;
-            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x, ++it) {
+            for (int i = pair; i < items && ok; i += pairs, ++it) {
+                const Item t = item_of(p, i);
                 const int ab = it & 1;
-                if (it >= 2 && !(ok = mbar_wait(bar(ACC_EMPTY + ab), ((it >> 1) - 1) & 1, abort, limit))) break;
+                if (it >= 2 && !(ok = mbar_wait(bar(C::ACC_EMPTY + ab), ((it >> 1) - 1) & 1, abort, limit))) break;
                 fence_after_sync();
-                for (int ks = 0; ks < p.k_steps; ++ks, ++g) {
-                    const int s = g % kStages;
-                    if (!(ok = mbar_wait(bar(FULL + s), (g / kStages) & 1, abort, limit))) break;
+                for (int ks = t.k0; ks < t.k1; ++ks, ++g) {
+                    const int s = g % C::kStages;
+                    if (!(ok = mbar_wait(bar(C::FULL + s), (g / C::kStages) & 1, abort, limit))) break;
                     fence_after_sync();
-                    const uint32_t off = s * (kStageBytes >> 4);
+                    const uint32_t off = s * (C::kStageBytes >> 4);
 #pragma unroll
                     for (int kk = 0; kk < kStepK / 16; ++kk)
-                        mma_ss_split(tmem + ab * kTileN, a_lo + off + kk * a_k, a_hi, b_lo + off + kk * b_k, b_hi, idesc,
-                                     (ks > 0 || kk > 0) ? 1u : 0u);
-                    mma_commit(bar(EMPTY + s));
+                        pair_mma(tmem + ab * NT, a_lo + off + kk * a_k, a_hi, b_lo + off + kk * b_k, b_hi, idesc,
+                                 (ks > t.k0 || kk > 0) ? 1u : 0u);
+                    pair_commit(bar(C::EMPTY + s));
                 }
                 if (!ok) break;
-                mma_commit(bar(ACC_FULL + ab));
+                pair_commit(bar(C::ACC_FULL + ab));
             }
             if (!ok) record_timeout(p, 2);
-            // every product issued completes before TMEM is released
-            int never = 0;
-            mma_commit(bar(DRAIN));
-            mbar_wait(bar(DRAIN), 0, &never, limit);
+            pair_commit(bar(C::DRAIN));
         }
+        // every product issued completes, and says so to both CTAs, before TMEM is released
+        if (lane == 0) {
+            int never = 0;
+            mbar_wait(bar(C::DRAIN), 0, &never, 2 * limit);
+        }
+        __syncwarp();
     } else {
         // ------------------------------------------------------------ epilogue: two warps for each quarter of the rows
         const int q = warp & 3, half = (warp - 2) >> 2;
         const uint32_t lane_off = (uint32_t)(q * 32) << 16;
-        constexpr int kChunks = kTileN / 2 / 32;
+        constexpr int kChunks = NT / 2 / 32;
         bool ok = true;
         int it = 0;
-        for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x, ++it) {
-            int mt, nt;
-            tile_of(p, t, mt, nt);
+        for (int i = pair; i < items && ok; i += pairs, ++it) {
+            const Item t = item_of(p, i);
             const int ab = it & 1;
-            if (!(ok = mbar_wait_warp(bar(ACC_FULL + ab), (it >> 1) & 1, abort, limit))) break;
+            if (!(ok = mbar_wait_warp(bar(C::ACC_FULL + ab), (it >> 1) & 1, abort, limit))) break;
             fence_after_sync();
-            const int row = mt * kTileM + q * 32 + lane;
+            const int row = t.mt * kTileM + rank * kHalfM + q * 32 + lane;
             for (int c = 0; c < kChunks; ++c) {
-                const int col = half * (kTileN / 2) + c * 32;
+                const int col = half * (NT / 2) + c * 32, f0 = t.nt * NT + col;
                 float v[32];
-                tmem_ld32(tmem + lane_off + ab * kTileN + col, v);
+                tmem_ld32(tmem + lane_off + ab * NT + col, v);
                 if (c == kChunks - 1) {          // in registers: the buffer is free for the tile after next
                     fence_before_sync();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(ACC_EMPTY + ab));
+                    if (lane == 0) remote_arrive(peer(bar(C::ACC_EMPTY + ab), 0));
                 }
-                if (row < p.M) finish<EPI>(p, (size_t)row * p.N, nt * kTileN + col, v);
+                if (row >= p.M) continue;
+                if constexpr (OUT == PART) {
+                    float* to = p.part + ((size_t)t.split * p.M + row) * p.N + f0;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8)
+                        if (f0 + e < p.N) put8(to + e, v + e, p.end.wide);
+                } else {
+                    linear_end<OUT == END>(p.end, (size_t)row * p.N, f0, p.N, v);
+                }
             }
         }
         if (!ok) record_timeout(p, 3);
     }
     fence_before_sync();
-    __syncthreads();
+    cluster_sync();                                      // the pair's shared memory and TMEM stay until both are done
     fence_after_sync();
-    if (warp == 1) tmem_dealloc(tmem, 2 * kTileN);
+    if (warp == 1) pair_tmem_dealloc(tmem, 2 * NT);
 }
 
 // ---------------------------------------------------------------- host side
@@ -268,63 +304,97 @@ bool operand_map(CUtensorMap* m, const void* p, int rows, int cols, bool kc, int
                      CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <bool AMn, bool BMn, bool EPI>
-cudaError_t launch(const LinShape& s, Params& p, int M, int N, int K, DeviceStatus* status, cudaStream_t st)
+template <bool AMn, bool BMn, int OUT, int NT>
+cudaError_t launch(const LinShape& s, Params& p, int pairs, cudaStream_t st)
 {
+    const size_t smem = kRingBytes + sizeof(Ctrl);
+    auto kernel = linear_gemm_kernel<AMn, BMn, OUT, NT>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    const int items = p.m_tiles * p.n_tiles * p.splits;
+    kernel<<<2 * (items < pairs ? items : pairs), kThreads, smem, st>>>(p);
+    return cudaGetLastError();
+}
+
+// C [M][N] = sum over K of A B; OUT: END or PLAIN (without splits).
+template <bool AMn, bool BMn, int OUT>
+cudaError_t product(const LinShape& s, const void* A, const void* B, int M, int N, int K, const LinearEnd& end, float* part,
+                    bool clear, DeviceStatus* status, cudaStream_t st)
+{
+    const LinearPlan plan = linear_plan(M, N, K);
+    Params p{};
     p.M = M; p.N = N;
     p.m_tiles = (M + kTileM - 1) / kTileM;
-    p.n_tiles = (N + kTileN - 1) / kTileN;
+    p.n_tiles = (N + plan.tile_n - 1) / plan.tile_n;
     p.k_steps = (K + kStepK - 1) / kStepK;
-    p.act = s.act;
-    p.wide = N % 16 == 0 && ((reinterpret_cast<uintptr_t>(p.c) | reinterpret_cast<uintptr_t>(p.Z)) & 31u) == 0;
+    p.splits = plan.splits;
+    p.end = end;
+    p.part = part;
+    p.clear = clear;
     p.status = status;
     p.wait_limit_ns = s.wait_limit_ns;
     p.skip_first = s.debug_flags & ROLA_DEBUG_SKIP_FIRST_K_COPY ? 1 : 0;
+    if (!operand_map(&p.a, A, AMn ? K : M, AMn ? M : K, !AMn, kHalfM) ||
+        !operand_map(&p.b, B, BMn ? K : N, BMn ? N : K, !BMn, plan.tile_n / 2))
+        return cudaErrorInvalidValue;
     int dev = 0, nsm = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     e = cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
-    const size_t smem = kSmemTiles + sizeof(Ctrl);
-    auto kernel = linear_gemm_kernel<AMn, BMn, EPI>;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    const int tiles = p.m_tiles * p.n_tiles;
-    kernel<<<tiles < nsm ? tiles : nsm, kThreads, smem, st>>>(p);
-    return cudaGetLastError();
+    const int pairs = nsm / 2;
+    auto go = [&](auto out) {
+        constexpr int O = decltype(out)::value;
+        return plan.tile_n == 256 ? launch<AMn, BMn, O, 256>(s, p, pairs, st) : launch<AMn, BMn, O, 128>(s, p, pairs, st);
+    };
+    if (plan.splits == 1) return go(std::integral_constant<int, OUT>());
+    e = go(std::integral_constant<int, PART>());
+    return e == cudaSuccess ? launch_linear_join(end, part, plan.splits, M, N, st) : e;
 }
 
 }  // namespace
 
-cudaError_t launch_linear_tc(const LinShape& s, const void* X, const void* W, const void* b, const void* R, void* Y,
-                             float* Z, DeviceStatus* status, cudaStream_t st)
+// Tile width and parts of K of least cost.  A pair takes 0.26 us a step of 64 k at 256 columns and 0.15 at 128, and some
+// 2 us at its ends that no other tile covers; parts are written and read once more in fp32 at some 5 TB/s, and their
+// join is a launch of 4 us.  76 pairs run at once.
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K)
 {
-    Params p{};
-    if (!operand_map(&p.a, X, s.M, s.K, true, kTileM) || !operand_map(&p.b, W, s.N, s.K, true, kTileN))
-        return cudaErrorInvalidValue;
-    p.c = static_cast<__nv_bfloat16*>(Y);
-    p.bias = static_cast<const __nv_bfloat16*>(b);
-    p.residual = static_cast<const __nv_bfloat16*>(R);
-    p.Z = Z;
-    return launch<false, false, true>(s, p, s.M, s.N, s.K, status, st);
+    const int64_t steps = (K + kStepK - 1) / kStepK;
+    LinearPlan best{256, 1};
+    double least = 1e30;
+    for (int tile_n : {256, 128})
+        for (int64_t splits = 1; splits <= 16 && splits * 4 <= steps + 3; ++splits) {
+            const int64_t items = ((M + kTileM - 1) / kTileM) * ((N + tile_n - 1) / tile_n) * splits;
+            const double turns = (double)((items + 75) / 76);
+            const double us = turns * (double)((steps + splits - 1) / splits) * (tile_n == 256 ? 0.26 : 0.15) + 2.0 +
+                              (splits > 1 ? 4.0 + 8.0 * (double)(splits * M * N) / 5e6 : 0.0);
+            if (us < least * 0.999) {
+                least = us;
+                best = {tile_n, (int)splits};
+            }
+        }
+    return best;
 }
 
-cudaError_t launch_linear_backward_tc(const LinShape& s, const void* X, const void* W, const void* dZ, void* dX,
-                                      void* dW, DeviceStatus* status, cudaStream_t st)
+cudaError_t launch_linear_tc(const LinShape& s, const void* X, const void* W, const void* b, const void* R, void* Y,
+                             float* Z, float* part, DeviceStatus* status, cudaStream_t st)
 {
-    if (dX) {
-        Params p{};
-        if (!operand_map(&p.a, dZ, s.M, s.N, true, kTileM) || !operand_map(&p.b, W, s.N, s.K, false, 0))
-            return cudaErrorInvalidValue;
-        p.c = static_cast<__nv_bfloat16*>(dX);
-        cudaError_t e = launch<false, true, false>(s, p, s.M, s.K, s.N, status, st);
-        if (e != cudaSuccess) return e;
-    }
-    if (!dW) return cudaSuccess;
-    Params p{};                                  // k = token
-    if (!operand_map(&p.a, dZ, s.M, s.N, false, 0) || !operand_map(&p.b, X, s.M, s.K, false, 0)) return cudaErrorInvalidValue;
-    p.c = static_cast<__nv_bfloat16*>(dW);
-    return launch<true, true, false>(s, p, s.N, s.K, s.M, status, st);
+    const LinearEnd end = linear_end_of(Y, b, R, Z, s.N, s.act);
+    return product<false, false, END>(s, X, W, s.M, s.N, s.K, end, part, true, status, st);
+}
+
+cudaError_t launch_linear_dx_tc(const LinShape& s, const void* W, const void* dZ, void* dX, float* part, bool clear,
+                                DeviceStatus* status, cudaStream_t st)
+{
+    const LinearEnd end = linear_end_of(dX, nullptr, nullptr, nullptr, s.K, ROLA_LOWRANK_ACT_IDENTITY);
+    return product<false, true, PLAIN>(s, dZ, W, s.M, s.K, s.N, end, part, clear, status, st);
+}
+
+cudaError_t launch_linear_dw_tc(const LinShape& s, const void* X, const void* dZ, void* dW, float* part, bool clear,
+                                DeviceStatus* status, cudaStream_t st)
+{
+    const LinearEnd end = linear_end_of(dW, nullptr, nullptr, nullptr, s.K, ROLA_LOWRANK_ACT_IDENTITY);
+    return product<true, true, PLAIN>(s, dZ, X, s.N, s.K, s.M, end, part, clear, status, st);     // k = token
 }
 
 }  // namespace rola

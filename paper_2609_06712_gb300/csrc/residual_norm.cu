@@ -207,6 +207,19 @@ constexpr uint64_t kWaitLimitNs = 2000000000ull;     // bound of the wait for a 
 template <int V, int EL>
 __device__ __forceinline__ float (&slice(float (&v)[EL], int i))[V] { return reinterpret_cast<float(&)[V]>(v[i * V]); }
 
+// v = 0 past the row's end.
+template <int V, bool FULL, int EL>
+__device__ __forceinline__ void clear_rest(int gt, int tpr, int pieces, float (&v)[EL])
+{
+    if constexpr (!FULL)
+#pragma unroll
+        for (int i = 0; i < EL / V; ++i) {
+            const bool in = gt + i * tpr < pieces;
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[i * V + e] = in ? v[i * V + e] : 0.0f;
+        }
+}
+
 // Pieces are 16 bytes where every row starts at a multiple of them, else one element, or two of bf16 where the width
 // and the pointers allow 4 bytes.
 template <typename T, int V>
@@ -326,37 +339,38 @@ struct Feed {
     __device__ __forceinline__ void read(const RnShape& sh, const RnArgs& a, int n, uint32_t skip, long long r,
                                          float (&v)[EL]) const
     {
-        constexpr int NV = EL / V;
         const int pieces = sh.d / V;
         const uint32_t at = here + skip + offset(sh, a, n, r);
+        if (!a.in[n]) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = gt + i * tpr;
-            if (a.in[n] && (FULL || c < pieces)) {
-                if constexpr (V * sizeof(T) == 16) {
-                    Piece<T, V> x;
-                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n"
-                                 : "=r"(x.w.x), "=r"(x.w.y), "=r"(x.w.z), "=r"(x.w.w)
-                                 : "r"(at + c * 16)
-                                 : "memory");
-                    unpack<T, V>(x, slice<V>(v, i));
-                } else if constexpr (sizeof(T) == 4) {
-                    asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v[i]) : "r"(at + c * 4) : "memory");
-                } else if constexpr (V == 2) {
-                    uint32_t x;
-                    asm volatile("ld.shared.u32 %0, [%1];\n" : "=r"(x) : "r"(at + c * 4) : "memory");
-                    v[2 * i] = __uint_as_float(x << 16);
-                    v[2 * i + 1] = __uint_as_float(x & 0xffff0000u);
-                } else {
-                    uint16_t x;
-                    asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(x) : "r"(at + c * 2) : "memory");
-                    v[i] = __uint_as_float((uint32_t)x << 16);
-                }
+            for (int e = 0; e < EL; ++e) v[e] = 0.0f;
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < EL / V; ++i) {
+            // past the row's end its last piece is read and cleared: no branch
+            const int c = gt + i * tpr, k = FULL ? c : min(c, pieces - 1);
+            if constexpr (V * sizeof(T) == 16) {
+                Piece<T, V> x;
+                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n"
+                             : "=r"(x.w.x), "=r"(x.w.y), "=r"(x.w.z), "=r"(x.w.w)
+                             : "r"(at + k * 16)
+                             : "memory");
+                unpack<T, V>(x, slice<V>(v, i));
+            } else if constexpr (sizeof(T) == 4) {
+                asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v[i]) : "r"(at + k * 4) : "memory");
+            } else if constexpr (V == 2) {
+                uint32_t x;
+                asm volatile("ld.shared.u32 %0, [%1];\n" : "=r"(x) : "r"(at + k * 4) : "memory");
+                v[2 * i] = __uint_as_float(x << 16);
+                v[2 * i + 1] = __uint_as_float(x & 0xffff0000u);
             } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e) v[i * V + e] = 0.0f;
+                uint16_t x;
+                asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(x) : "r"(at + k * 2) : "memory");
+                v[i] = __uint_as_float((uint32_t)x << 16);
             }
         }
+        clear_rest<V, FULL>(gt, tpr, pieces, v);
     }
     __device__ __forceinline__ void refill(const RnShape& sh, const RnArgs& a)       // after every thread of the group has read
     {
@@ -508,17 +522,6 @@ __device__ __forceinline__ void scaled_add(float (&t)[EL], const float (&v)[EL],
     for (int e = 0; e < EL; e += 2) fma2(&t[e], &v[e], kk, &t[e]);
 }
 
-// v = 0 past the row's end.
-template <int V, bool FULL, int EL>
-__device__ __forceinline__ void clear_rest(int gt, int tpr, int pieces, float (&v)[EL])
-{
-    if constexpr (!FULL)
-#pragma unroll
-        for (int i = 0; i < EL / V; ++i)
-            if (gt + i * tpr >= pieces)
-#pragma unroll
-                for (int e = 0; e < V; ++e) v[i * V + e] = 0.0f;
-}
 // This thread's pieces of a row into `row`.
 template <typename T, int V, bool FULL, int EL>
 __device__ __forceinline__ void put_row(T* row, int gt, int tpr, int pieces, float (&v)[EL])
@@ -1002,7 +1005,10 @@ cudaError_t fwd(const RnShape& s, RnArgs& a, cudaStream_t st)
 {
     if (s.d <= 256) return fwd_one<T, V, 8, true, 128, 6>(s, a, st);
     if (s.d <= 512) return fwd_one<T, V, 16, true, 128, 4>(s, a, st);
-    constexpr int kFewer = !kWide<T, V>;                   // CTAs: addresses of single elements take more registers
+    // single elements take more instructions a row, and more warps hide them (32760 x 1537: ... us with 16 a thread)
+    if constexpr (V == 1)
+        if (s.d <= 8 * 256) return fwd_one<T, V, 8, false, 256, 3>(s, a, st);
+    constexpr int kFewer = !kWide<T, V>;             // CTAs: addresses of small pieces take more registers
     if (s.d <= 16 * 160) return fwd_one<T, V, 16, false, 160, 3 - kFewer>(s, a, st);
     if (s.d <= 16 * 320) return fwd_one<T, V, 16, false, 320, 2 - kFewer>(s, a, st);
     if (s.d <= 16 * 512) return fwd_one<T, V, 16, false, 512, 1>(s, a, st);
