@@ -35,14 +35,11 @@ cudaError_t launch_linear_dx_tc(const LinShape& s, const void* W, const void* dZ
 cudaError_t launch_linear_dw_tc(const LinShape& s, const void* X, const void* dZ, void* dW, float* part, bool clear,
                                 DeviceStatus* status, cudaStream_t st);
 
-// Columns of a tile (256 or 128) and parts of the K axis of a product [M][N] over K on tensor cores.
-struct LinearPlan {
-    int tile_n, splits;
-};
-LinearPlan linear_plan(int64_t M, int64_t N, int64_t K);
+// Parts of the K axis of a product [M][N] over K on tensor cores.
+int linear_splits(int64_t M, int64_t N, int64_t K);
 inline size_t linear_part_bytes(int64_t M, int64_t N, int64_t K)
 {
-    const int splits = linear_plan(M, N, K).splits;
+    const int splits = linear_splits(M, N, K);
     return splits > 1 ? 4 * (size_t)splits * M * N : 0;
 }
 

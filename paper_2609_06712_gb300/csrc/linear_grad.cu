@@ -105,8 +105,25 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const LinearEnd end, c
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += x[e];
     }
-    const int f0 = (int)(at % N);
-    linear_end<true>(end, at - f0, f0, N, v);
+    if (end.bias) {
+        float b[8];
+        load8(end.bias + at % N, b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += b[e];
+    }
+    if (end.Z) store8(end.Z + at, v);
+    if (end.act != ROLA_LOWRANK_ACT_IDENTITY)
+        with_act(end.act, [&](auto act) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = act.phi(v[e]);
+        });
+    if (end.residual) {
+        float r[8];
+        load8(end.residual + at, r);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += r[e];
+    }
+    store8(end.c + at, v);
 }
 
 template <typename T>

@@ -34,6 +34,19 @@ bool encode_2d(CUtensorMap* m, CUtensorMapDataType type, int esz, const void* pt
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool encode_parts(CUtensorMap* m, const float* ptr, int64_t parts, int64_t rows, int64_t cols)
+{
+    const auto enc = encoder();
+    if (!enc) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
+    const cuuint64_t strides[2] = {(cuuint64_t)cols * 4, (cuuint64_t)rows * cols * 4};
+    const cuuint32_t box[3] = {32, 32, 1};
+    const cuuint32_t step[3] = {1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<float*>(ptr), dims, strides, box, step,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool encode_rows(CUtensorMap* m, const void* ptr, int64_t rows, int64_t heads, int box_rows)
 {
     const auto enc = encoder();

@@ -14,6 +14,9 @@ namespace rola {
 bool encode_2d(CUtensorMap* m, CUtensorMapDataType type, int esz, const void* ptr, int64_t rows, int64_t cols,
                int box_cols, int box_rows, CUtensorMapSwizzle swizzle);
 
+// [parts][rows][cols] fp32 (cols a multiple of 4), boxes of one part's 32 rows x 32 columns in 128-byte swizzle.
+bool encode_parts(CUtensorMap* m, const float* ptr, int64_t parts, int64_t rows, int64_t cols);
+
 namespace tc {
 
 // x * element size must be a multiple of 16.
@@ -24,6 +27,21 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* map, uint3
             dst),
         "l"(map), "r"(bar), "r"(x), "r"(y)
         : "memory");
+}
+
+// Stores of a box from shared memory (bulk-group completion); the coordinates lie inside the tensor, and what of the
+// box does not is not written.
+__device__ __forceinline__ void tma_store_2d(const void* map, uint32_t src, int x, int y)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];\n" ::"l"(map), "r"(src),
+                 "r"(x), "r"(y)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const void* map, uint32_t src, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];\n" ::"l"(map), "r"(src),
+                 "r"(x), "r"(y), "r"(z)
+                 : "memory");
 }
 
 }  // namespace tc
