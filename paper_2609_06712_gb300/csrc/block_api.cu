@@ -136,7 +136,7 @@ LinShape make_shape(const rola_linear_config_t& c)
 enum LinearForm { kLinearByRows, kLinearFew, kLinearTiles };
 LinearForm linear_form(const LinShape& s)
 {
-    return s.M <= kLinearRows ? kLinearByRows : linear_few(s) ? kLinearFew : kLinearTiles;
+    return linear_by_rows(s) ? kLinearByRows : linear_few(s) ? kLinearFew : kLinearTiles;
 }
 LinearForm linear_dx_form(const LinShape& s) { return s.M <= kFfnFewTokens ? kLinearFew : kLinearTiles; }
 

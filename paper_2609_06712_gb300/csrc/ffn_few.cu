@@ -31,6 +31,7 @@
 #include "block_ops.cuh"
 #include "cluster.cuh"
 #include "linear.cuh"
+#include "linear_finish.cuh"
 #include "tcgen05.cuh"
 #include "tma_2d.cuh"
 
@@ -278,10 +279,7 @@ __global__ void __launch_bounds__(kThreads, 2) ffn_few_kernel(const __grid_const
                 x[0] += b.x; x[1] += b.y; x[2] += b.z; x[3] += b.w;
             }
             if (p.G) *reinterpret_cast<float4*>(p.G + at) = make_float4(x[0], x[1], x[2], x[3]);
-            with_act(p.act, [&](auto act) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = act.phi(x[e]);
-            });
+            linear_phi(p.act, x);
             if (p.residual) {
                 const float4 r = load4(p.residual + at);
                 x[0] += r.x; x[1] += r.y; x[2] += r.z; x[3] += r.w;
@@ -429,12 +427,15 @@ cudaError_t launch_ffn_few_grad(const FfnShape& s, const void* Wg, const void* W
     return launch<kDX>(s, p, true, status, st);
 }
 
-// As ffn_few, of one product.
+// One tile of up to 96 tokens, and up to seven while the weights that they all read stay below 3.2e7 elements.  Us, this
+// form / tiles of CTA pairs, weights from HBM:
+//   1536 x 1536: 128 tokens 7.5 / 11.4, 672 11.3 / 14.2;  1536 x 6144: 256 tokens 14.2 / 15.3, 384 22.1 / 15.7
+//   8192 x 1024: 384 tokens 16.2 / 16.9, 514 20.6 / 18.2;  1536 x 9216: 192 tokens 14.9 / 15.7, 256 21.4 / 15.7
+//   5120 x 5120: 96 tokens 16.1 / 19.3, 128 20.4 / 19.8;  5120 x 30720: 96 tokens 62 / 66, 128 101 / 66
 bool linear_few(const LinShape& s)
 {
     const int64_t tiles = (s.M + kMaxTokens - 1) / kMaxTokens;
-    return tiles == 1 || (tiles <= 7 && tiles * s.K * s.N <= 150000000 &&
-                          (int64_t)((s.M + 127) / 128) * ((s.N + 255) / 256) < 76);
+    return tiles == 1 || (tiles <= 7 && tiles * s.K * s.N <= 32000000);
 }
 
 cudaError_t launch_linear_few(const LinShape& s, const void* X, const void* W, const void* b, const void* R, void* Y,

@@ -14,9 +14,9 @@ struct LinShape {
 // Z = X W^T + b, Y = R + phi(Z); b, R and Z may be NULL
 cudaError_t launch_linear_simt(const LinShape& s, const void* X, const void* W, const void* b, const void* R, void* Y,
                                float* Z, cudaStream_t st);                                                 // fp32
-// bf16, by tokens: up to kLinearRows weight rows against them, then weight tiles against few tokens, then 256-token tiles
-// on tensor cores.  Each clears the status word.
-constexpr int kLinearRows = 4;
+// bf16, by tokens: weight rows against up to four, then weight tiles against few tokens, then 256-token tiles on tensor
+// cores.  Each clears the status word.
+bool linear_by_rows(const LinShape& s);
 bool linear_few(const LinShape& s);
 cudaError_t launch_linear_rows(const LinShape& s, const void* X, const void* W, const void* b, const void* R, void* Y,
                                float* Z, DeviceStatus* status, cudaStream_t st);

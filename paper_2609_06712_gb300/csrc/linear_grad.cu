@@ -26,7 +26,28 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8])
 }
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) { store16(p, x); }
 
-// ACT: one of rola_lowrank_act_t (its accurate form: db is not rounded to bf16), or -1 without Z.
+// d *= phi'(z) of eight values.  bf16 layers take the fast forms of SiLU and GELU, whose errors (about 1e-6) are below
+// what the sums over d_in leave in z.
+template <typename T, int ACT>
+__device__ __forceinline__ void times_slope(float (&d)[8], float (&z)[8])
+{
+    if constexpr (sizeof(T) == 2 && ACT == ROLA_LOWRANK_ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) FastGelu::slope(*reinterpret_cast<float(*)[2]>(&z[e]));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] *= z[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float a, da;
+            if constexpr (sizeof(T) == 2 && ACT == ROLA_LOWRANK_ACT_SILU) FastSilu::grad(z[e], a, da);
+            else gate_act_grad(ACT, z[e], a, da);
+            d[e] *= da;
+        }
+    }
+}
+
+// ACT: one of rola_lowrank_act_t, or -1 without Z.
 template <typename T, int ACT>
 __global__ void __launch_bounds__(32 * kWarps) linear_grad_kernel(int M, int N, const T* __restrict__ dY,
                                                                   const float* __restrict__ Z, T* __restrict__ dZ,
@@ -47,12 +68,7 @@ __global__ void __launch_bounds__(32 * kWarps) linear_grad_kernel(int M, int N, 
             if constexpr (ACT >= 0) {
                 float z[8];
                 load8(Z + at, z);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float a, da;
-                    gate_act_grad(ACT, z[e], a, da);
-                    d[e] *= da;
-                }
+                times_slope<T, ACT>(d, z);
                 store8(dZ + at, d);
             }
 #pragma unroll
@@ -112,11 +128,7 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const LinearEnd end, c
         for (int e = 0; e < 8; ++e) v[e] += b[e];
     }
     if (end.Z) store8(end.Z + at, v);
-    if (end.act != ROLA_LOWRANK_ACT_IDENTITY)
-        with_act(end.act, [&](auto act) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = act.phi(v[e]);
-        });
+    linear_phi(end.act, v);
     if (end.residual) {
         float r[8];
         load8(end.residual + at, r);

@@ -2,7 +2,7 @@
 //
 //   Y = R + phi(X W^T + b)
 //
-// HBM-bound (two tokens at 5120 x 30720: 315 MB of weights, 46 us at the measured 6.8 TB/s).  A warp takes R weight rows, 16
+// For weights of up to 32 MB, whose time is latency: of the loads, of the sums, of the call.  A warp takes R weight rows, 16
 // bytes of each a lane and step, against all tokens, whose words it reads from L1; the products are added in fp32 in each
 // lane and then over the lanes.  Plain loads: with no tensor maps, shared-memory limits or clusters to set up a call costs
 // the host a launch, which is most of a small layer's time, and the weights need no more (a tile of the tensor cores would
@@ -109,6 +109,11 @@ cudaError_t rows_of(const LinShape& s, const void* X, const void* W, const void*
 }
 
 }  // namespace
+
+// Up to four tokens, and weights of up to 32 MB.  Us, this form / weight tiles (ffn_few.cu), weights from HBM, one token
+// and four:  256 x 1536: 2.0, 2.4 / 4.6, 4.8;  1536 x 9216: 7.2, 9.3 / 10.0, 10.3;  8192 x 1024: 6.3, 8.5 / 11.6, 11.6;
+// 4096 x 5120: 12.3, 16.1 / 11.5, 11.3;  5120 x 30720: 52, 94 / 51, 52.
+bool linear_by_rows(const LinShape& s) { return s.M <= 4 && (int64_t)s.K * s.N <= 16000000; }
 
 cudaError_t launch_linear_rows(const LinShape& s, const void* X, const void* W, const void* b, const void* R, void* Y,
                                float* Z, DeviceStatus* status, cudaStream_t st)

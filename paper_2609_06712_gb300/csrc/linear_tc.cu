@@ -56,6 +56,7 @@ enum Bar { FULL = 0, EMPTY = FULL + kMaxStages, ACC_FULL = EMPTY + kMaxStages, A
            DRAIN = ACC_EMPTY + 2, RES = DRAIN + 1, NUM_BARS = RES + kEpiWarps };
 struct Ctrl {
     uint64_t bar[NUM_BARS];
+    alignas(16) __nv_bfloat16 bias[kEpiWarps][kTileN / 2];   // of an epilogue warp's columns of the present tile
     uint32_t tmem_base;
     int abort;
 };
@@ -193,6 +194,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear_
         fence_mbar_init();
         // before any CTA can record a timeout, which takes 1 ms at least
         if (p.clear && blockIdx.x == 0) p.status->code = p.status->where = 0;
+        tma_prefetch_desc(&p.a);
+        tma_prefetch_desc(&p.b);
+        tma_prefetch_desc(&p.c);
     }
     if (warp == 1) pair_tmem_alloc(smem_u32(&cb.tmem_base), 2 * kTileN);
     fence_before_sync();
@@ -292,7 +296,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear_
         constexpr int kCols = OUT == PART ? 32 : 64, kChunks = kTileN / 2 / kCols;       // of a piece
         bool ok = true;
         int it = 0, asked = 0, got = 0;                  // residual pieces
-        // the piece is free (its last store has read it), and the residual's part at (x, y) on its way into it
+        // the piece is free (its last store has read it, and every lane the last tile's bias), and the residual's part at (x, y) on its way into it
         auto begin = [&](int x, int y) {
             if (lane == 0) {
                 bulk_wait_read_all();
@@ -308,6 +312,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear_
             const Item t = item_of(p, i);
             const int ab = it & 1, y = t.mt * kTileM + rank * kHalfM + q * 32, x0 = t.nt * kTileN + half * (kTileN / 2);
             begin(x0, y);
+            if (kEnd && p.bias) {                        // four columns a lane; N is a multiple of 8
+                const int x = min(x0 + lane * 4, p.N - 4);
+                *reinterpret_cast<uint2*>(&cb.bias[ew][lane * 4]) = *reinterpret_cast<const uint2*>(p.bias + x);
+                __syncwarp();
+            }
             if (!(ok = mbar_wait_warp(bar(ACC_FULL + ab), (it >> 1) & 1, abort, limit))) break;
             fence_after_sync();
             for (int c = 0; c < kChunks && ok; ++c) {
@@ -331,9 +340,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear_
                     if constexpr (kEnd) {
                         if (p.bias)
 #pragma unroll
-                            for (int e = 0; e < 32; e += 8) {            // N is a multiple of 8
+                            for (int e = 0; e < 32; e += 8) {
                                 float b[8];
-                                load16(p.bias + min(x + h * 32 + e, p.N - 8), b);
+                                load16(&cb.bias[ew][c * kCols + h * 32 + e], b);
 #pragma unroll
                                 for (int j = 0; j < 8; ++j) v[e + j] += b[j];
                             }
@@ -351,11 +360,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear_
                                 bulk_commit();
                             }
                         }
-                        if (p.act != ROLA_LOWRANK_ACT_IDENTITY)
-                            with_act(p.act, [&](auto act) {
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) v[j] = act.phi(v[j]);
-                            });
+                        linear_phi(p.act, v);
                         if (p.add)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
@@ -396,7 +401,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) linear_
         if (lane == 0) {                                 // what is in flight reads and writes this CTA's shared memory
             int never = 0;
             for (; got < asked; ++got) mbar_wait(bar(RES + ew), got & 1, &never, limit);
-            bulk_wait_all();
+            bulk_wait_read_all();
         }
         __syncwarp();
     }
