@@ -5,8 +5,15 @@
 namespace rola {
 namespace {
 
+// The driver's function, which wants a context on the calling thread: a thread's first call of the library may be one that
+// encodes a map before any other.
 PFN_cuTensorMapEncodeTiled_v12000 encoder()
 {
+    static thread_local bool bound = false;
+    if (!bound) {
+        int dev = 0;
+        bound = cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess;
+    }
     static const PFN_cuTensorMapEncodeTiled_v12000 enc = []() -> PFN_cuTensorMapEncodeTiled_v12000 {
         void* f = nullptr;
         cudaDriverEntryPointQueryResult q;

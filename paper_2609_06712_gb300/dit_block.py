@@ -7,11 +7,25 @@
 The norms, both attentions and the feed-forward are this library's operators with their backward passes; the
 linear projections are torch's.  ``python -m paper_2609_06712_gb300.dit_block`` takes a few training steps on a
 small synthetic layer and prints the loss of each.
+
+With a conditioning vector (``d_cond``) the block is modulated by it, sample by sample, and everything in it is this
+library's: a linear layer makes two shifts, scales and gates, and each branch joins the stream through its gate in the
+kernel that also makes the next branch's input:
+
+    shift_1, scale_1, gate_1, shift_2, scale_2, gate_2 = W_mod SiLU(cond) + b_mod
+    y = norm(x) (1 + scale_1) + shift_1
+    x, y = x + gate_1 W_o RoLA(y), norm of it
+    x, y = x + W_co attention(y, text), norm of it (1 + scale_2) + shift_2
+    x = x + gate_2 FFN(y)
+
+``--conditioned`` trains that form.
 """
 from __future__ import annotations
 
+import sys
+
 import torch
-from torch.nn.functional import linear
+from torch.nn.functional import linear, silu
 
 from . import rola
 
@@ -19,9 +33,11 @@ EPS = 1e-6
 
 
 class DiTBlock(torch.nn.Module):
-    """One block over the token grid of a layer config (configs.py); d_model = H * 128 + the text's width d_text."""
+    """One block over the token grid of a layer config (configs.py); d_model = H * 128 + the text's width d_text;
+    d_cond, if given, is the width of the conditioning vector of each sample."""
 
-    def __init__(self, cfg: dict, d_text: int, d_ff: int, act: str = "silu", dtype=torch.bfloat16, device="cuda"):
+    def __init__(self, cfg: dict, d_text: int, d_ff: int, act: str = "silu", dtype=torch.bfloat16, device="cuda",
+                 d_cond: int | None = None):
         super().__init__()
         self.cfg, self.H, self.act = rola.make_config(cfg, rola._DTYPES[dtype]), cfg["H"], act
         d, r = self.H * 128, cfg["r"]
@@ -35,6 +51,8 @@ class DiTBlock(torch.nn.Module):
         self.W_gate, self.W_up, self.W_down = weight(d_ff, d), weight(d_ff, d), weight(d, d_ff)
         self.norms = torch.nn.ParameterList(torch.nn.Parameter(t) for _ in range(3)
                                             for t in (torch.ones(d, **made), torch.zeros(d, **made)))
+        if d_cond is not None:
+            self.W_mod, self.b_mod = weight(6 * d, d_cond), torch.nn.Parameter(torch.zeros(6 * d, **made))
 
     def _norm(self, i, x):
         return rola.LayerNormFunction.apply(x, self.norms[2 * i], self.norms[2 * i + 1], EPS)
@@ -46,10 +64,33 @@ class DiTBlock(torch.nn.Module):
     def _join(self, o):
         return o.transpose(1, 2).reshape(o.shape[0], o.shape[2], self.H * 128)
 
-    def forward(self, x, text, text_len=None):
-        """x [B][N][d_model], text [B][L][d_text], text_len int32 [B] (None: the whole text)."""
+    def forward(self, x, text, text_len=None, cond=None):
+        """x [B][N][d_model], text [B][L][d_text], text_len int32 [B] (None: the whole text), cond [B][d_cond] of a
+        conditioned block."""
         with torch.cuda.device(x.device):            # the module launches on the current device
+            if cond is not None:
+                return self._conditioned(x, text, text_len, cond)
             return self._forward(x, text, text_len)
+
+    def _join_and_norm(self, i, x, h, gate, scale, shift):
+        """x + gate h, and norm i of it, scaled and shifted."""
+        return rola.ResidualNormFunction.apply(x, h, gate, None, self.norms[2 * i], self.norms[2 * i + 1], scale, shift,
+                                               "layer", "none", EPS)
+
+    def _conditioned(self, x, text, text_len, cond):
+        project = rola.LinearFunction.apply          # X, W, bias, residual, activation
+        mod = project(silu(cond), self.W_mod, self.b_mod, None, "identity").view(x.shape[0], 6, x.shape[2])
+        shift_1, scale_1, gate_1, shift_2, scale_2, gate_2 = mod.unbind(1)
+        _, y = self._join_and_norm(0, x, None, None, scale_1, shift_1)
+        q, k, v = self._heads(project(y, self.W_qkv, None, None, "identity"), 3)
+        h = self._join(rola.RoLAFunction.apply(self.cfg, q, k, v, self.P_q, self.P_k, None))
+        x, y = self._join_and_norm(1, x, project(h, self.W_o, None, None, "identity"), gate_1, None, None)
+        (q,) = self._heads(project(y, self.W_cq, None, None, "identity"), 1)
+        k, v = self._heads(project(text, self.W_ckv, None, None, "identity"), 2)
+        h = self._join(rola.AttentionFunction.apply(q, k, v, text_len, False))
+        x, y = self._join_and_norm(2, x, project(h, self.W_co, None, None, "identity"), None, scale_2, shift_2)
+        h = rola.FfnFunction.apply(y, self.W_gate, self.W_up, self.W_down, self.act)
+        return rola.ResidualNormFunction.apply(x, h, gate_2, None, None, None, None, None, "none", "none", EPS)[0]
 
     def _forward(self, x, text, text_len):
         q, k, v = self._heads(linear(self._norm(0, x), self.W_qkv), 3)
@@ -59,18 +100,19 @@ class DiTBlock(torch.nn.Module):
         return x + rola.FfnFunction.apply(self._norm(2, x), self.W_gate, self.W_up, self.W_down, self.act)
 
 
-def train(steps: int = 5, lr: float = 0.2, seed: int = 0):
+def train(steps: int = 5, lr: float = 0.2, seed: int = 0, conditioned: bool = False):
     """Losses of `steps` plain gradient steps towards a fixed random target on the tiny layer."""
     from . import configs
     torch.manual_seed(seed)
     cfg = configs.get("tiny")
-    block = DiTBlock(cfg, d_text=192, d_ff=704)
+    block = DiTBlock(cfg, d_text=192, d_ff=704, d_cond=256 if conditioned else None)
     made = dict(dtype=torch.bfloat16, device="cuda")
     x, target = (torch.randn(1, cfg["N"], cfg["H"] * 128, **made) for _ in range(2))
     text, text_len = torch.randn(1, 77, 192, **made), torch.tensor([40], dtype=torch.int32, device="cuda")
+    cond = torch.randn(1, 256, **made) if conditioned else None
     losses = []
     for _ in range(steps):
-        loss = (block(x, text, text_len).float() - target.float()).square().mean()
+        loss = (block(x, text, text_len, cond).float() - target.float()).square().mean()
         block.zero_grad(set_to_none=True)
         loss.backward()
         with torch.no_grad():
@@ -81,5 +123,5 @@ def train(steps: int = 5, lr: float = 0.2, seed: int = 0):
 
 
 if __name__ == "__main__":
-    for i, value in enumerate(train()):
+    for i, value in enumerate(train(conditioned="--conditioned" in sys.argv[1:])):
         print(f"step {i}: loss {value:.4f}")
