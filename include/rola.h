@@ -563,7 +563,7 @@ typedef struct {
     int32_t act;               /* phi, one of rola_lowrank_act_t; default ROLA_LOWRANK_ACT_IDENTITY */
     rola_dtype_t dtype;        /* ROLA_BF16 (default) or ROLA_FP32 */
     int32_t wait_limit_ms;     /* bound of every device-side wait (0 = 2000 ms); at most 60000 */
-    int32_t debug_flags;       /* as rola_ffn_config_t */
+    int32_t debug_flags;       /* as rola_ffn_config_t (small layers of up to four tokens wait for nothing) */
 } rola_linear_config_t;
 
 /* Fill *cfg with defaults (sizes zero).  Returns ROLA_ERR_INVALID_ARG on NULL. */

@@ -550,14 +550,13 @@ def residual_norm_backward_workspace(c: RolaResidualNormConfig, device="cuda") -
     return _bytes(_lib.rola_residual_norm_backward_workspace_bytes(c), "rola_residual_norm_backward_workspace_bytes", device)
 
 
-def _mod(t, c, dt, where: str, name: str, dev: int):
-    """The address of a vector of each sample [groups][d], whose samples are c.mod_stride (0: d) elements apart."""
+def _mod(t, shape, apart: int, dt, where: str, name: str, dev: int):
+    """The address of a vector of each sample, of shape (groups, d), whose samples are `apart` elements from each other."""
     if t is None:
         return None
-    apart = c.mod_stride or c.d
-    if (t.dtype is not dt or t.shape != (c.groups, c.d) or (c.d > 1 and t.stride(1) != 1) or t.get_device() != dev
-            or (c.groups > 1 and t.stride(0) != apart)):
-        raise ValueError(f"{where}: {name} must be a tensor on GPU {dev}, {dt} of shape {(c.groups, c.d)} with strides "
+    if t.dtype is not dt or t.shape != shape or t.get_device() != dev or (
+            t.stride() != (apart, 1) and ((shape[0] > 1 and t.stride(0) != apart) or (shape[1] > 1 and t.stride(1) != 1))):
+        raise ValueError(f"{where}: {name} must be a tensor on GPU {dev}, {dt} of shape {shape} with strides "
                          f"{(apart, 1)}, not {t.dtype} {tuple(t.shape)} with {t.stride()} on {t.device}")
     return t.data_ptr()
 
@@ -568,11 +567,12 @@ def residual_norm(c, x, h, out, y, *, gate=None, gamma_h=None, gamma=None, beta=
     x, h, out, y [groups][rows][d]; gate, scale, shift [groups][d] with c.mod_stride between the samples; gamma_h, gamma,
     beta [d]; every vector may be None.  h and out None: the norm of x; y None: no norm.  stats (fp32
     [groups][rows][4]), if given, receives what residual_norm_backward reads."""
-    w, dt, shape, d = "rola_residual_norm", _TORCH_DTYPES.get(c.dtype), (c.groups, c.rows, c.d), (c.d,)
+    w, dt, B, n, width = "rola_residual_norm", _TORCH_DTYPES.get(c.dtype), c.groups, c.rows, c.d
+    shape, per, d, apart = (B, n, width), (B, width), (width,), c.mod_stride or width
     dev = _gpu(x, w, "x")
     _run(_lib.rola_residual_norm, w, dev, stream, c, _a(x, dt, shape, w, "x", dev), _a(h, dt, shape, w, "h", dev),
-         _mod(gate, c, dt, w, "gate", dev), _a(gamma_h, dt, d, w, "gamma_h", dev), _a(gamma, dt, d, w, "gamma", dev),
-         _a(beta, dt, d, w, "beta", dev), _mod(scale, c, dt, w, "scale", dev), _mod(shift, c, dt, w, "shift", dev),
+         _mod(gate, per, apart, dt, w, "gate", dev), _a(gamma_h, dt, d, w, "gamma_h", dev), _a(gamma, dt, d, w, "gamma", dev),
+         _a(beta, dt, d, w, "beta", dev), _mod(scale, per, apart, dt, w, "scale", dev), _mod(shift, per, apart, dt, w, "shift", dev),
          _a(out, dt, shape, w, "out", dev), _a(y, dt, shape, w, "y", dev),
          _a(stats, _F32, shape[:2] + (4,), w, "stats", dev))
 
@@ -582,11 +582,12 @@ def residual_norm_backward(c, x, h, stats, dout, dy, dx, dh, ws, *, gate=None, g
                            stream=None):
     """dx, dh of residual_norm from the gradients dout and dy of its results (None: 0 / no y), and those of its vectors
     (fp32, dense, in the vectors' shapes; None: not wanted)."""
-    w, dt, shape, d = "rola_residual_norm_backward", _TORCH_DTYPES.get(c.dtype), (c.groups, c.rows, c.d), (c.d,)
-    dev, per = _gpu(x, w, "x"), (c.groups, c.d)
+    w, dt, B, n, width = "rola_residual_norm_backward", _TORCH_DTYPES.get(c.dtype), c.groups, c.rows, c.d
+    shape, per, d, apart = (B, n, width), (B, width), (width,), c.mod_stride or width
+    dev = _gpu(x, w, "x")
     _run(_lib.rola_residual_norm_backward, w, dev, stream, c, _a(x, dt, shape, w, "x", dev), _a(h, dt, shape, w, "h", dev),
-         _mod(gate, c, dt, w, "gate", dev), _a(gamma_h, dt, d, w, "gamma_h", dev), _a(gamma, dt, d, w, "gamma", dev),
-         _a(beta, dt, d, w, "beta", dev), _mod(scale, c, dt, w, "scale", dev),
+         _mod(gate, per, apart, dt, w, "gate", dev), _a(gamma_h, dt, d, w, "gamma_h", dev), _a(gamma, dt, d, w, "gamma", dev),
+         _a(beta, dt, d, w, "beta", dev), _mod(scale, per, apart, dt, w, "scale", dev),
          _a(stats, _F32, shape[:2] + (4,), w, "stats", dev), _a(dout, dt, shape, w, "dout", dev),
          _a(dy, dt, shape, w, "dy", dev), _a(dx, dt, shape, w, "dx", dev), _a(dh, dt, shape, w, "dh", dev),
          _a(dgate, _F32, per, w, "dgate", dev), _a(dgamma_h, _F32, d, w, "dgamma_h", dev),
