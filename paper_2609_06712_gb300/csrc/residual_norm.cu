@@ -595,7 +595,7 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
     const int group = WARP ? threadIdx.x >> 5 : 0, part = WARP ? blockIdx.x * kWarpGroups + group : blockIdx.x;
     if (part >= a.parts) return;                         // a whole warp: no barrier of the CTA follows
     Feed<T, V, EL, 2, FULL> q;
-    q.tpr = WARP ? 32 : blockDim.x;
+    q.tpr = WARP ? 32 : kWide<T, V> ? (int)blockDim.x : TH;     // (small pieces: addresses are then known to the compiler)
     q.gt = WARP ? threadIdx.x & 31 : threadIdx.x;
     q.depth = depth;
     q.end = rn_row(sh.total, a.parts, part + 1);
@@ -664,7 +664,7 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
     if (part >= a.parts) return;
     const bool normed = sh.norm != ROLA_NORM_NONE;
     Feed<T, V, EL, 4, FULL> q;
-    q.tpr = WARP ? 32 : blockDim.x;
+    q.tpr = WARP ? 32 : kWide<T, V> ? (int)blockDim.x : TH;     // (small pieces: addresses are then known to the compiler)
     q.gt = WARP ? threadIdx.x & 31 : threadIdx.x;
     q.depth = depth;
     q.end = rn_row(sh.total, a.parts, part + 1);
@@ -957,13 +957,13 @@ struct Launch {
     size_t smem;
 };
 template <typename K>
-cudaError_t shape_of(K kernel, const RnShape& s, bool warp, int el, int registers, size_t row_bytes, long long most, Launch* l)
+cudaError_t shape_of(K kernel, const RnShape& s, bool warp, int el, int fixed, int registers, size_t row_bytes, long long most, Launch* l)
 {
     int nsm = 0;
     cudaError_t e = sm_count(&nsm);
     if (e != cudaSuccess) return e;
     const int groups = warp ? kWarpGroups : 1;
-    l->threads = warp ? 32 * kWarpGroups : ((s.d + el - 1) / el + 31) / 32 * 32;
+    l->threads = warp ? 32 * kWarpGroups : fixed ? fixed : ((s.d + el - 1) / el + 31) / 32 * 32;
     int ctas = 512 / registers * 4 / (l->threads / 32);
     ctas = ctas < 1 ? 1 : ctas > 8 ? 8 : ctas;
     while (ctas > 1 && groups * row_bytes * 2 * ctas > kRingBytes) --ctas;       // two rows a group at least, if they fit
@@ -992,7 +992,7 @@ cudaError_t fwd_one(const RnShape& s, RnArgs& a, cudaStream_t st)
     Launch l;
     auto kernel = rn_fwd_kernel<T, V, EL, WARP, FULL, TH, MIN>;
     const size_t row = (size_t)place_bytes(s.d, sizeof(T), kWide<T, V>) * (a.h ? 2 : 1);
-    cudaError_t e = shape_of(kernel, s, WARP, EL, registers_of(TH, MIN), row, 1ll << 30, &l);
+    cudaError_t e = shape_of(kernel, s, WARP, EL, kWide<T, V> ? 0 : TH, registers_of(TH, MIN), row, 1ll << 30, &l);
     if (e != cudaSuccess) return e;
     a.in[0] = a.x;
     a.in[1] = a.h;
@@ -1009,7 +1009,7 @@ cudaError_t bwd_one(const RnShape& s, RnArgs& a, cudaStream_t st)
     auto kernel = rn_bwd_kernel<T, V, EL, WARP, FULL, TH, MIN>;
     const int matrices = (s.norm != ROLA_NORM_NONE ? 1 : 0) + (a.h ? 1 : 0) + (a.dy ? 1 : 0) + (a.dout ? 1 : 0);
     const size_t row = (size_t)place_bytes(s.d, sizeof(T), kWide<T, V>) * matrices;
-    cudaError_t e = shape_of(kernel, s, WARP, EL, registers_of(TH, MIN), row, rn_parts(s), &l);
+    cudaError_t e = shape_of(kernel, s, WARP, EL, kWide<T, V> ? 0 : TH, registers_of(TH, MIN), row, rn_parts(s), &l);
     if (e != cudaSuccess) return e;
     a.in[0] = s.norm != ROLA_NORM_NONE ? a.x : nullptr;
     a.in[1] = a.h;
@@ -1028,13 +1028,19 @@ cudaError_t fwd(const RnShape& s, RnArgs& a, cudaStream_t st)
 {
     if (s.d <= 256) return fwd_one<T, V, 8, true, 128, 6>(s, a, st);
     if (s.d <= 512) return fwd_one<T, V, 16, true, 128, 4>(s, a, st);
-    // Single elements take more instructions a row, and more warps hide them (32760 x 1537: ... us with 16 a thread).  Where an
-    // SM has a few rows only, it is one row's time that counts.
-    if (V == 1 || s.total <= kFewRows)
-        if (s.d <= 8 * 256) return fwd_one<T, V, 8, false, 256, 3>(s, a, st);
-    constexpr int kFewer = !kWide<T, V>;             // CTAs: addresses of small pieces take more registers
-    if (s.d <= 16 * 160) return fwd_one<T, V, 16, false, 160, 3 - kFewer>(s, a, st);
-    if (s.d <= 16 * 320) return fwd_one<T, V, 16, false, 320, 2 - kFewer>(s, a, st);
+    // where an SM has a few rows only, it is one row's time that counts
+    if (s.total <= kFewRows && s.d <= 8 * 256) return fwd_one<T, V, 8, false, 256, 3>(s, a, st);
+    if constexpr (!kWide<T, V>) {
+        // CTAs of a fixed size: 32760 x 1537 156 us, with the least number of warps 276
+        if (s.d <= 16 * 64) return fwd_one<T, V, 16, false, 64, 6>(s, a, st);
+        if (s.d <= 16 * 128) return fwd_one<T, V, 16, false, 128, 3>(s, a, st);
+        if (s.d <= 16 * 160) return fwd_one<T, V, 16, false, 160, 2>(s, a, st);
+        if (s.d <= 16 * 224) return fwd_one<T, V, 16, false, 224, 1>(s, a, st);
+        if (s.d <= 16 * 320) return fwd_one<T, V, 16, false, 320, 1>(s, a, st);
+    } else {
+        if (s.d <= 16 * 160) return fwd_one<T, V, 16, false, 160, 3>(s, a, st);
+        if (s.d <= 16 * 320) return fwd_one<T, V, 16, false, 320, 2>(s, a, st);
+    }
     if (s.d <= 16 * 512) return fwd_one<T, V, 16, false, 512, 1>(s, a, st);
     if constexpr (kWide<T, V>)
         if (s.d <= kFwdRegisters) return fwd_one<T, V, 32, false, 512, 1>(s, a, st);
@@ -1048,6 +1054,12 @@ cudaError_t bwd(const RnShape& s, RnArgs& a, cudaStream_t st)
     if (s.d <= 256) return bwd_one<T, V, 8, true, 128, 4>(s, a, st);
     if (s.d <= 512) return bwd_one<T, V, 16, true, 128, 2>(s, a, st);
     if (s.total <= kFewRows && s.d <= 8 * 256) return bwd_one<T, V, 8, false, 256, 2>(s, a, st);
+    if constexpr (!kWide<T, V>) {
+        if (s.d <= 16 * 64) return bwd_one<T, V, 16, false, 64, 6>(s, a, st);
+        if (s.d <= 16 * 128) return bwd_one<T, V, 16, false, 128, 3>(s, a, st);
+        if (s.d <= 16 * 160) return bwd_one<T, V, 16, false, 160, 2>(s, a, st);
+        if (s.d <= 16 * 224) return bwd_one<T, V, 16, false, 224, 1>(s, a, st);
+    }
     if (s.d <= 16 * 320) return bwd_one<T, V, 16, false, 320, 1>(s, a, st);
     if (s.d <= kBwdRegisters) return bwd_one<T, V, 16, false, 512, 1>(s, a, st);
     a.parts = rn_parts(s);
