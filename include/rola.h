@@ -599,7 +599,7 @@ rola_status_t rola_linear_train(const rola_linear_config_t* cfg, const void* X, 
  * summed in fp32 before that rounding.
  *   X, W, Z : as rola_linear_train read and wrote them (Z NULL with the identity);  dY : [tokens][d_out]
  *   dX : out, [tokens][d_in];  dW : out, [d_out][d_in], both cfg->dtype;  db : out, fp32 [d_out].  Each may be
- *        NULL (not wanted), not all three
+ *        NULL (not wanted), not all three; they overlap no other argument and not each other
  */
 rola_status_t rola_linear_backward(const rola_linear_config_t* cfg, const void* X, const void* W, const float* Z,
                                    const void* dY, void* dX, void* dW, float* db, void* ws, size_t ws_bytes,

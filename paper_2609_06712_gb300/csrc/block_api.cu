@@ -164,12 +164,20 @@ LinWorkspace linear_layout(const rola_linear_config_t& c, bool backward)
     return w;
 }
 
+// Whether the output p starts where one of the others does.  (A CTA would read there what another has written.)
+template <typename... Q>
+bool same_start(const void* p, Q... others)
+{
+    return p && ((p == static_cast<const void*>(others)) || ...);
+}
+
 rola_status_t linear_forward(const rola_linear_config_t* cfg, const void* X, const void* W, const void* b, const void* R,
                              void* Y, float* Z, void* ws, size_t ws_bytes, void* stream)
 {
     if (!X || !W || !Y || !aligned(16, X, W, b, R, Y, Z)) return ROLA_ERR_INVALID_ARG;
     const LinWorkspace w = linear_layout(*cfg, false);
     ROLA_CHECK(check_ws(ws, ws_bytes, w.total));
+    if (same_start(Y, X, W, b, Z, ws) || same_start(Z, X, W, b, R, ws)) return ROLA_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     DeviceStatus* status = at<DeviceStatus>(ws, w.status);
     const LinShape s = make_shape(*cfg);
@@ -519,6 +527,8 @@ rola_status_t rola_linear_backward(const rola_linear_config_t* cfg, const void* 
     if (!aligned(16, X, W, Z, dY, dX, dW, db)) return ROLA_ERR_INVALID_ARG;
     const LinWorkspace w = linear_layout(*cfg, true);
     ROLA_CHECK(check_ws(ws, ws_bytes, w.total));
+    if (same_start(dX, X, W, Z, dY, dW, db, ws) || same_start(dW, X, W, Z, dY, db, ws) || same_start(db, X, W, Z, dY, ws))
+        return ROLA_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const LinShape s = make_shape(*cfg);
     DeviceStatus* status = at<DeviceStatus>(ws, w.status);

@@ -68,3 +68,17 @@ def test_null_and_misaligned_pointers(rl, name, n, nullable):
     assert getattr(lib, name)(ctypes.byref(c), *[p] * n, 255, None) == rl.ROLA_ERR_WORKSPACE
     if name == "rola_linear_backward":
         assert lib.rola_linear_backward(ctypes.byref(c), p, p, p, p, None, None, None, p, 1 << 40, None) == rl.ROLA_ERR_INVALID_ARG
+
+
+def test_outputs_that_start_where_another_tensor_does(rl):
+    """Y may be the residual; every other output in the place of an argument would be read after it is written."""
+    lib, c = rl.library(), rl.make_linear_config(64, 64, 64, "silu")
+    p = [1 << 20 + i for i in range(8)]
+    for name, n, outs, may in (("rola_linear", 6, (4,), {(4, 3)}), ("rola_linear_train", 7, (4, 5), {(4, 3)}),
+                               ("rola_linear_backward", 8, (4, 5, 6), set())):
+        for i in outs:
+            for j in range(n):
+                if i == j or (i, j) in may or (j, i) in may:
+                    continue
+                q = [ctypes.c_void_p(p[j if k == i else k]) for k in range(n)]
+                assert getattr(lib, name)(ctypes.byref(c), *q, 1 << 40, None) == rl.ROLA_ERR_INVALID_ARG, (name, i, j)
