@@ -756,6 +756,7 @@ class LinearFunction(torch.autograd.Function):
         r = None if residual is None else residual.contiguous().view(-1, residual.shape[-1])
         linear_train(c, x, W, None if b is None else b.contiguous(), r, Y, Z, linear_workspace(c, x.device))
         ctx.c, ctx.bias_dtype = c, None if b is None else b.dtype
+        ctx.residual_shape = None if residual is None else residual.shape
         ctx.save_for_backward(x, W, Z)
         return Y.view(*X.shape[:-1], c.d_out)
 
@@ -771,7 +772,7 @@ class LinearFunction(torch.autograd.Function):
             linear_backward(c, x, W, Z, dY.contiguous().view(c.tokens, c.d_out), dX, dW, db,
                             linear_backward_workspace(c, x.device))
         return (None if dX is None else dX.view(*dY.shape[:-1], c.d_in), dW, None if db is None else db.to(ctx.bias_dtype),
-                dY if need[3] else None, None)
+                dY.reshape(ctx.residual_shape) if need[3] else None, None)
 
 
 class ResidualNormFunction(torch.autograd.Function):

@@ -268,6 +268,13 @@ def test_autograd_of_some_inputs(rl):
         assert (leaves[i].grad.double() - ref[i].grad).norm() <= 1e-5 * ref[i].grad.norm()
 
 
+def test_a_residual_of_another_shape_gets_its_gradient_in_it(rl):
+    case = Case(rl, 24, 64, 128, "silu", torch.float32)
+    X, R = case.X.view(2, 12, 64), case.R.clone().requires_grad_()
+    rl.LinearFunction.apply(X, case.W, case.b, R, "silu").backward(case.dY.view(2, 12, 128))
+    assert torch.equal(R.grad, case.dY)
+
+
 def test_refusals(rl):
     case = Case(rl, 4, 64, 128, "silu", torch.bfloat16)
     c, X, W, b, R = case.c, case.X, case.W, case.b, case.R
