@@ -36,6 +36,8 @@ class DiTBlock(torch.nn.Module):
     """One block over the token grid of a layer config (configs.py); d_model = H * 128 + the text's width d_text;
     d_cond, if given, is the width of the conditioning vector of each sample."""
 
+    d_cond = None                                    # width of the conditioning vector, of a conditioned block
+
     def __init__(self, cfg: dict, d_text: int, d_ff: int, act: str = "silu", dtype=torch.bfloat16, device="cuda",
                  d_cond: int | None = None):
         super().__init__()
@@ -52,6 +54,7 @@ class DiTBlock(torch.nn.Module):
         self.norms = torch.nn.ParameterList(torch.nn.Parameter(t) for _ in range(3)
                                             for t in (torch.ones(d, **made), torch.zeros(d, **made)))
         if d_cond is not None:
+            self.d_cond = d_cond
             self.W_mod, self.b_mod = weight(6 * d, d_cond), torch.nn.Parameter(torch.zeros(6 * d, **made))
 
     def _norm(self, i, x):
@@ -67,6 +70,9 @@ class DiTBlock(torch.nn.Module):
     def forward(self, x, text, text_len=None, cond=None):
         """x [B][N][d_model], text [B][L][d_text], text_len int32 [B] (None: the whole text), cond [B][d_cond] of a
         conditioned block."""
+        if (cond is None) != (self.d_cond is None) or cond is not None and cond.shape != (x.shape[0], self.d_cond):
+            raise ValueError(f"DiTBlock: cond must be {'None' if self.d_cond is None else f'[B][{self.d_cond}]'}, not "
+                             f"{None if cond is None else tuple(cond.shape)}")
         with torch.cuda.device(x.device):            # the module launches on the current device
             if cond is not None:
                 return self._conditioned(x, text, text_len, cond)
