@@ -19,8 +19,8 @@
 // in a slot of its own, and a second kernel, launched ahead, adds the slots in a fixed order.  All statistics and sums
 // are fp32.  Rows too long for registers, or of a length that no form takes, go through memory in several passes.
 //
-// Measured, bf16, with gate, scale and shift: 75600 x 5120 forward 490 us (6.3 TB/s, 93 % of a copy), backward 750 us (6.2);
-// 2 x 16380 x 1536 forward 74, backward 112 us (5.4, 5.4; the ramp and the tail count); with a norm behind the branch too,
+// Measured, bf16, with gate, scale and shift: 75600 x 5120 forward 514 us (6.0 TB/s, 89 % of a copy), backward 750 us (6.2);
+// 2 x 16380 x 1536 forward 76, backward 112 us (5.3, 5.4; the ramp and the tail count); with a norm behind the branch too,
 // 3 x 4095 x 2560 46 and 83 us.  Backward, rows of 5121 to 8192 elements spill 270 bytes a thread (20000 x 8192: 3.8 TB/s).
 //
 // The variance is taken about the rounded mean, as in the layer norm.
@@ -928,7 +928,7 @@ bool wants_sums(const RnArgs& a) { return a.dgate || a.dgamma_h || a.dgamma || a
 constexpr int kMostParts = 4864, kMostCtas = 1216;       // of warps, of CTAs: 32 and 8 on each of 152 SMs
 constexpr int kFwdRegisters = 16384, kBwdRegisters = 8192;       // longest rows held in registers (forward, single elements: 8192)
 
-constexpr int kFewRows = 1216;                           // 8 for each of 152 SMs
+constexpr int kFewRows = 456, kFewRowsBwd = 1216;        // 3 and 8 for each of 152 SMs
 
 // Whether every row and every vector starts at a multiple of `to` bytes.
 bool starts_at(int to, const RnShape& s, const RnArgs& a, int esz)
@@ -1028,10 +1028,11 @@ cudaError_t fwd(const RnShape& s, RnArgs& a, cudaStream_t st)
 {
     if (s.d <= 256) return fwd_one<T, V, 8, true, 128, 6>(s, a, st);
     if (s.d <= 512) return fwd_one<T, V, 16, true, 128, 4>(s, a, st);
-    // where an SM has a few rows only, it is one row's time that counts
-    if (s.total <= kFewRows && s.d <= 8 * 256) return fwd_one<T, V, 8, false, 256, 3>(s, a, st);
     if constexpr (!kWide<T, V>) {
-        // CTAs of a fixed size: 32760 x 1537 156 us, with the least number of warps 276
+        // Where an SM has a few rows only, it is one row's time that counts: 300 x 777 5.8 us, 8.8 with 16 elements a thread
+        // (600 rows 8.8 and 9.1, in fp32 7.9 and 6.8; rows of 16-byte pieces gain nothing: 600 x 2048 5.7 and 4.5)
+        if (s.total <= kFewRows && s.d <= 8 * 256) return fwd_one<T, V, 8, false, 256, 3>(s, a, st);
+        // CTAs of a fixed size: 32760 x 1537 153 us, with the least number of warps 276
         if (s.d <= 16 * 64) return fwd_one<T, V, 16, false, 64, 6>(s, a, st);
         if (s.d <= 16 * 128) return fwd_one<T, V, 16, false, 128, 3>(s, a, st);
         if (s.d <= 16 * 160) return fwd_one<T, V, 16, false, 160, 2>(s, a, st);
@@ -1053,7 +1054,8 @@ cudaError_t bwd(const RnShape& s, RnArgs& a, cudaStream_t st)
 {
     if (s.d <= 256) return bwd_one<T, V, 8, true, 128, 4>(s, a, st);
     if (s.d <= 512) return bwd_one<T, V, 16, true, 128, 2>(s, a, st);
-    if (s.total <= kFewRows && s.d <= 8 * 256) return bwd_one<T, V, 8, false, 256, 2>(s, a, st);
+    // the same: 300 x 777 12.2 us, 14.7 with 16 elements a thread; 1200 x 1536 14.6 and 15.6 (600 and fewer alike)
+    if (s.total <= kFewRowsBwd && s.d <= 8 * 256) return bwd_one<T, V, 8, false, 256, 2>(s, a, st);
     if constexpr (!kWide<T, V>) {
         if (s.d <= 16 * 64) return bwd_one<T, V, 16, false, 64, 6>(s, a, st);
         if (s.d <= 16 * 128) return bwd_one<T, V, 16, false, 128, 3>(s, a, st);

@@ -178,6 +178,22 @@ def test_vectors_that_are_slices_of_a_modulation(rl, d, apart, dname):
 
 
 @pytest.mark.parametrize("dname", sorted(DTYPES))
+@pytest.mark.parametrize("d", [777, 1286, 1537, 2059, 3583, 5119, 8191])
+def test_many_rows_of_small_pieces(rl, d, dname):
+    """Widths of no 16-byte pieces, one for each number of threads, over several turns of the ring."""
+    case = Case(rl, 5, 521 if d < 4000 else 131, d, "layer", "rms", ALL, DTYPES[dname], seed=d)
+    case.check(case.run())
+
+
+@pytest.mark.parametrize("dname", sorted(DTYPES))
+@pytest.mark.parametrize("d", [777, 1536])
+@pytest.mark.parametrize("rows", [456, 457, 1216, 1217])
+def test_where_few_rows_end(rl, rows, d, dname):
+    case = Case(rl, 1, rows, d, "rms", "layer", ALL, DTYPES[dname], seed=rows)
+    case.check(case.run())
+
+
+@pytest.mark.parametrize("dname", sorted(DTYPES))
 def test_many_rows_per_cta(rl, dname):
     """Samples that begin and end within a CTA's rows, over several turns of its ring."""
     for B, n, d in ((3, 4001, 264), (1, 9001, 1536), (700, 13, 520), (2, 3000, 5120)):
