@@ -5,7 +5,7 @@
 // lane sums its columns in registers, the warps meet in shared memory in warp order, the parts in a second kernel in
 // part order: the same bits every time.  The sums are of dZ in fp32, before it is rounded.
 //
-// Measured: GELU at 8190 x 6144 66 us (402 MB, 6.1 TB/s; with erfcf and expf 143 us), the sums of 32760 x 1536 alone 16 us.
+// Measured: GELU at 8190 x 6144 69 us (402 MB, 5.8 TB/s; with erfcf and expf 143 us), the sums of 32760 x 1536 alone 16 us.
 #include "linear.cuh"
 #include "linear_finish.cuh"
 

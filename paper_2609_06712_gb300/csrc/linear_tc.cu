@@ -21,9 +21,9 @@
 // Few tiles with a long K axis (the weights' gradients: K is the token) are split along K; the parts go to the
 // workspace in fp32, and a second kernel adds them in order and finishes the outputs (launch_linear_join).
 //
-// Measured, bf16: 16380 x 5120 x 5120 with a residual 472 us (1820 TFLOP/s, 89 % of the tensor pipe), 32760 x 1536 x 4608 260 us
+// Measured, bf16: 16380 x 5120 x 5120 with a residual 473 us (1815 TFLOP/s, 89 % of the tensor pipe), 32760 x 1536 x 4608 260 us
 // (1780), 8190 x 1536 x 6144 with GELU 106 us (1465), 514 x 4096 x 5120 with GELU 27 us.  What a large one lacks is the last
-// turn of tiles; what a small one lacks are its ends (8 us) and pairs without a tile.
+// turn of tiles; what a small one lacks are its ends (some 5 us) and pairs without a tile.
 //
 // Every mbarrier wait is bounded; a wait that gives up records ROLA_ERR_TIMEOUT in the status word, and the CTA stops
 // issuing, lets what it issued complete, meets its pair and frees its TMEM.
