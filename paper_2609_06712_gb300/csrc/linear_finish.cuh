@@ -25,6 +25,8 @@ inline LinearEnd linear_end_of(void* c, const void* bias, const void* residual, 
 
 // GELU of bf16 layers, two values at a time.  With u = |z|, x = u / sqrt 2 and erfcx(x) = e^(x^2) erfc(x):
 //   tail = Phi(-u) = erfcx(x) e^(-z^2 / 2) / 2,  gelu(z) = max(z, 0) - u tail,  gelu'(z) = Phi(z) + z e^(-z^2 / 2) / sqrt(2 pi)
+// u is held at 16, past which the tail underflows.  max(z, 0) is z / 2 + |z / 2| (exact but in odd subnormals), so that
+// z = -inf gives NaN in every form of the layer, as the definition z Phi(z) = -inf * 0 does (and gelu' at both infinities).
 // erfcx is t P(t), t = 1 / (1 + 0.44 x): P of degree 7 fitted here to the least relative error over 0 <= x <= 10 (2e-7, with
 // fp32's roundings 5e-7), beyond which the tail is 0 beside any z.  One exponential serves both; its argument's rounding adds
 // 2^-23 z^2 relative to the tail.  About 11 instructions a value, where erfcf takes some 45: of the feed-forward's
@@ -71,10 +73,12 @@ struct FastGelu {
     static __device__ __forceinline__ void phi(float (&z)[2])
     {
         float u[2], tail[2], e[2], top[2];
+        const float half[2] = {0.5f, 0.5f};
         parts(z, u, tail, e);
+        fma2(top, z, half, 0.0f);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            top[i] = z[i] <= 0.0f ? 0.0f : z[i];         // (fmaxf would make a NaN 0)
+            top[i] += fabsf(top[i]);
             u[i] = -u[i];
         }
         fma2(z, u, tail, top);
