@@ -743,11 +743,14 @@ class AttentionFunction(torch.autograd.Function):
 
 class LinearFunction(torch.autograd.Function):
     """A linear layer with its epilogue as a differentiable torch op: ``apply(X, W, b, residual, act)``;
-    X [..., d_in], residual [..., d_out]; b and residual may be None."""
+    X [..., d_in], residual [..., d_out] or [tokens, d_out]; b and residual may be None."""
 
     @staticmethod
     def forward(ctx, X, W, b, residual, act):
         x, W = X.contiguous().view(-1, X.shape[-1]), W.contiguous()
+        shapes = (*X.shape[:-1], W.shape[0]), (x.shape[0], W.shape[0])
+        if residual is not None and residual.shape not in shapes:    # another order of the tokens has as many elements
+            raise ValueError(f"rola_linear: residual must be {shapes[0]} or {shapes[1]}, not {tuple(residual.shape)}")
         c = make_linear_config(x.shape[0], x.shape[1], W.shape[0], act, _dtype_of(x, "rola_linear"))
         Y = torch.empty((c.tokens, c.d_out), dtype=x.dtype, device=x.device)
         Z = None
