@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(128) rn_columns_kernel(const RnShape sh, const
         E = fmaf(e.t, e.hh, E);
         if (r + 1 == r1 || (r + 1) % sh.rows == 0) {
             const int dp = rn_padded(sh.d);
-            float* out = a.part + (size_t)(part + s) * 3 * dp + c;
+            float* out = a.part + rn_slot(part, s, sh.d) + c;
             out[0] = A;
             out[dp] = B;
             out[2 * (size_t)dp] = E;
@@ -790,7 +790,7 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
         }
         if (a.part) {
             const int dp = rn_padded(sh.d);
-            float* out = a.part + (size_t)(part + s) * 3 * dp;
+            float* out = a.part + rn_slot(part, s, sh.d);
 #pragma unroll
             for (int i = 0; i < EL / V; ++i) {
                 const int p = (q.gt + i * q.tpr) * V;
@@ -838,18 +838,18 @@ __global__ void __launch_bounds__(32 * kReduceWarps) rn_reduce_kernel(const __gr
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, quad = lane & 7;
     const int c = blockIdx.x * 32 + quad * 4, dp = rn_padded(sh.d), at_once = kReduceWarps / ways, way = w % ways;
     const bool branch = blockIdx.y + (a.norm_sums ? 0 : 1) == 1;
-    const int s_begin = (int)((long long)sh.groups * blockIdx.z / gridDim.z);
-    const int s_end = (int)((long long)sh.groups * (blockIdx.z + 1) / gridDim.z);
+    const uint32_t s_begin = (uint32_t)((long long)sh.groups * blockIdx.z / gridDim.z);
+    const uint32_t s_end = (uint32_t)((long long)sh.groups * (blockIdx.z + 1) / gridDim.z);
     float4 total[2] = {};                                // over the samples: of (1 + scale) A and (1 + scale) B, or of gate E
-    for (int s0 = s_begin; s0 < s_end; s0 += at_once) {
-        const int s = s0 + w / ways;
+    for (uint32_t s0 = s_begin; s0 < s_end; s0 += at_once) {     // (unsigned: s may pass s_end, and with it 31 bits)
+        const uint32_t s = s0 + w / ways;
         float4 x[2] = {};
         if (s < s_end && c < sh.d) {
             const int lo = rn_part(sh.total, a.parts, (long long)s * sh.rows);
             const int hi = rn_part(sh.total, a.parts, (long long)(s + 1) * sh.rows - 1);
 #pragma unroll 4
             for (int i = lo + way * 4 + (lane >> 3); i <= hi; i += ways * 4) {
-                const float* p = a.part + (size_t)(i + s) * 3 * dp + c;
+                const float* p = a.part + rn_slot(i, s, sh.d) + c;
                 x[0] = x[0] + *reinterpret_cast<const float4*>(p + (branch ? 2 * dp : 0));
                 if (!branch) x[1] = x[1] + *reinterpret_cast<const float4*>(p + dp);
             }
@@ -1091,7 +1091,7 @@ cudaError_t backward(const RnShape& s, RnArgs& a, cudaStream_t st)
     a.norm_sums = a.dgamma || a.dbeta || a.dscale || a.dshift;
     const bool branch_sums = a.dgate || a.dgamma_h, shared = a.dgamma || a.dbeta || a.dgamma_h;
     int ways = kReduceWarps;
-    while (ways > 1 && ways * s.groups > kReduceWarps) ways /= 2;
+    while (ways > 1 && (int64_t)ways * s.groups > kReduceWarps) ways /= 2;
     const int z = rn_shares(s), columns = (s.d + 31) / 32;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(columns, a.norm_sums && branch_sums ? 2 : 1, z);
@@ -1119,8 +1119,8 @@ int rn_parts(const RnShape& s)
 int rn_shares(const RnShape& s)
 {
     // 32 samples a share at least, and some 4000 CTAs at most
-    const int columns = (s.d + 31) / 32, most = (4096 + columns - 1) / columns, want = (s.groups + 31) / 32;
-    return want < most ? want : most;
+    const int64_t columns = (s.d + 31) / 32, most = (4096 + columns - 1) / columns, want = ((int64_t)s.groups + 31) / 32;
+    return (int)(want < most ? want : most);
 }
 
 bool rn_long(const RnShape& s) { return s.d > kBwdRegisters; }

@@ -36,6 +36,11 @@ __host__ __device__ __forceinline__ int rn_part(long long total, int parts, long
 }
 
 __host__ __device__ __forceinline__ int rn_padded(int d) { return (d + 3) / 4 * 4; }
+// Where a slot's sums start, in floats.  (Part and sample together may pass 31 bits, not 32.)
+__host__ __device__ __forceinline__ size_t rn_slot(uint32_t part, uint32_t s, int d)
+{
+    return (size_t)(part + s) * 3 * rn_padded(d);
+}
 
 int rn_shares(const RnShape& s);                     // shares of the samples in the sums over them
 int rn_parts(const RnShape& s);                      // most parts of the backward, for the workspace
