@@ -621,6 +621,8 @@ typedef struct {
                                   (default) or at least d; 0 is d.  They may be slices of one modulation [groups][6 d] */
     float eps;                 /* of both norms, >= 0; default 1e-6 */
     rola_dtype_t dtype;        /* ROLA_BF16 (default) or ROLA_FP32 */
+    int32_t wait_limit_ms;     /* bound of every device-side wait (0 = 2000 ms); at most 60000 */
+    int32_t debug_flags;       /* as rola_ffn_config_t (rows of over 16384 elements, backward 8192, wait for nothing) */
 } rola_residual_norm_config_t;
 
 /* Fill *cfg with defaults (sizes zero).  Returns ROLA_ERR_INVALID_ARG on NULL. */
@@ -643,6 +645,9 @@ rola_status_t rola_residual_norm_config_init(rola_residual_norm_config_t* cfg);
  *           (0 where there is no such norm), what the backward pass reads
  * Tensors need their element's alignment only (with d and mod_stride multiples of 16 bytes and 16-byte aligned
  * pointers the wide path runs).
+ * The call has no status word.  A row whose copy into shared memory does not arrive within wait_limit_ms, and the rows
+ * that were to be copied behind it for the same CTA (or warp), are NaN in every output, as in the backward pass, and there
+ * also the sums that they are part of.
  */
 rola_status_t rola_residual_norm(const rola_residual_norm_config_t* cfg, const void* x, const void* h, const void* gate,
                                  const void* gamma_h, const void* gamma, const void* beta, const void* scale,

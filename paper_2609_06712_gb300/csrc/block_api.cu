@@ -292,6 +292,8 @@ rola_status_t validate(const rola_residual_norm_config_t* c)
     if (c->mod_stride != 0 && c->mod_stride < c->d) return ROLA_ERR_INVALID_ARG;
     if (!(c->eps >= 0.0f) || !isfinite(c->eps) || (c->dtype != ROLA_BF16 && c->dtype != ROLA_FP32))
         return ROLA_ERR_INVALID_ARG;
+    if (c->wait_limit_ms < 0 || c->wait_limit_ms > 60000) return ROLA_ERR_INVALID_ARG;
+    if (c->debug_flags & ~ROLA_DEBUG_SKIP_FIRST_K_COPY) return ROLA_ERR_INVALID_ARG;
     if (c->d > (1 << 20) || (int64_t)c->groups * c->rows > ((int64_t)1 << 40) / c->d) return ROLA_ERR_UNSUPPORTED;
     return ROLA_OK;
 }
@@ -304,6 +306,8 @@ RnShape make_shape(const rola_residual_norm_config_t& c)
     s.mod_stride = c.mod_stride ? c.mod_stride : c.d;
     s.total = (int64_t)c.groups * c.rows;
     s.eps = c.eps;
+    s.wait_limit_ns = wait_limit_ns(c.wait_limit_ms);
+    s.debug_flags = c.debug_flags;
     return s;
 }
 

@@ -220,7 +220,6 @@ constexpr int kWarpGroups = 4;                       // rows of a CTA whose rows
 constexpr int kMaxDepth = 16;                        // rows in a group's ring
 constexpr size_t kRingBytes = 208 << 10;             // of the rings of an SM's CTAs
 constexpr size_t kBarBytes = kWarpGroups * kMaxDepth * 8;
-constexpr uint64_t kWaitLimitNs = 2000000000ull;     // bound of the wait for a row
 
 // The elements of piece i of a thread's EL.
 template <int V, int EL>
@@ -253,12 +252,16 @@ __host__ __device__ __forceinline__ uint32_t place_bytes(int d, int esz, bool wi
 
 // A group's rows [next, end) of the matrices a.in (those that are not NULL), brought ahead into `depth` slots of shared
 // memory by bulk copies, one per matrix, with an mbarrier a slot.  A slot is refilled after its row has been read into
-// registers by the whole group.  Pieces of less than 16 bytes: rows that start at any element; they are copied with the whole 16-byte words that
-// they begin and end in, and where such a word is not all inside the matrix (its first and last row) element by element.
+// registers by the whole group.  A row that does not arrive is lost: it becomes NaN (the call has no status word).  A thread
+// that has waited in vain sees what is under way land, so long as it does within the limit once more, then waits no more, and
+// if it is the copying one issues no more copies: the group's rows behind those are lost too.
+// Pieces of less than 16 bytes: rows that start at any element; they are copied with the whole 16-byte words that they begin
+// and end in, and where such a word is not all inside the matrix (its first and last row) element by element.
 template <typename T, int V, int EL, int N, bool FULL>
 struct Feed {
     long long next, end;
     int tpr, gt, depth, slot, phase;
+    bool lost;                           // this thread has waited in vain
     uint32_t ring, bars, here, step;     // here: the present slot; step: bytes of a slot
 
     static __device__ __forceinline__ uint32_t place(const RnShape& sh) { return place_bytes(sh.d, sizeof(T), kWide<T, V>); }
@@ -342,17 +345,58 @@ struct Feed {
         here = ring;
         next = r0;
         slot = phase = 0;
+        lost = false;
         if (gt == 0) {
             for (int i = 0; i < depth; ++i) tc::mbar_init(bars + i * 8, 1);
             tc::fence_mbar_init();
+            int i = 0;
+            if (sh.debug_flags & ROLA_DEBUG_SKIP_FIRST_K_COPY) {     // test hook: the first row is never announced nor copied
+                ++next;
+                ++i;
+            }
 #pragma unroll 1
-            for (int i = 0; i < depth && next < end; ++i) copy(sh, a, i);
+            for (; i < depth && next < end; ++i) copy(sh, a, i);
         }
     }
-    __device__ __forceinline__ bool wait() const
+    // Until row r is in its slot, or NaN.
+    __device__ __forceinline__ void wait(const RnShape& sh, const RnArgs& a, long long r)
     {
-        int never = 0;
-        return tc::mbar_wait(bars + slot * 8, phase, &never, kWaitLimitNs);
+        if (!tc::mbar_try_wait(bars + slot * 8, phase)) wait_longer(sh, a, r);
+    }
+    __device__ __forceinline__ void wait_longer(const RnShape& sh, const RnArgs& a, long long r)
+    {
+        if (!lost) {
+            int gave_up = 0;
+            if (tc::mbar_wait(bars + slot * 8, phase, &gave_up, sh.wait_limit_ns)) return;
+            lost = true;
+            next = end;
+            int to = slot, parity = phase;
+#pragma unroll 1
+            for (int i = 0; i < depth; ++i) {
+                gave_up = 0;
+                tc::mbar_wait(bars + to * 8, parity, &gave_up, sh.wait_limit_ns / kMaxDepth);
+                if (++to == depth) {
+                    to = 0;
+                    parity ^= 1;
+                }
+            }
+        }
+        uint32_t row = here;                             // NaN in all that this thread reads of it
+#pragma unroll 1
+        for (int n = 0; n < N; ++n) {
+            if (!a.in[n]) continue;
+            const uint32_t at = row + offset(sh, a, n, r);
+#pragma unroll 1
+            for (int c = gt; c < sh.d / V; c += tpr) {
+                if constexpr (kWide<T, V>)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};\n" ::"r"(at + c * 16), "r"(0xffffffffu) : "memory");
+                else if constexpr (V * sizeof(T) == 4)
+                    asm volatile("st.shared.b32 [%0], %1;\n" ::"r"(at + c * 4), "r"(0xffffffffu) : "memory");
+                else
+                    asm volatile("st.shared.b16 [%0], %1;\n" ::"r"(at + c * 2), "h"((uint16_t)0xffff) : "memory");
+            }
+            row += place(sh);
+        }
     }
     // Row r of matrix n (`skip` bytes into a slot) as fp32, zeros where there is none.
     __device__ __forceinline__ void read(const RnShape& sh, const RnArgs& a, int n, uint32_t skip, long long r,
@@ -431,9 +475,6 @@ __device__ __forceinline__ void put_piece(T* p, const float (&v)[V])
     if constexpr (sizeof(T) == 2 && V == 2) *reinterpret_cast<uint32_t*>(p) = pack_bf16(v[0], v[1]);
     else store_piece<T, V>(p, v);
 }
-
-// Of a row whose copy never arrived (the call has no status word): NaN, in an element of each thread.
-#define kLost __int_as_float(0x7fc00000)
 
 // Sums of N = 1, 2, 4 or 8 values over the threads of a group, the same bits in every thread.  While a lane holds more
 // than one value a step hands half of them to the lane across and takes the others' (8 values take 9 shuffles, not
@@ -613,11 +654,10 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
         load_vectors<T, V, EL, true, FULL>(sh, a, s, q.gt, q.tpr, pieces, g, c, b);
 #pragma unroll 1
         for (; r < stop; ++r, at += sh.d) {
-            const bool ok = q.wait();
+            q.wait(sh, a, r);
             float u[EL], hh[EL];
             q.read(sh, a, 0, 0, r, u);
             q.read(sh, a, 1, place, r, hh);
-            if (!ok) u[0] = kLost;
             bool held = true;
             auto refill = [&]() {
                 if (!held) return;
@@ -688,13 +728,12 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpGroups : TH, MIN)
         for (; r < stop; ++r, at += sh.d) {
             const float4 now = st;
             if (r + 1 < q.end) st = reinterpret_cast<const float4*>(a.stats)[r + 1];
-            const bool ok = q.wait();
+            q.wait(sh, a, r);
             float v[EL], hh[EL], dy[EL], t[EL];
             q.read(sh, a, 0, 0, r, v);
             q.read(sh, a, 1, k1, r, hh);
             q.read(sh, a, 2, k2, r, dy);
             q.read(sh, a, 3, k3, r, t);
-            if (!ok) t[0] = hh[0] = kLost;
             bool held = true;
             auto refill = [&]() {
                 if (!held) return;

@@ -10,6 +10,8 @@ struct RnShape {
     int norm, branch;                // rola_norm_t of the sum and of the branch
     long long mod_stride, total;     // total: groups rows
     float eps;
+    int debug_flags;
+    uint64_t wait_limit_ns;          // of a row's copy
 };
 
 // Vectors that are not there are NULL.  Backward: part and moments are workspace.

@@ -72,7 +72,7 @@ class RolaLinearConfig(ctypes.Structure):
 class RolaResidualNormConfig(ctypes.Structure):
     """Mirror of rola_residual_norm_config_t."""
     _fields_ = [(n, ctypes.c_int32) for n in ("groups", "rows", "d", "norm", "branch_norm", "mod_stride")] + [
-        ("eps", ctypes.c_float), ("dtype", ctypes.c_int32)]
+        ("eps", ctypes.c_float)] + [(n, ctypes.c_int32) for n in ("dtype", "wait_limit_ms", "debug_flags")]
 
 
 ROLA_DEBUG_SKIP_FIRST_K_COPY = 1
