@@ -575,9 +575,11 @@ size_t rola_linear_workspace_bytes(const rola_linear_config_t* cfg);
 size_t rola_linear_backward_workspace_bytes(const rola_linear_config_t* cfg);
 
 /*
- * Linear layer with its epilogue, in one kernel:
+ * Linear layer with its epilogue:
  *   Z = X W^T + b,  Y = residual + phi(Z)
- * The sum over d_in, the bias, phi and the residual are fp32; Y is rounded once.
+ * One kernel; where few tiles have a long d_in its parts are joined by a second, which then has the epilogue.  The sum
+ * over d_in, the bias, phi and the residual are fp32; Y is rounded once.  GELU is the exact form (rola_lowrank_act_t):
+ * for weights trained with its tanh approximation it is another function, by up to 4.8e-4.
  *   X : [tokens][d_in];  W : [d_out][d_in] (the nn.Linear layout);  b : [d_out], or NULL (0), all cfg->dtype
  *   residual : [tokens][d_out], cfg->dtype, or NULL (0)
  *   Y : out, [tokens][d_out], cfg->dtype; may be residual, and overlaps no other argument

@@ -21,9 +21,10 @@
 // Few tiles with a long K axis (the weights' gradients: K is the token) are split along K; the parts go to the
 // workspace in fp32, and a second kernel adds them in order and finishes the outputs (launch_linear_join).
 //
-// Measured, bf16: 16380 x 5120 x 5120 with a residual 473 us (1815 TFLOP/s, 89 % of the tensor pipe), 32760 x 1536 x 4608 260 us
-// (1780), 8190 x 1536 x 6144 with GELU 106 us (1465), 514 x 4096 x 5120 with GELU 27 us.  What a large one lacks is the last
-// turn of tiles; what a small one lacks are its ends (some 5 us) and pairs without a tile.
+// Measured, bf16, between GPUs (whose power cap differs): 16380 x 5120 x 5120 with a residual 457 to 496 us (1732 to 1877
+// TFLOP/s, 89 % of the tensor pipe), 32760 x 1536 x 4608 254 to 270 us (1717 to 1825), 8190 x 1536 x 6144 with GELU 101 us
+// (1530), 514 x 4096 x 5120 with GELU 27 us.  What a large one lacks is the last turn of tiles; what a small one lacks are its
+// ends (some 5 us) and pairs without a tile.
 //
 // Every mbarrier wait is bounded; a wait that gives up records ROLA_ERR_TIMEOUT in the status word, and the CTA stops
 // issuing, lets what it issued complete, meets its pair and frees its TMEM.
@@ -481,7 +482,8 @@ cudaError_t product(const LinShape& s, const void* A, const void* B, int M, int 
 
 // Parts of the K axis of least cost.  A pair takes 0.3 us a step of 64 k and some 3 us at its ends that no other tile
 // covers; parts are written and read once more in fp32 at some 5 TB/s, and their join is a launch of 4 us.  76 pairs
-// run at once.  (Tiles of 256 x 128 are no way to more items: a step of theirs takes as long, 0.3 us at 32760 x 1536 x 1536.)
+// run at once.  (Tiles of 256 x 128 are no way to more items with steps of 64 k: a step of theirs takes as long, 0.3 us at
+// 32760 x 1536 x 1536, most of it its wait, its announcement and its commit.  Deeper steps were not tried.)
 int linear_splits(int64_t M, int64_t N, int64_t K)
 {
     const int64_t steps = (K + kStepK - 1) / kStepK, tiles = ((M + kTileM - 1) / kTileM) * ((N + kTileN - 1) / kTileN);

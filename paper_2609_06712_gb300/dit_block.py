@@ -8,9 +8,10 @@ The norms, both attentions and the feed-forward are this library's operators wit
 linear projections are torch's.  ``python -m paper_2609_06712_gb300.dit_block`` takes a few training steps on a
 small synthetic layer and prints the loss of each.
 
-With a conditioning vector (``d_cond``) the block is modulated by it, sample by sample, and everything in it is this
-library's: a linear layer makes two shifts, scales and gates, and each branch joins the stream through its gate in the
-kernel that also makes the next branch's input:
+With a conditioning vector (``d_cond``) the block is modulated by it, sample by sample, and its projections are this
+library's too (torch's are left: the conditioning's SiLU, and the copies of q, k and v into heads and back): a linear
+layer makes two shifts, scales and gates, and each branch joins the stream through its gate in the kernel that also
+makes the next branch's input:
 
     shift_1, scale_1, gate_1, shift_2, scale_2, gate_2 = W_mod SiLU(cond) + b_mod
     y = norm(x) (1 + scale_1) + shift_1
