@@ -624,7 +624,7 @@ typedef struct {
     float eps;                 /* of both norms, >= 0; default 1e-6 */
     rola_dtype_t dtype;        /* ROLA_BF16 (default) or ROLA_FP32 */
     int32_t wait_limit_ms;     /* bound of every device-side wait (0 = 2000 ms); at most 60000 */
-    int32_t debug_flags;       /* as rola_ffn_config_t (rows of over 16384 elements, backward 8192, wait for nothing) */
+    int32_t debug_flags;       /* as rola_ffn_config_t (rows too long for registers wait for nothing) */
 } rola_residual_norm_config_t;
 
 /* Fill *cfg with defaults (sizes zero).  Returns ROLA_ERR_INVALID_ARG on NULL. */
